@@ -51,6 +51,8 @@ typedef enum {
 enum { DIGEST_ACT_RELU = 0, DIGEST_ACT_IDENTITY = 1 };
 enum { DIGEST_PUSH_BOUNDARY = 0, DIGEST_PUSH_ALL_OWNED = 1 };
 enum { DIGEST_PULL_ROWS = 0, DIGEST_PULL_AGGREGATE = 1 };
+/* Element types of the calls that take them (all others are fp32). */
+enum { DIGEST_F32 = 0, DIGEST_BF16 = 1, DIGEST_F16 = 2 };
 
 /* Message describing the last non-OK status returned on this thread. */
 const char *digest_last_error(void);
@@ -430,6 +432,59 @@ digest_status digest_softmax_xent_static(int64_t n_rows, int32_t n_classes,
  */
 digest_status digest_sgd_average(float *w, const float *const *grads, int32_t n_grads,
                                  int64_t count, float lr, void *hip_stream);
+
+/*
+ * Layer norm between layers, with the activation behind it: over each of
+ * n_rows rows of `width` elements,
+ *   mean = (1/width) sum_c x_c,  var = (1/width) sum_c (x_c - mean)^2,
+ *   rstd = (var + eps)^-1/2,
+ *   y_c  = act((x_c - mean) rstd gain_c + shift_c)
+ * and the gradients of
+ *   D   = dy (identity) or dy 1[y > 0] (ReLU),  xh = (x - mean) rstd:
+ *   dx_c     = rstd (D_c gain_c - (1/width) sum_c D_c gain_c
+ *                    - xh_c (1/width) sum_c D_c gain_c xh_c)
+ *   dgain_c  = sum over the rows of D_c xh_c,  dshift_c = that of D_c.
+ * A layer of a normalised network is the layer call with
+ * DIGEST_ACT_IDENTITY followed by this one with the layer's activation.
+ *   n_rows   0 .. 2^31 - 2;  width 1 .. 65536.
+ *   type     element type of x, y, dy and dx (DIGEST_F32, _BF16, _F16); the
+ *            other arrays are fp32, and so is every sum.
+ *   x, y, dy, dx  device arrays of rows, each with its row stride in
+ *            elements (ldx, ldy, lddy, lddx: width .. 2^31 - 1); rows may
+ *            start at any element, what lies between them is left alone.
+ *            y may be x and dx may be dy (with the same stride); apart from
+ *            that outputs overlap nothing.
+ *   gain, shift  device [width]; NULL: ones, zeros.
+ *   eps      a positive normal number.
+ *   stats    device [n_rows][2], (mean, rstd) of each row, 8-byte aligned;
+ *            written by the forward (NULL: not kept), read by the backward.
+ * Every sum runs in a fixed order (equal calls give equal bits).  A row with
+ * a NaN or an infinity is NaN (through the ReLU too) and touches no other;
+ * rows whose squared deviations pass fp32's range come out as shift.
+ * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
+ */
+digest_status digest_layer_norm_forward(int64_t n_rows, int32_t width, int32_t type,
+                                        const void *x, int64_t ldx, const float *gain,
+                                        const float *shift, float eps, int32_t act, void *y,
+                                        int64_t ldy, float *stats, void *hip_stream);
+
+/* Bytes of the backward's workspace. */
+digest_status digest_layer_norm_query(int64_t n_rows, int32_t width, size_t *workspace_bytes);
+
+/*
+ * The backward.  y (the forward's output) is read with DIGEST_ACT_RELU only;
+ * dx, dgain and dshift may each be NULL (not wanted).  Without rows dgain
+ * and dshift are zero.  workspace: 256-byte aligned device memory of at
+ * least the queried bytes for the partial sums of dgain and dshift (NULL
+ * when neither is wanted); its contents need not be kept between calls, and
+ * calls that may overlap need one each.
+ */
+digest_status digest_layer_norm_backward(int64_t n_rows, int32_t width, int32_t type,
+                                         const void *x, int64_t ldx, const float *gain,
+                                         int32_t act, const void *y, int64_t ldy, const void *dy,
+                                         int64_t lddy, const float *stats, void *dx, int64_t lddx,
+                                         float *dgain, float *dshift, void *workspace,
+                                         size_t bytes, void *hip_stream);
 
 /*
  * Synchronisation schedule of Algorithm 1 (pure, host only): in round

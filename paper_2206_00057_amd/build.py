@@ -1,13 +1,14 @@
 """Build ``libdigest.so`` in-tree for gfx950.
 
-Host code (``csrc/digest_host.cpp``) is plain C++ built with g++ against the
-HIP runtime headers; the kernels (``csrc/digest_kernels.hip``) are built with
-hipcc for gfx950.  Packed-fp32 instructions are disabled for all GPU code.
+Host code (``HOST_SOURCES``) is plain C++ built with g++ against the HIP
+runtime headers; the kernels (``KERNEL_SOURCES``) are built with hipcc for
+gfx950.  Packed-fp32 instructions are disabled for all GPU code.
 
     python -m paper_2206_00057_amd.build
 """
 from __future__ import annotations
 
+import concurrent.futures
 import os
 import subprocess
 import sys
@@ -20,6 +21,8 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdigest.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
+HOST_SOURCES = ("digest_host", "digest_train")
+KERNEL_SOURCES = ("digest_kernels", "norm_kernels")
 
 HIPCC_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -42,14 +45,19 @@ def _run(cmd, verbose):
 
 def build(verbose: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
-    host_o = os.path.join(BUILD, "digest_host.o")
-    kern_o = os.path.join(BUILD, "digest_kernels.o")
-    _run(["g++", *CXX_FLAGS, "-c", os.path.join(CSRC, "digest_host.cpp"), "-o", host_o], verbose)
-    _run([os.path.join(ROCM, "bin", "hipcc"), *HIPCC_FLAGS, "-c",
-          os.path.join(CSRC, "digest_kernels.hip"), "-o", kern_o], verbose)
+    jobs, objs = [], []
+    for name in HOST_SOURCES:
+        objs.append(os.path.join(BUILD, name + ".o"))
+        jobs.append(["g++", *CXX_FLAGS, "-c", os.path.join(CSRC, name + ".cpp"), "-o", objs[-1]])
+    for name in KERNEL_SOURCES:
+        objs.append(os.path.join(BUILD, name + ".o"))
+        jobs.append([os.path.join(ROCM, "bin", "hipcc"), *HIPCC_FLAGS, "-c",
+                     os.path.join(CSRC, name + ".hip"), "-o", objs[-1]])
+    with concurrent.futures.ThreadPoolExecutor(len(jobs)) as pool:
+        list(pool.map(lambda cmd: _run(cmd, verbose), jobs))
     tmp = LIB + f".tmp{os.getpid()}"
     _run([os.path.join(ROCM, "bin", "hipcc"), f"--offload-arch={ARCH}", "-shared", "-fPIC",
-          host_o, kern_o, "-o", tmp], verbose)
+          *objs, "-o", tmp], verbose)
     os.replace(tmp, LIB)
     return LIB
 

@@ -1,8 +1,8 @@
 """Host-only sanitizer build of the C ABI (AddressSanitizer + UBSan).
 
-The host code (``csrc/digest_host.cpp``: argument checks, the partition's
+The host code (``build.HOST_SOURCES``: argument checks, the partition's
 index maps, workspace layout, launch planning) is compiled by g++ with the
-sanitizers and linked with the ordinary gfx950 kernel object into
+sanitizers and linked with the ordinary gfx950 kernel objects into
 ``_build/libdigest_host_sanitized.so``.  No GPU code is built with a
 sanitizer.  The library is for CPU-side runs only (creating, querying and
 exporting partitions, every error path); load it with the sanitizer runtimes
@@ -38,15 +38,17 @@ def runtime_preload() -> str:
 
 def build(verbose: bool = False) -> str:
     os.makedirs(B.BUILD, exist_ok=True)
-    kern_o = os.path.join(B.BUILD, "digest_kernels.o")
-    if not os.path.exists(kern_o):
+    kern_o = [os.path.join(B.BUILD, name + ".o") for name in B.KERNEL_SOURCES]
+    if not all(os.path.exists(o) for o in kern_o):
         B.build(verbose)
-    host_o = os.path.join(B.BUILD, "digest_host_sanitized.o")
     flags = [f for f in B.CXX_FLAGS if f != "-O2"] + ["-O1", "-g"] + SANITIZERS
-    B._run(["g++", *flags, "-c", os.path.join(B.CSRC, "digest_host.cpp"), "-o", host_o],
-           verbose)
+    host_o = []
+    for name in B.HOST_SOURCES:
+        host_o.append(os.path.join(B.BUILD, name + "_sanitized.o"))
+        B._run(["g++", *flags, "-c", os.path.join(B.CSRC, name + ".cpp"), "-o", host_o[-1]],
+               verbose)
     tmp = LIB + f".tmp{os.getpid()}"
-    B._run(["g++", "-shared", *SANITIZERS, host_o, kern_o, "-o", tmp,
+    B._run(["g++", "-shared", *SANITIZERS, *host_o, *kern_o, "-o", tmp,
             "-L", os.path.join(B.ROCM, "lib"), "-lamdhip64",
             f"-Wl,-rpath,{os.path.join(B.ROCM, 'lib')}"], verbose)
     os.replace(tmp, LIB)

@@ -3,6 +3,7 @@
 // workspace layout, and the launch sequence of each C-ABI call.
 #include "digest.h"
 #include "kernels.h"
+#include "status.h"
 
 #include <hip/hip_runtime_api.h>
 
@@ -17,11 +18,17 @@
 #include <string>
 #include <vector>
 
+using digest::fail;
+using digest::hip_check;
 using digest::SpmmBlock;
 
 namespace {
 
 thread_local std::string g_last_error;
+
+}  // namespace
+
+namespace digest {
 
 digest_status fail(digest_status st, const char *fmt, ...)
 {
@@ -33,6 +40,17 @@ digest_status fail(digest_status st, const char *fmt, ...)
     g_last_error = buf;
     return st;
 }
+
+digest_status hip_check(hipError_t e, const char *what)
+{
+    if (e != hipSuccess)
+        return fail(DIGEST_EHIP, "%s: %s", what, hipGetErrorString(e));
+    return DIGEST_OK;
+}
+
+}  // namespace digest
+
+namespace {
 
 // Kernel kinds reported by the instrumentation.
 enum Kind : int32_t {
@@ -956,13 +974,6 @@ struct Timed {
             (void)hipEventRecord(b, s);
     }
 };
-
-digest_status hip_check(hipError_t e, const char *what)
-{
-    if (e != hipSuccess)
-        return fail(DIGEST_EHIP, "%s: %s", what, hipGetErrorString(e));
-    return DIGEST_OK;
-}
 
 // Weight gradients of at least this many flops run on the side stream,
 // concurrently with the input-gradient chain (smaller ones lose more to the

@@ -41,6 +41,7 @@
 #include <utility>
 #include <vector>
 
+#include "device.h"
 #include "kernels.h"
 
 // The library's fixed scratch array for callers that cannot allocate
@@ -52,22 +53,6 @@ static __device__ __align__(256) float scratch[digest::kStaticScratchFloats];
 
 namespace digest {
 namespace {
-
-constexpr int kWave = 64;
-
-// The dispatcher deals workgroups to the 8 XCDs (each with its own L2) in
-// turn by linear id.  xcd_contiguous maps the linear id p of an n-workgroup
-// grid to a logical id such that every XCD receives one contiguous run of
-// logical ids, in increasing order; it is a bijection of [0, n).  Kernels
-// order their logical work so that neighbours share operand data.
-constexpr uint32_t kXcds = 8;
-
-__device__ __forceinline__ uint32_t xcd_contiguous(uint32_t p, uint32_t n)
-{
-    const uint32_t q = n / kXcds, rem = n % kXcds;
-    const uint32_t x = p % kXcds, slot = p / kXcds;
-    return (x < rem ? x * (q + 1) : rem * (q + 1) + (x - rem) * q) + slot;
-}
 
 template <int VEC>
 __device__ __forceinline__ void load_vec(const float *p, float (&x)[VEC])
@@ -1060,15 +1045,6 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
-
-// A workgroup barrier for data in LDS alone: __syncthreads() also waits for
-// the global loads in flight, which are the next tiles.
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
 
 // Eight floats as the sums of three bf16 each, kSplitScale x = h + m + l: h is
 // x rounded to bf16, m what is left rounded, l what is left then (each step's

@@ -23,6 +23,7 @@ MODEL_GCN, MODEL_GAT = 0, 1
 ACT_RELU, ACT_IDENTITY = 0, 1
 PUSH_BOUNDARY, PUSH_ALL_OWNED = 0, 1
 PULL_ROWS, PULL_AGGREGATE = 0, 1
+F32, BF16, F16 = 0, 1, 2
 
 _lib = None
 
@@ -82,6 +83,31 @@ def lib():
             f.restype = res
         _lib = L
     return _lib
+
+
+_train = None
+
+
+def _train_lib():
+    """The library with the operators that belong to no partition (layer norm);
+    raises if this build of the ABI lacks them."""
+    global _train
+    if _train is None or _train is not lib():
+        L = lib()
+        P, i32, i64, sz, f32 = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t,
+                                ctypes.c_float)
+        sig = {
+            "digest_layer_norm_query": [i64, i32, P],
+            "digest_layer_norm_forward": [i64, i32, i32, P, i64, P, P, f32, i32, P, i64, P, P],
+            "digest_layer_norm_backward": [i64, i32, i32, P, i64, P, i32, P, i64, P, i64, P, P,
+                                           i64, P, P, P, sz, P],
+        }
+        for name, args in sig.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = ctypes.c_int
+        _train = L
+    return _train
 
 
 def _check(status):
@@ -472,3 +498,102 @@ def digest_profile_model(p, model=MODEL_GCN):
             if b[j] or f[j] or e[j]:
                 out[f"{name}.l{sl}"] = (float(b[j]), float(f[j]), int(e[j]))
     return out
+
+
+# Operators that belong to no partition: layer norm.
+
+def _here(t, name):
+    """t is a tensor on the current device (where the kernels run)."""
+    import torch
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+
+
+def _elem_type(t, name):
+    import torch
+    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    if t.dtype not in types:
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return types[t.dtype]
+
+
+def _rows(t, like, name):
+    """(pointer, row stride) of a 2-D tensor of the shape and type of ``like``
+    whose rows are contiguous."""
+    _here(t, name)
+    if t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name} must be {list(like.shape)}, got {list(t.shape)}")
+    if t.dtype != like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    n, d = t.shape
+    if d > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: the elements of a row must be contiguous")
+    ld = t.stride(0) if n > 1 else d
+    if ld < d:
+        raise ValueError(f"{name}: rows must not overlap")
+    return ctypes.c_void_p(t.data_ptr()), ld
+
+
+def _vector(t, numel, name):
+    import torch
+    if t is None:
+        return None
+    _here(t, name)
+    return _dev(t, torch.float32, numel, name)
+
+
+def _workspace(t):
+    import torch
+    if t is None:
+        return None, 0
+    _here(t, "workspace")
+    if not t.is_contiguous():
+        raise ValueError("workspace must be contiguous")
+    return ctypes.c_void_p(t.data_ptr()), t.numel() * t.element_size()
+
+
+def digest_layer_norm_query(n_rows, width):
+    """Bytes of the layer norm backward's workspace."""
+    out = ctypes.c_size_t(0)
+    _check(_train_lib().digest_layer_norm_query(int(n_rows), int(width), ctypes.byref(out)))
+    return int(out.value)
+
+
+def digest_layer_norm_forward(x, gain, shift, y, stats=None, eps=1e-5, act=ACT_IDENTITY,
+                              stream=None):
+    """y = act(layer norm of each row of x [n, d]); gain, shift float32 [d] or
+    None; stats float32 [n, 2] keeps (mean, rstd) for the backward."""
+    _here(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [n, d]")
+    n, d = x.shape
+    px, ldx = _rows(x, x, "x")
+    py, ldy = _rows(y, x, "y")
+    _check(_train_lib().digest_layer_norm_forward(
+        n, d, _elem_type(x, "x"), px, ldx, _vector(gain, d, "gain"), _vector(shift, d, "shift"),
+        float(eps), int(act), py, ldy, _vector(stats, 2 * n, "stats"), _stream(stream)))
+
+
+def digest_layer_norm_backward(x, gain, y, dy, stats, dx, dgain, dshift, workspace,
+                               act=ACT_IDENTITY, stream=None):
+    """dx, dgain, dshift of digest_layer_norm_forward (each may be None); y, its
+    output, is read with ACT_RELU only; workspace: a CUDA tensor of at least
+    digest_layer_norm_query(n, d) bytes (None without dgain and dshift)."""
+    _here(x, "x")
+    if x.dim() != 2:
+        raise ValueError("x must be [n, d]")
+    n, d = x.shape
+    px, ldx = _rows(x, x, "x")
+    py, ldy = _rows(y, x, "y") if act == ACT_RELU else (None, 0)
+    pdy, lddy = _rows(dy, x, "dy")
+    pdx, lddx = _rows(dx, x, "dx") if dx is not None else (None, 0)
+    ws, nbytes = _workspace(workspace)
+    if stats is None:
+        raise ValueError("stats is required")
+    _check(_train_lib().digest_layer_norm_backward(
+        n, d, _elem_type(x, "x"), px, ldx, _vector(gain, d, "gain"), int(act), py, ldy, pdy, lddy,
+        _vector(stats, 2 * n, "stats"), pdx, lddx, _vector(dgain, d, "dgain"),
+        _vector(dshift, d, "dshift"), ws, nbytes, _stream(stream)))
