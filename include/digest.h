@@ -487,6 +487,67 @@ digest_status digest_layer_norm_backward(int64_t n_rows, int32_t width, int32_t 
                                          size_t bytes, void *hip_stream);
 
 /*
+ * Orthogonalised matrices by Newton-Schulz products: for each of `count`
+ * matrices U (rows[i] x cols[i], HOST arrays),
+ *   X_0 = U / |U|_F  (U = 0: X_0 = 0),
+ *   X  <- a X + b (X X^T) X + c (X X^T)^2 X   for each step,  out = X,
+ * an odd polynomial of U's singular values with its singular vectors kept:
+ * with the default coefficients (a, b, c) = (3.4445, -4.7750, 2.0315) and 5
+ * steps (the Muon optimiser) they come out between about 0.7 and 1.2.
+ *   count    1 .. 256;  rows, cols 1 .. 65536, each matrix its own.
+ *   type     element type of in and out.  The products have fp32 accuracy
+ *            whatever the type (each operand as two fp16 of 22 bits
+ *            together, sums in fp32), and the result is rounded once.
+ *   in, out  HOST arrays of device pointers to row-major matrices, with
+ *            HOST arrays of row strides in elements (cols[i] .. 2^31 - 1;
+ *            NULL: contiguous).  out[i] may be in[i] with the same stride;
+ *            apart from that outputs overlap neither inputs nor each other.
+ *   steps    1 .. 64;  coeffs HOST [steps][3] (NULL: the default in each
+ *            step).  The bounds of the singular values must stay within
+ *            2^-20 .. 2^20.
+ *   workspace  256-byte aligned device memory of at least the queried bytes
+ *            (digest_orthogonalize_query: for the same list of sizes, this
+ *            call and digest_muon_average); nothing is kept in it between
+ *            calls, and calls that may overlap need one each.
+ * A matrix with a NaN or an infinity comes out as NaN throughout and touches
+ * no other.  Equal calls give equal bits.
+ * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
+ */
+digest_status digest_orthogonalize_query(int32_t count, const int32_t *rows, const int32_t *cols,
+                                         size_t *workspace_bytes);
+digest_status digest_orthogonalize(int32_t count, const int32_t *rows, const int32_t *cols,
+                                   int32_t type, const void *const *in, const int64_t *ld_in,
+                                   void *const *out, const int64_t *ld_out, int32_t steps,
+                                   const float *coeffs, void *workspace, size_t bytes,
+                                   void *hip_stream);
+
+/*
+ * Global parameter update of Algorithm 1 with the Muon optimiser in place of
+ * the plain step of digest_sgd_average, for the weight matrices W_i of
+ * `count` layers at once:
+ *   g   = (1/M) sum_{m < M} grads[i M + m]          (in m order)
+ *   mom <- beta mom + g;   u = g + beta mom (nesterov) or mom
+ *   W   <- (1 - lr decay) W - lr scales[i] O(u),
+ * O the orthogonalised matrix of digest_orthogonalize (steps, coeffs as
+ * there).
+ *   w, momentum  HOST arrays of `count` device pointers, row-major
+ *            contiguous fp32, updated in place; no two of them overlap.
+ *   grads    HOST array of count * n_grads device pointers (matrix i's M
+ *            gradients from i M on), not modified, overlapping neither.
+ *   n_grads  M, 1 .. 64, the same for every matrix.
+ *   scales   HOST [count] (NULL: ones), e.g. sqrt(max(1, cols / rows)) for
+ *            weights that map rows to cols.
+ * A matrix with a gradient or momentum that is not finite becomes NaN.
+ * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
+ */
+digest_status digest_muon_average(int32_t count, const int32_t *rows, const int32_t *cols,
+                                  float *const *w, float *const *momentum,
+                                  const float *const *grads, int32_t n_grads, float lr, float beta,
+                                  float decay, const float *scales, int32_t nesterov,
+                                  int32_t steps, const float *coeffs, void *workspace,
+                                  size_t bytes, void *hip_stream);
+
+/*
  * Synchronisation schedule of Algorithm 1 (pure, host only): in round
  * iter (1-based) with interval K >= 1, *do_pull = (iter mod K == 0) and
  * *do_push = ((iter-1) mod K == 0); both apply to levels 1..L-1.

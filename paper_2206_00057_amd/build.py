@@ -22,7 +22,7 @@ LIB = os.path.join(PKG, "libdigest.so")
 ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 ARCH = "gfx950"
 HOST_SOURCES = ("digest_host", "digest_train")
-KERNEL_SOURCES = ("digest_kernels", "norm_kernels")
+KERNEL_SOURCES = ("digest_kernels", "norm_kernels", "orth_kernels")
 
 HIPCC_FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
                "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

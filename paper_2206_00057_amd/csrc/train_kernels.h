@@ -28,4 +28,56 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
                                 int64_t lddx, float *dgain, float *dshift, float *part,
                                 hipStream_t s);
 
+// Orthogonalised matrices: X_0 = U / |U|_F, then steps of
+// X <- (a I + b A + c A^2) X with A = X X^T, for X wide (r <= c; a tall U is
+// worked on as its transpose).  X, its transpose, A and B = a I + b A + c A^2
+// lie in memory as split planes: each value times a power of two as the sum
+// of two fp16, in rows whose k runs in blocks of 32, 32 high parts and then 32
+// low parts (one 128-byte line).  Rows are padded to kOrthTile, k to
+// kOrthPadK, with zeros.
+constexpr int kOrthItems = 16;       // matrices of one launch
+constexpr int kOrthGrads = 192;      // gradient pointers of one launch (its arguments stay below 4 KB)
+constexpr int kOrthTile = 128;
+constexpr int kOrthPadK = 64;
+constexpr int kOrthSumBlocks = 256;  // partial sums of |U|_F^2, at most
+constexpr int64_t kOrthSumRun = 4096;
+
+struct OrthItem {
+    int32_t rows, cols;              // of U and of the result
+    int32_t r, c, rp, cp, rk, ck;    // of X: sides, rows padded, k padded
+    const void *u;                   // U: the caller's, or fp32 in the workspace (muon)
+    void *out;                       // the result, or the weights (muon)
+    int64_t ldu, ldo;
+    float *mom;                      // muon: momentum, in place
+    float scale;                     // muon: w <- keep w - scale O
+    int32_t sums;                    // partial sums in part
+    double *part;
+    uint16_t *X, *Xt[2], *A, *B;
+};
+struct OrthBatch {
+    int32_t n;
+    OrthItem item[kOrthItems];
+};
+struct OrthGrads {
+    const float *g[kOrthGrads];      // item i: g[i * per_item ..]
+};
+// Scale exponents of one step: planes hold value * 2^e.
+struct OrthStep {
+    float a, b, c;
+    int32_t ex, ea, eb, en;          // X, A, B, and X after the step
+    int32_t from;                    // Xt[from] is read, Xt[from ^ 1] written
+};
+// part: sums of squares of U.
+hipError_t launch_orth_sum(const OrthBatch &b, int32_t type, hipStream_t s);
+// mom <- beta mom + g, u <- (nesterov ? g + beta mom : mom) with g the mean of
+// the item's gradients, and part as above.
+hipError_t launch_muon_momentum(const OrthBatch &b, const OrthGrads &g, int32_t per_item,
+                                float beta, bool nesterov, hipStream_t s);
+// X and Xt[0] from U: U / |U|_F * 2^e (zero for U = 0).
+hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStream_t s);
+// One step.  last: the result goes to out, as `type`, or (muon) into the
+// weights: out <- keep out - scale O.
+hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
+                            int32_t type, float keep, hipStream_t s);
+
 }  // namespace digest

@@ -89,8 +89,8 @@ _train = None
 
 
 def _train_lib():
-    """The library with the operators that belong to no partition (layer norm);
-    raises if this build of the ABI lacks them."""
+    """The library with the operators that belong to no partition (layer norm,
+    orthogonalised updates); raises if this build of the ABI lacks them."""
     global _train
     if _train is None or _train is not lib():
         L = lib()
@@ -101,6 +101,10 @@ def _train_lib():
             "digest_layer_norm_forward": [i64, i32, i32, P, i64, P, P, f32, i32, P, i64, P, P],
             "digest_layer_norm_backward": [i64, i32, i32, P, i64, P, i32, P, i64, P, i64, P, P,
                                            i64, P, P, P, sz, P],
+            "digest_orthogonalize_query": [i32, P, P, P],
+            "digest_orthogonalize": [i32, P, P, i32, P, P, P, P, i32, P, P, sz, P],
+            "digest_muon_average": [i32, P, P, P, P, P, i32, f32, f32, f32, P, i32, i32, P, P, sz,
+                                    P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -500,7 +504,7 @@ def digest_profile_model(p, model=MODEL_GCN):
     return out
 
 
-# Operators that belong to no partition: layer norm.
+# Operators that belong to no partition: layer norm, orthogonalised updates.
 
 def _here(t, name):
     """t is a tensor on the current device (where the kernels run)."""
@@ -597,3 +601,98 @@ def digest_layer_norm_backward(x, gain, y, dy, stats, dx, dgain, dshift, workspa
         n, d, _elem_type(x, "x"), px, ldx, _vector(gain, d, "gain"), int(act), py, ldy, pdy, lddy,
         _vector(stats, 2 * n, "stats"), pdx, lddx, _vector(dgain, d, "dgain"),
         _vector(dshift, d, "dshift"), ws, nbytes, _stream(stream)))
+
+
+MUON_COEFFS = (3.4445, -4.7750, 2.0315)   # the default odd polynomial of each step
+
+
+def _sides(shapes):
+    n = len(shapes)
+    return ((ctypes.c_int32 * n)(*[int(s[0]) for s in shapes]),
+            (ctypes.c_int32 * n)(*[int(s[1]) for s in shapes]))
+
+
+def _coeffs(coeffs, steps):
+    """None, (a, b, c) for every step, or one triple per step."""
+    if coeffs is None:
+        return None
+    if not any(hasattr(c, "__len__") for c in coeffs):
+        coeffs = [coeffs] * int(steps)
+    if len(coeffs) != int(steps) or any(len(c) != 3 for c in coeffs):
+        raise ValueError("coeffs must be (a, b, c) or one triple per step")
+    flat = [float(v) for c in coeffs for v in c]
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def digest_orthogonalize_query(shapes):
+    """Bytes of the workspace of digest_orthogonalize and digest_muon_average
+    for matrices of these (rows, cols)."""
+    if not len(shapes):
+        raise ValueError("need at least one matrix")
+    rows, cols = _sides(shapes)
+    out = ctypes.c_size_t(0)
+    _check(_train_lib().digest_orthogonalize_query(len(shapes), rows, cols, ctypes.byref(out)))
+    return int(out.value)
+
+
+def digest_orthogonalize(mats, outs, workspace, steps=5, coeffs=None, stream=None):
+    """outs[i] = the orthogonalised matrix of mats[i] (2-D, one dtype); outs may
+    be mats; workspace: a CUDA tensor of at least digest_orthogonalize_query
+    bytes for the same shapes."""
+    n = len(mats)
+    if n < 1 or len(outs) != n:
+        raise ValueError("need as many outputs as matrices, and one at least")
+    _here(mats[0], "mats[0]")
+    kind = _elem_type(mats[0], "mats[0]")
+    ins, outp = [], []
+    for i, (m, o) in enumerate(zip(mats, outs)):
+        _here(m, f"mats[{i}]")
+        if m.dim() != 2 or 0 in m.shape:
+            raise ValueError(f"mats[{i}] must be a matrix with rows and columns")
+        if m.dtype != mats[0].dtype:
+            raise TypeError(f"mats[{i}] must be {mats[0].dtype}, got {m.dtype}")
+        ins.append(_rows(m, m, f"mats[{i}]"))
+        outp.append(_rows(o, m, f"outs[{i}]"))
+    rows, cols = _sides([m.shape for m in mats])
+    ptrs, lds = ctypes.c_void_p * n, ctypes.c_int64 * n
+    ws, nbytes = _workspace(workspace)
+    _check(_train_lib().digest_orthogonalize(
+        n, rows, cols, kind, ptrs(*[p.value for p, _ in ins]), lds(*[l for _, l in ins]),
+        ptrs(*[p.value for p, _ in outp]), lds(*[l for _, l in outp]), int(steps),
+        _coeffs(coeffs, steps), ws, nbytes, _stream(stream)))
+
+
+def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0, scales=None,
+                        nesterov=True, steps=5, coeffs=None, stream=None):
+    """The Muon update of the weight matrices ws (with their momenta, float32,
+    in place) by the mean of each one's gradients: grads[i] lists the M
+    gradients of ws[i]."""
+    import torch
+    n = len(ws)
+    if n < 1 or len(momenta) != n or len(grads) != n:
+        raise ValueError("need a momentum and a list of gradients for each matrix, and one at "
+                         "least")
+    M = len(grads[0])
+    if M < 1 or any(len(g) != M for g in grads):
+        raise ValueError("need the same number of gradients for each matrix, and one at least")
+    if scales is not None and len(scales) != n:
+        raise ValueError("need one scale for each matrix")
+    flat = {"ws": [], "momenta": [], "grads": []}
+    for i, w in enumerate(ws):
+        _here(w, f"ws[{i}]")
+        if w.dim() != 2 or 0 in w.shape:
+            raise ValueError(f"ws[{i}] must be a matrix with rows and columns")
+        for name, ts in (("ws", [w]), ("momenta", [momenta[i]]), ("grads", grads[i])):
+            for t in ts:
+                _here(t, f"{name}[{i}]")
+                if t.shape != w.shape:
+                    raise ValueError(f"{name}[{i}] must be {list(w.shape)}, got {list(t.shape)}")
+                flat[name].append(_dev(t, torch.float32, w.numel(), f"{name}[{i}]").value)
+    rows, cols = _sides([w.shape for w in ws])
+    arr = lambda v: (ctypes.c_void_p * len(v))(*v)
+    work, nbytes = _workspace(workspace)
+    _check(_train_lib().digest_muon_average(
+        n, rows, cols, arr(flat["ws"]), arr(flat["momenta"]), arr(flat["grads"]), M, float(lr),
+        float(beta), float(decay),
+        (ctypes.c_float * n)(*[float(v) for v in scales]) if scales is not None else None,
+        int(bool(nesterov)), int(steps), _coeffs(coeffs, steps), work, nbytes, _stream(stream)))

@@ -48,3 +48,89 @@ def test_layer_norm_query():
     for n, d in ((-1, 8), (4, 0), (4, 65537), (2 ** 31 - 1, 8)):
         with pytest.raises(D.DigestError):
             q(n, d)
+
+
+def _i32(*v):
+    return (ctypes.c_int32 * len(v))(*v)
+
+
+def _i64(*v):
+    return (ctypes.c_int64 * len(v))(*v)
+
+
+def _f32(*v):
+    return (ctypes.c_float * len(v))(*v)
+
+
+def _ptrs(*v):
+    return (ctypes.c_void_p * len(v))(*v)
+
+
+P = [(i + 1) << 20 for i in range(12)]   # fake addresses, a megabyte apart
+
+
+def test_orthogonalize_refuses():
+    L = D._train_lib()
+
+    def call(n=2, rows=_i32(4, 8), cols=_i32(8, 4), t=D.F32, ins=_ptrs(P[0], P[1]), ldi=None,
+             outs=_ptrs(P[2], P[3]), ldo=None, steps=5, coeffs=None, ws=FAKE, nbytes=1 << 30):
+        return L.digest_orthogonalize(n, rows, cols, t, ins, ldi, outs, ldo, steps, coeffs, ws,
+                                      nbytes, None)
+
+    for kw in [dict(n=0), dict(n=-1), dict(n=257), dict(rows=None), dict(cols=None),
+               dict(rows=_i32(0, 8)), dict(cols=_i32(8, 65537)), dict(t=3), dict(ins=None),
+               dict(outs=None), dict(ins=_ptrs(P[0], None)), dict(ins=_ptrs(P[0] + 2, P[1])),
+               dict(outs=_ptrs(P[2], P[3] + 1)), dict(ldi=_i64(7, 4)), dict(ldo=_i64(8, 3)),
+               dict(ldi=_i64(8, 2 ** 31)), dict(outs=_ptrs(P[2], P[2])), dict(steps=0),
+               dict(steps=65), dict(steps=1, coeffs=_f32(float("nan"), 0, 0)),
+               dict(steps=1, coeffs=_f32(1, float("inf"), 0)),
+               dict(steps=1, coeffs=_f32(0, 0, 0)),               # nothing is left
+               dict(steps=2, coeffs=_f32(1e4, 0, 0, 1e4, 0, 0)),  # grows out of range
+               dict(ws=None), dict(ws=ctypes.c_void_p((1 << 20) + 64))]:
+        assert call(**kw) == D.EINVAL, kw
+    need = D.digest_orthogonalize_query([(4, 8), (8, 4)])
+    assert call(nbytes=need - 1) == D.ENOMEM
+
+
+def test_muon_refuses():
+    L = D._train_lib()
+
+    def call(n=2, rows=_i32(4, 8), cols=_i32(8, 4), w=_ptrs(P[0], P[1]), mom=_ptrs(P[2], P[3]),
+             grads=_ptrs(P[4], P[5], P[6], P[7]), m=2, steps=5, coeffs=None, ws=FAKE,
+             nbytes=1 << 30):
+        return L.digest_muon_average(n, rows, cols, w, mom, grads, m, 0.1, 0.9, 0.0, None, 1,
+                                     steps, coeffs, ws, nbytes, None)
+
+    for kw in [dict(n=0), dict(n=257), dict(rows=None), dict(rows=_i32(4, 0)), dict(m=0),
+               dict(m=65), dict(w=None), dict(mom=None), dict(grads=None),
+               dict(w=_ptrs(P[0], None)), dict(mom=_ptrs(P[2], P[3] + 1)),
+               dict(grads=_ptrs(P[4], P[5], None, P[7])), dict(steps=0),
+               dict(w=_ptrs(P[0], P[0])),                         # one weight twice
+               dict(w=_ptrs(P[0], P[0] + 124)),                   # overlapping by 4 bytes
+               dict(mom=_ptrs(P[0], P[3])),                       # a momentum on a weight
+               dict(grads=_ptrs(P[4], P[5], P[6], P[3] + 64)),    # a gradient on a momentum
+               dict(grads=_ptrs(P[0] - 124, P[5], P[6], P[7])),   # its end on a weight
+               dict(ws=None)]:
+        assert call(**kw) == D.EINVAL, kw
+    need = D.digest_orthogonalize_query([(4, 8), (8, 4)])
+    assert call(nbytes=need - 1) == D.ENOMEM
+    # side by side, and gradients shared, are fine: refused for the workspace alone
+    assert call(w=_ptrs(P[0], P[0] + 128), mom=_ptrs(P[0] + 256, P[0] + 384),
+                grads=_ptrs(*[P[0] + 512] * 4), nbytes=0) == D.ENOMEM
+
+
+def test_orthogonalize_query():
+    q = D.digest_orthogonalize_query
+    # five planes of 4 bytes an element, padded: at most 128 x 128 more each side
+    for shapes in ([(1, 1)], [(64, 16)], [(256, 602)], [(4096, 4096)], [(7, 9000), (40, 40)]):
+        b = q(shapes)
+        low = sum(4 * (3 * r * c + 2 * min(r, c) ** 2) for r, c in shapes)
+        up = lambda v: v + 256
+        high = sum(4 * (3 * up(r) * up(c) + 2 * up(min(r, c)) ** 2) + 8192 for r, c in shapes)
+        assert b % 256 == 0 and low <= b <= high, (shapes, b)
+    # groups of sixteen share their memory
+    assert q([(100, 100)] * 40) == q([(100, 100)] * 16)
+    with pytest.raises(D.DigestError):
+        q([(0, 4)])
+    with pytest.raises(ValueError):
+        q([])
