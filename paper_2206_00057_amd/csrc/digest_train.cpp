@@ -123,8 +123,7 @@ size_t place(OrthItem &it, int32_t rows, int32_t cols, char *base)
 {
     it.rows = rows, it.cols = cols;
     it.r = std::min(rows, cols), it.c = std::max(rows, cols);
-    it.rp = pad(it.r, digest::kOrthTile), it.cp = pad(it.c, digest::kOrthTile);
-    it.rk = pad(it.r, digest::kOrthPadK), it.ck = pad(it.c, digest::kOrthPadK);
+    it.rp = it.rk = pad(it.r, digest::kOrthPad), it.cp = it.ck = pad(it.c, digest::kOrthPad);
     it.sums = (int32_t)std::min<int64_t>(
         digest::kOrthSumBlocks,
         ((int64_t)rows * cols + digest::kOrthSumRun - 1) / digest::kOrthSumRun);
@@ -161,12 +160,11 @@ size_t orth_workspace(int32_t count, const int32_t *rows, const int32_t *cols)
 {
     size_t most = 0;
     for (int32_t i = 0; i < count; i += digest::kOrthItems) {
+        OrthBatch b{};
         size_t bytes = 0;
-        for (int32_t j = i; j < std::min(count, i + digest::kOrthItems); ++j) {
-            OrthItem it;
-            bytes += place(it, rows[j], cols[j], nullptr);
-        }
-        most = std::max(most, bytes);
+        for (int32_t j = i; j < std::min(count, i + digest::kOrthItems); ++j)
+            bytes += place(b.item[b.n++], rows[j], cols[j], nullptr);
+        most = std::max(most, bytes + align_up(digest::orth_partials(b)));
     }
     return most;
 }
@@ -216,14 +214,15 @@ digest_status plan_steps(int32_t steps, const float *coeffs, OrthStep *out)
 }
 
 digest_status run_steps(const OrthBatch &batch, const OrthStep *plan, int32_t steps, bool muon,
-                        int32_t type, float keep, hipStream_t s)
+                        int32_t type, float keep, void *partials, hipStream_t s)
 {
     if (digest_status st = hip_check(
             digest::launch_orth_split(batch, muon ? DIGEST_F32 : type, plan[0].ex, s), "split"))
         return st;
     for (int32_t k = 0; k < steps; ++k)
         if (digest_status st = hip_check(digest::launch_orth_step(batch, plan[k], k + 1 == steps,
-                                                                  muon, type, keep, s),
+                                                                  muon, type, keep,
+                                                                  (float *)partials, s),
                                          "orthogonalisation step"))
             return st;
     return DIGEST_OK;
@@ -386,7 +385,7 @@ digest_status digest_orthogonalize(int32_t count, const int32_t *rows, const int
         }
         if (digest_status st = hip_check(digest::launch_orth_sum(batch, type, s), "norm"))
             return st;
-        if (digest_status st = run_steps(batch, plan, steps, false, type, 0.f, s))
+        if (digest_status st = run_steps(batch, plan, steps, false, type, 0.f, base, s))
             return st;
     }
     return DIGEST_OK;
@@ -474,7 +473,7 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
                 return st;
         }
         if (digest_status st =
-                run_steps(batch, plan, steps, true, DIGEST_F32, 1.f - lr * decay, s))
+                run_steps(batch, plan, steps, true, DIGEST_F32, 1.f - lr * decay, base, s))
             return st;
     }
     return DIGEST_OK;

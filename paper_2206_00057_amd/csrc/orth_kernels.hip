@@ -30,6 +30,12 @@ typedef float floatx16 __attribute__((ext_vector_type(16)));
 constexpr int kThreads = 256;
 constexpr int kBlockK = 32;   // k of one line of a plane: 32 high, 32 low parts
 
+// The wave's number in its workgroup, in a scalar register.
+__device__ __forceinline__ int wave_id()
+{
+    return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+}
+
 // Offset (fp16) of k in a row of a plane; the low part lies kBlockK further.
 __device__ __forceinline__ int64_t plane_at(int64_t row, int32_t pitch, int k)
 {
@@ -177,210 +183,481 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
 //   kResult  the same into the caller's matrix
 //   kUpdate  the same into the weights
 enum OrthMode { kGram, kPoly, kApply, kResult, kUpdate };
+constexpr bool symmetric(int mode) { return mode == kGram || mode == kPoly; }
 
-constexpr int kBM = kOrthTile;                       // tile of D, both sides
-constexpr int kWaveTile = kBM / 2;                   // 4 waves, 2 x 2
-constexpr int kSub = kWaveTile / 32;                 // 32 x 32 blocks of a wave, each side
-constexpr int kLine = 8;                             // 16-byte chunks of a line
+constexpr int kLine = 8;   // 16-byte chunks of a line
 
 struct OrthParams {
     float alpha;         // plane products to the stored value's scale
     float diag, lin;     // kPoly: a 2^eb, b 2^(eb - ea)
     float keep;
     int32_t from;
-    int32_t tile0[kOrthItems + 1];
+    // Workgroups: the whole tiles [0, whole), then the parts of the others
+    // (chunk lines of k each, item i's parts from work0[i] on).
+    int32_t whole, chunk;
+    int32_t tile0[kOrthItems + 1], work0[kOrthItems + 1], parts[kOrthItems];
+    float *partials;
 };
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
-template <int MODE, class T>
-__global__ __launch_bounds__(kThreads, 2) void k_orth_gemm(OrthBatch b, OrthParams pr)
+template <int MODE>
+__device__ __forceinline__ void operands(const OrthItem &it, const OrthParams &pr, int &K,
+                                         const char *&P, const char *&Q)
 {
-    constexpr bool SYM = MODE == kGram || MODE == kPoly;
-    // [row][chunk]: chunk j of row i holds the line's chunk j ^ (i & 7), so
-    // that eight rows' reads of one chunk fall into different banks
-    __shared__ half8 lds0[2][kBM * kLine], lds1[2][kBM * kLine];
+    K = MODE == kGram ? it.ck : it.rk;
+    P = (const char *)(MODE == kGram ? it.X : MODE == kPoly ? it.A : it.B);
+    Q = (const char *)(MODE == kGram ? it.X : MODE == kPoly ? it.A : it.Xt[pr.from]);
+}
 
-    const uint32_t logical = xcd_contiguous(blockIdx.x, gridDim.x);
-    int i = 0;
-    while (i + 1 < b.n && (int)logical >= pr.tile0[i + 1])
-        ++i;
-    const OrthItem &it = b.item[i];
-    int t = (int)logical - pr.tile0[i];
-    int tm, tn;
+// Tile t of an item, tiles of BM x BN.  Symmetric products: the tiles that
+// reach above the diagonal (BM = f BN), by column.
+template <bool SYM, int BM, int BN>
+__device__ __forceinline__ void tile_of(const OrthItem &it, int t, int &tm, int &tn)
+{
     if constexpr (SYM) {
-        // tiles on and above the diagonal, column by column
-        tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
-        while (tn * (tn + 1) / 2 > t)
-            --tn;
-        while ((tn + 1) * (tn + 2) / 2 <= t)
-            ++tn;
-        tm = t - tn * (tn + 1) / 2;
+        constexpr int F = BM / BN;
+        // columns F j .. F j + F - 1 have j + 1 tiles each: F j (j + 1) / 2 before them
+        int j = (int)((sqrtf(8.f * (float)t / F + 1.f) - 1.f) * 0.5f);
+        while (F * (j * (j + 1) / 2) > t)
+            --j;
+        while (F * ((j + 1) * (j + 2) / 2) <= t)
+            ++j;
+        t -= F * (j * (j + 1) / 2);
+        tn = F * j + t / (j + 1);
+        tm = t % (j + 1);
     } else {
-        const int gm = it.rp / kBM;
+        const int gm = (it.rp + BM - 1) / BM;
         tm = t % gm;
         tn = t / gm;
     }
-    const int K = MODE == kGram ? it.ck : it.rk;
-    const half8 *P = reinterpret_cast<const half8 *>(MODE == kGram   ? it.X
-                                                     : MODE == kPoly ? it.A
-                                                                     : it.B) +
-                     (int64_t)tm * kBM * (K / 4);
-    const half8 *Q = reinterpret_cast<const half8 *>(MODE == kGram   ? it.X
-                                                     : MODE == kPoly ? it.A
-                                                                     : it.Xt[pr.from]) +
-                     (int64_t)tn * kBM * (K / 4);
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int wm = wave / 2 * kWaveTile, wn = wave % 2 * kWaveTile;
+}
+template <bool SYM, int BM, int BN>
+int tiles_of(const OrthItem &it)
+{
+    const int gm = (it.rp + BM - 1) / BM;
+    if (!SYM)
+        return gm * ((it.cp + BN - 1) / BN);
+    constexpr int F = BM / BN;
+    const int gn = (it.rp + BN - 1) / BN, j = gn / F;
+    return F * (j * (j + 1) / 2) + (gn - F * j) * (j + 1);
+}
 
-    floatx16 acc[kSub][kSub];
+// Stores four products of one column n, rows m .. m + 3 (a multiple of 4), of
+// the 32 x 32 block at (mb, nb), which lies inside the padded product.
+// `mirror`: the block's transposed is nobody else's to store.
+template <int MODE, class T>
+__device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, int m, int n,
+                                    const float (&x)[4], bool mirror)
+{
+    float v[4];
 #pragma unroll
-    for (int x = 0; x < kSub; ++x)
+    for (int e = 0; e < 4; ++e)
+        v[e] = x[e] * pr.alpha;
+    if constexpr (MODE == kPoly) {
+        // (A is symmetric: its row n holds the four side by side)
+        const _Float16 *a = (const _Float16 *)it.A + plane_at(n, it.rk, m);
+        const half4 h = *reinterpret_cast<const half4 *>(a);
+        const half4 l = *reinterpret_cast<const half4 *>(a + kBlockK);
 #pragma unroll
-        for (int y = 0; y < kSub; ++y)
+        for (int e = 0; e < 4; ++e)
+            v[e] = fmaf((float)h[e] + (float)l[e], pr.lin, v[e]) + (m + e == n ? pr.diag : 0.f);
+    }
+    if constexpr (MODE == kGram || MODE == kPoly || MODE == kApply) {
+        half4 h, l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (_Float16)v[e];
+            l[e] = (_Float16)(v[e] - (float)h[e]);
+        }
+        _Float16 *d = (_Float16 *)(MODE == kGram ? it.A : MODE == kPoly ? it.B : it.X);
+        const int pitch = symmetric(MODE) ? it.rk : it.ck;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int64_t at = plane_at(m + e, pitch, n);
+            d[at] = h[e];
+            d[at + kBlockK] = l[e];
+        }
+        if (mirror) {   // four consecutive k
+            _Float16 *dt = symmetric(MODE) ? d : (_Float16 *)it.Xt[pr.from ^ 1];
+            const int64_t at = plane_at(n, it.rk, m);
+            *reinterpret_cast<half4 *>(dt + at) = h;
+            *reinterpret_cast<half4 *>(dt + at + kBlockK) = l;
+        }
+    } else {
+        const bool tall = it.rows > it.cols;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (m + e < it.r && n < it.c) {
+                T *o = (T *)it.out + (tall ? (int64_t)n * it.ldo + m + e
+                                           : (int64_t)(m + e) * it.ldo + n);
+                if constexpr (MODE == kUpdate)
+                    *o = (T)(pr.keep * (float)*o - it.scale * v[e]);
+                else
+                    *o = (T)v[e];
+            }
+    }
+}
+
+// A symmetric product's 32 x 32 block at (mb, nb): blocks below the diagonal
+// are the mirror of those above.
+template <int MODE>
+__device__ __forceinline__ bool stored(const OrthItem &it, int mb, int nb)
+{
+    if (symmetric(MODE))
+        return mb <= nb && nb < it.rk;
+    return mb < it.rp && nb < it.cp;
+}
+
+// The large products: BM x BN of D per workgroup, WM x WN waves of TM x TN
+// blocks of 32 x 32.  One line (32 k) of both operands' rows at a time in LDS,
+// the next one on its way there.
+template <int MODE, class T, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthParams pr)
+{
+    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32;
+    // [row][chunk]: chunk j of row i holds the line's chunk j ^ (i & 7), so
+    // that eight rows' reads of one chunk fall into different banks
+    __shared__ half8 lds0[(BM + BN) * kLine], lds1[(BM + BN) * kLine];
+
+    int w = blockIdx.x, i = 0, t, part = -1;
+    if (w < pr.whole) {
+        w = (int)xcd_contiguous(w, pr.whole);
+        while (i + 1 < b.n && w >= pr.tile0[i + 1])
+            ++i;
+        t = w - pr.tile0[i];
+    } else {
+        while (i + 1 < b.n && w >= pr.work0[i + 1])
+            ++i;
+        part = (w - pr.work0[i]) % pr.parts[i];
+        t = max(pr.whole - pr.tile0[i], 0) + (w - pr.work0[i]) / pr.parts[i];
+    }
+    const OrthItem &it = b.item[i];
+    int tm, tn, K;
+    tile_of<symmetric(MODE), BM, BN>(it, t, tm, tn);
+    const char *P, *Q;
+    operands<MODE>(it, pr, K, P, Q);
+    const int lane = threadIdx.x % kWave, wave = wave_id();
+    const int wm = wave / WN * TM * 32, wn = wave % WN * TN * 32;
+
+    floatx16 acc[TM][TN];
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+#pragma unroll
+        for (int y = 0; y < TN; ++y)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 acc[x][y][e] = 0.f;
 
-    // one line (32 k) of every row of both operands into LDS: a wave's
-    // instruction takes 8 rows, 16 bytes a lane
-    constexpr int kLoads = kBM / (8 * (kThreads / kWave));
-    const int lrow = lane / kLine, chunk = (lane % kLine) ^ (lrow & 7);
-    auto load = [&](int kb, half8 (*dst)[kBM * kLine]) {
+    // A wave's instruction takes 8 rows, 16 bytes a lane; rows past the
+    // operand repeat its last eight (their products are not stored).
+    const int64_t pitch = (int64_t)K * 4;   // bytes of a row
+    const int prow = it.rp, qrow = symmetric(MODE) ? it.rp : it.cp;
+    const int lrow = lane / kLine;
+    const uint32_t loff = (uint32_t)(lrow * pitch) + 16 * ((lane % kLine) ^ lrow);
+    auto load = [&](int kb, half8 *dst) {
 #pragma unroll
-        for (int q = 0; q < kLoads; ++q) {
-            const int row = (wave * kLoads + q) * 8;
-            const int64_t at = (int64_t)(row + lrow) * (K / 4) + kb * kLine + chunk;
-            __builtin_amdgcn_global_load_lds((global_void *)(P + at),
-                                             (lds_void *)(&dst[0][row * kLine]), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_void *)(Q + at),
-                                             (lds_void *)(&dst[1][row * kLine]), 16, 0, 0);
+        for (int q = 0; q < BM / 8; q += W) {
+            const int row = 8 * (q + wave);
+            const char *src = P + min(tm * BM + row, prow - 8) * pitch + kb * 128;
+            __builtin_amdgcn_global_load_lds((global_void *)(src + loff),
+                                             (lds_void *)(&dst[row * kLine]), 16, 0, 0);
         }
+#pragma unroll
+        for (int q = 0; q < BN / 8; q += W) {
+            const int row = 8 * (q + wave);
+            const char *src = Q + min(tn * BN + row, qrow - 8) * pitch + kb * 128;
+            __builtin_amdgcn_global_load_lds((global_void *)(src + loff),
+                                             (lds_void *)(&dst[(BM + row) * kLine]), 16, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
-    auto multiply = [&](const half8 (*src)[kBM * kLine]) {
+    auto multiply = [&](const half8 *src) {
+        const int r = lane % 32;
 #pragma unroll
         for (int s = 0; s < kBlockK / 16; ++s) {
-            half8 p[2][kSub], q[2][kSub];
-            const int r = lane % 32;
+            half8 p[2][TM], q[2][TN];
 #pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const int c = (4 * part + 2 * s + lane / 32) ^ (r & 7);
+            for (int h = 0; h < 2; ++h) {
+                const int c = (4 * h + 2 * s + lane / 32) ^ (r & 7);
 #pragma unroll
-                for (int x = 0; x < kSub; ++x) {
-                    p[part][x] = src[0][(wm + 32 * x + r) * kLine + c];
-                    q[part][x] = src[1][(wn + 32 * x + r) * kLine + c];
-                }
+                for (int x = 0; x < TM; ++x)
+                    p[h][x] = src[(wm + 32 * x + r) * kLine + c];
+#pragma unroll
+                for (int y = 0; y < TN; ++y)
+                    q[h][y] = src[(BM + wn + 32 * y + r) * kLine + c];
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k)
 #pragma unroll
-                for (int x = 0; x < kSub; ++x)
+                for (int x = 0; x < TM; ++x)
 #pragma unroll
-                    for (int y = 0; y < kSub; ++y)
+                    for (int y = 0; y < TN; ++y)
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                             p[k == 2][x], q[k == 1][y], acc[x][y], 0, 0, 0);
         }
     };
-    const int nk = K / kBlockK;   // even: k is padded to 64
-    load(0, lds0);
+    const int k0 = part < 0 ? 0 : part * pr.chunk;
+    const int k1 = part < 0 ? K / kBlockK : min(K / kBlockK, k0 + pr.chunk);
+    load(k0, lds0);
     __syncthreads();
-    for (int kb = 0; kb < nk; kb += 2) {
+    for (int kb = k0; kb < k1; kb += 2) {   // (an even number of lines)
         load(kb + 1, lds1);
         multiply(lds0);
         __syncthreads();
-        if (kb + 2 < nk)
+        if (kb + 2 < k1)
             load(kb + 2, lds0);
         multiply(lds1);
         __syncthreads();
     }
 
-    // element e of a lane: row 8 (e / 4) + 4 (lane / 32) + e % 4, column lane % 32
+    // (what the stores need is formed here, not kept through the loop)
+    int lane_out = lane;
+    asm volatile("" : "+v"(lane_out));
+    // element e of a lane: row 8 (e / 4) + 4 (lane_out / 32) + e % 4, column lane % 32
     // of its 32 x 32 block
 #pragma unroll
-    for (int x = 0; x < kSub; ++x)
+    for (int x = 0; x < TM; ++x)
 #pragma unroll
-        for (int y = 0; y < kSub; ++y) {
-            const int mb = tm * kBM + wm + 32 * x, n = tn * kBM + wn + 32 * y + lane % 32;
-            const int nb = n - lane % 32;
+        for (int y = 0; y < TN; ++y) {
+            const int mb = tm * BM + wm + 32 * x, nb = tn * BN + wn + 32 * y;
+            if (!stored<MODE>(it, mb, nb))
+                continue;
 #pragma unroll
-            for (int e4 = 0; e4 < 4; ++e4) {
-                const int m = mb + 8 * e4 + 4 * (lane / 32);
+            for (int g = 0; g < 4; ++g) {
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    v[e] = acc[x][y][4 * e4 + e] * pr.alpha;
-                if constexpr (MODE == kPoly) {
-                    const _Float16 *A = (const _Float16 *)it.A;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float l = 0.f;
-                        if (nb < it.rk) {
-                            const int64_t at = plane_at(m + e, it.rk, n);
-                            l = (float)A[at] + (float)A[at + kBlockK];
-                        }
-                        v[e] = fmaf(l, pr.lin, v[e]) + (m + e == n ? pr.diag : 0.f);
-                    }
-                }
-                if constexpr (MODE == kGram || MODE == kPoly || MODE == kApply) {
-                    half4 h, l;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        h[e] = (_Float16)v[e];
-                        l[e] = (_Float16)(v[e] - (float)h[e]);
-                    }
-                    _Float16 *d = (_Float16 *)(MODE == kGram ? it.A : MODE == kPoly ? it.B : it.X);
-                    const int pitch = SYM ? it.rk : it.ck;
-                    if (nb < pitch)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const int64_t at = plane_at(m + e, pitch, n);
-                            d[at] = h[e];
-                            d[at + kBlockK] = l[e];
-                        }
-                    // the transposed: four consecutive k.  (A diagonal tile
-                    // holds both halves itself.)
-                    if ((!SYM || tm != tn) && mb < it.rk) {
-                        _Float16 *dt = SYM ? d : (_Float16 *)it.Xt[pr.from ^ 1];
-                        const int64_t at = plane_at(n, it.rk, m);
-                        *reinterpret_cast<half4 *>(dt + at) = h;
-                        *reinterpret_cast<half4 *>(dt + at + kBlockK) = l;
-                    }
+                    v[e] = acc[x][y][4 * g + e];
+                if (part < 0) {
+                    put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane_out / 32), nb + lane_out % 32, v,
+                                 !symmetric(MODE) || mb != nb);
                 } else {
-                    const bool tall = it.rows > it.cols;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (m + e < it.r && n < it.c) {
-                            const int64_t at = tall ? (int64_t)n * it.ldo + m + e
-                                                    : (int64_t)(m + e) * it.ldo + n;
-                            T *o = (T *)it.out + at;
-                            if constexpr (MODE == kUpdate)
-                                *o = (T)(pr.keep * (float)*o - it.scale * v[e]);
-                            else
-                                *o = (T)v[e];
-                        }
+                    float *d = pr.partials + (int64_t)(w - pr.whole) * (BM * BN) +
+                               ((((wave * TM + x) * TN + y) * 4 + g) * kWave + lane_out) * 4;
+                    *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
                 }
             }
         }
 }
 
-template <class F>
-int32_t fill_tiles(const OrthBatch &b, OrthParams &pr, F tiles)
+// Sums the parts of the tiles that were split, one wave a 32 x 32 block.
+template <int MODE, class T, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams pr)
+{
+    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, BLOCKS = W * TM * TN;
+    const int lane = threadIdx.x % kWave;
+    const int at = blockIdx.x * (kThreads / kWave) + wave_id();
+    int tile = pr.whole + at / BLOCKS, i = 0;
+    while (i + 1 < b.n && tile >= pr.tile0[i + 1])
+        ++i;
+    const OrthItem &it = b.item[i];
+    const int first = max(pr.whole, pr.tile0[i]);   // the item's first split tile
+    int tm, tn;
+    tile_of<symmetric(MODE), BM, BN>(it, tile - pr.tile0[i], tm, tn);
+    const int blk = at % BLOCKS, wave = blk / (TM * TN), x = blk / TN % TM, y = blk % TN;
+    const int mb = tm * BM + (wave / WN * TM + x) * 32, nb = tn * BN + (wave % WN * TN + y) * 32;
+    if (!stored<MODE>(it, mb, nb))
+        return;
+    const float *src = pr.partials +
+                       (int64_t)(pr.work0[i] - pr.whole + (tile - first) * pr.parts[i]) * (BM * BN) +
+                       (blk * 4 * kWave + lane) * 4;
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < pr.parts[i]; ++p) {
+            const float4 f = *reinterpret_cast<const float4 *>(src + (int64_t)p * (BM * BN) +
+                                                               g * kWave * 4);
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+        put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane / 32), nb + lane % 32, v,
+                     !symmetric(MODE) || mb != nb);
+    }
+}
+
+// The small products, bound by latency: 64 x 64 of D per workgroup, whose
+// waves split k among themselves (a line in turn, straight from memory into
+// the registers that multiply) and add their sums through LDS in wave order.
+constexpr int kSmallWaves = 8;
+constexpr int kSmall = 64;
+
+template <int MODE, class T>
+__global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, OrthParams pr)
+{
+    __shared__ float4 sum[kSmallWaves][16][kWave];
+    int i = 0;
+    const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x);
+    while (i + 1 < b.n && w >= pr.tile0[i + 1])
+        ++i;
+    const OrthItem &it = b.item[i];
+    int tm, tn, K;
+    tile_of<symmetric(MODE), kSmall, kSmall>(it, w - pr.tile0[i], tm, tn);
+    const char *P, *Q;
+    operands<MODE>(it, pr, K, P, Q);
+    const int lane = threadIdx.x % kWave, wave = wave_id();
+    const int64_t pitch = (int64_t)K * 4;
+    const uint32_t loff = (uint32_t)((lane % 32) * pitch) + 16 * (lane / 32);
+    P += tm * kSmall * pitch;
+    Q += tn * kSmall * pitch;
+
+    floatx16 acc[2][2];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                acc[x][y][e] = 0.f;
+    struct Line {
+        half8 p[2][2][2], q[2][2][2];   // [16 k][part][block]
+    };
+    auto load = [&](int kb, Line &l) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int64_t o = 32 * x * pitch + kb * 128 + 64 * h + 32 * s;
+                    l.p[s][h][x] = *reinterpret_cast<const half8 *>(P + o + loff);
+                    l.q[s][h][x] = *reinterpret_cast<const half8 *>(Q + o + loff);
+                }
+    };
+    auto multiply = [&](const Line &l) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int y = 0; y < 2; ++y)
+                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                            l.p[s][k == 2][x], l.q[s][k == 1][y], acc[x][y], 0, 0, 0);
+    };
+    const int nk = K / kBlockK;
+    if (wave < nk) {
+        Line l0, l1;
+        load(wave, l0);
+        for (int kb = wave; kb < nk; kb += 2 * kSmallWaves) {
+            // (past the end: the last line again, not multiplied)
+            load(min(kb + kSmallWaves, nk - 1), l1);
+            multiply(l0);
+            if (kb + kSmallWaves >= nk)
+                break;
+            load(min(kb + 2 * kSmallWaves, nk - 1), l0);
+            multiply(l1);
+        }
+    }
+    const int waves = min(kSmallWaves, nk);   // the others' sums are zero
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                sum[wave][(2 * x + y) * 4 + g][lane] =
+                    make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
+                                acc[x][y][4 * g + 3]);
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 16 / kSmallWaves; ++j) {
+        const int at = wave * (16 / kSmallWaves) + j, x = at / 8, y = at / 4 % 2, g = at % 4;
+        const int mb = tm * kSmall + 32 * x, nb = tn * kSmall + 32 * y;
+        if (!stored<MODE>(it, mb, nb))
+            continue;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int p = 0; p < waves; ++p) {
+            const float4 f = sum[p][at][lane];
+            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        }
+        put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane / 32), nb + lane % 32, v,
+                     !symmetric(MODE) || mb != nb);
+    }
+}
+
+// The large kernel's shape, and its workgroups on the card at a time.
+#ifndef ORTH_SHAPE
+#define ORTH_SHAPE 2, 4, 4, 2
+#endif
+constexpr int kShape[4] = {ORTH_SHAPE};
+constexpr int kBM = kShape[0] * kShape[2] * 32, kBN = kShape[1] * kShape[3] * 32;
+#ifndef ORTH_SLOTS
+#define ORTH_SLOTS 256
+#endif
+constexpr int kSlots = ORTH_SLOTS;
+constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each)
+
+template <bool SYM>
+int lines_of(const OrthItem &it, int mode)
+{
+    return (mode == kGram ? it.ck : it.rk) / kBlockK;
+}
+
+// Splits the k of the tiles that are left over when the whole ones have
+// filled the card's slots evenly: into as many parts as there are slots.
+template <int MODE>
+int32_t plan_tiles(const OrthBatch &b, OrthParams &pr)
+{
+    constexpr bool SYM = symmetric(MODE);
+    pr.tile0[0] = 0;
+    for (int i = 0; i < b.n; ++i)
+        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<SYM, kBM, kBN>(b.item[i]);
+    const int32_t tiles = pr.tile0[b.n];
+    pr.whole = tiles - tiles % kSlots;
+    auto parts = [&](int chunk) {
+        int32_t n = 0;
+        for (int i = 0; i < b.n; ++i) {
+            const int left = pr.tile0[i + 1] - std::max(pr.whole, pr.tile0[i]);
+            const int lines = lines_of<SYM>(b.item[i], MODE);
+            pr.parts[i] = (lines + chunk - 1) / chunk;
+            pr.work0[i] = pr.whole + n;
+            if (left > 0)
+                n += left * pr.parts[i];
+        }
+        pr.work0[b.n] = pr.whole + n;
+        return n;
+    };
+    int most = 0;
+    for (int i = 0; i < b.n; ++i)
+        most = std::max(most, lines_of<SYM>(b.item[i], MODE));
+    pr.chunk = kMinChunk;
+    while (pr.chunk < most && parts(pr.chunk) > kSlots)
+        pr.chunk += std::max(2, pr.chunk / 32 * 2);
+    const int32_t n = parts(pr.chunk);
+    if (n == tiles - pr.whole) {   // nothing to split
+        pr.whole = tiles;
+        return tiles;
+    }
+    return pr.whole + n;
+}
+
+// 64 x 64 tiles up to which the small kernel is the faster one.
+constexpr int kSmallTiles = 512;
+template <int MODE>
+int32_t small_tiles(const OrthBatch &b, OrthParams &pr)
 {
     pr.tile0[0] = 0;
     for (int i = 0; i < b.n; ++i)
-        pr.tile0[i + 1] = pr.tile0[i] + tiles(b.item[i]);
+        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<symmetric(MODE), kSmall, kSmall>(b.item[i]);
     return pr.tile0[b.n];
 }
 
 template <int MODE, class T>
 hipError_t gemm(const OrthBatch &b, OrthParams pr, hipStream_t s)
 {
-    const int32_t n = fill_tiles(b, pr, [](const OrthItem &it) {
-        const int gm = it.rp / kBM, gn = it.cp / kBM;
-        return MODE == kGram || MODE == kPoly ? gm * (gm + 1) / 2 : gm * gn;
-    });
-    k_orth_gemm<MODE, T><<<n, kThreads, 0, s>>>(b, pr);
+    int32_t n = small_tiles<MODE>(b, pr);
+    if (n <= kSmallTiles) {
+        k_orth_small<MODE, T><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
+        return hipGetLastError();
+    }
+    n = plan_tiles<MODE>(b, pr);
+    k_orth_gemm<MODE, T, ORTH_SHAPE><<<n, kShape[0] * kShape[1] * kWave, 0, s>>>(b, pr);
+    if (pr.whole < pr.tile0[b.n])
+        k_orth_join<MODE, T, ORTH_SHAPE>
+            <<<(pr.tile0[b.n] - pr.whole) * (kBM / 32) * (kBN / 32) / (kThreads / kWave), kThreads, 0,
+               s>>>(b, pr);
     return hipGetLastError();
 }
 
@@ -433,10 +710,23 @@ hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStr
     return hipGetLastError();
 }
 
-hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
-                            int32_t type, float keep, hipStream_t s)
+size_t orth_partials(const OrthBatch &b)
 {
     OrthParams pr{};
+    auto bytes = [&](int32_t small, int32_t work) {
+        return small <= kSmallTiles ? 0 : (size_t)(work - pr.whole) * kBM * kBN * sizeof(float);
+    };
+    size_t most = 0;
+    most = std::max(most, bytes(small_tiles<kGram>(b, pr), plan_tiles<kGram>(b, pr)));
+    most = std::max(most, bytes(small_tiles<kPoly>(b, pr), plan_tiles<kPoly>(b, pr)));
+    return std::max(most, bytes(small_tiles<kApply>(b, pr), plan_tiles<kApply>(b, pr)));
+}
+
+hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
+                            int32_t type, float keep, float *partials, hipStream_t s)
+{
+    OrthParams pr{};
+    pr.partials = partials;
     pr.keep = keep;
     pr.from = st.from;
     pr.alpha = std::ldexp(1.f, st.ea - 2 * st.ex);

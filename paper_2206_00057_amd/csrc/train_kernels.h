@@ -33,12 +33,11 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
 // worked on as its transpose).  X, its transpose, A and B = a I + b A + c A^2
 // lie in memory as split planes: each value times a power of two as the sum
 // of two fp16, in rows whose k runs in blocks of 32, 32 high parts and then 32
-// low parts (one 128-byte line).  Rows are padded to kOrthTile, k to
-// kOrthPadK, with zeros.
+// low parts (one 128-byte line).  Rows and k are padded to kOrthPad, with
+// zeros.
 constexpr int kOrthItems = 16;       // matrices of one launch
 constexpr int kOrthGrads = 192;      // gradient pointers of one launch (its arguments stay below 4 KB)
-constexpr int kOrthTile = 128;
-constexpr int kOrthPadK = 64;
+constexpr int kOrthPad = 64;
 constexpr int kOrthSumBlocks = 256;  // partial sums of |U|_F^2, at most
 constexpr int64_t kOrthSumRun = 4096;
 
@@ -75,9 +74,11 @@ hipError_t launch_muon_momentum(const OrthBatch &b, const OrthGrads &g, int32_t 
                                 float beta, bool nesterov, hipStream_t s);
 // X and Xt[0] from U: U / |U|_F * 2^e (zero for U = 0).
 hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStream_t s);
+// Bytes of the steps' partial sums (joined), 16-byte aligned.
+size_t orth_partials(const OrthBatch &b);
 // One step.  last: the result goes to out, as `type`, or (muon) into the
 // weights: out <- keep out - scale O.
 hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
-                            int32_t type, float keep, hipStream_t s);
+                            int32_t type, float keep, float *partials, hipStream_t s);
 
 }  // namespace digest
