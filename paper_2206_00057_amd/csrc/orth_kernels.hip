@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device.h"
 #include "train_kernels.h"
@@ -28,7 +29,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
-constexpr int kBlockK = 32;   // k of one line of a plane: 32 high, 32 low parts
+constexpr int kBlockK = 32;   // k of one line of LDS
 
 // The wave's number in its workgroup, in a scalar register.
 __device__ __forceinline__ int wave_id()
@@ -36,10 +37,14 @@ __device__ __forceinline__ int wave_id()
     return __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
 }
 
-// Offset (fp16) of k in a row of a plane; the low part lies kBlockK further.
+// Where a plane keeps (row, k), k a multiple of 8: the eight values from there
+// on lie side by side, 16 bytes of the matrix instruction's operand, in the
+// order of its lanes: [row / 32][k / 16][part][k / 8 % 2][row % 32][8].  The
+// part (high, low) is kPart further, a block of 32 rows pitch * 64 fp16.
+constexpr int kPart = 512;
 __device__ __forceinline__ int64_t plane_at(int64_t row, int32_t pitch, int k)
 {
-    return row * 2 * pitch + (k / kBlockK) * (2 * kBlockK) + k % kBlockK;
+    return (row / 32 * pitch + k / 16 * 16) * 64 + (k / 8 % 2) * 256 + row % 32 * 8;
 }
 
 // ---------------------------------------------------------------------------
@@ -63,23 +68,72 @@ __device__ __forceinline__ double block_sum(double v)
     return v;
 }
 
+// Runs of kOrthSumRun elements of a matrix, a vector of V a thread: f(element
+// index, count) for each thread's vectors; the matrix's rows one after another
+// where they are contiguous, else each row's runs.
+template <int V, class F>
+__device__ __forceinline__ void for_vectors(const OrthItem &it, int64_t ld, F f)
+{
+    const bool flat = ld == it.cols;
+    const int64_t len = flat ? (int64_t)it.rows * it.cols : it.cols;
+    const int64_t runs = (len + kOrthSumRun - 1) / kOrthSumRun;
+    for (int64_t q = blockIdx.x; q < runs * (flat ? 1 : it.rows); q += it.sums) {
+        const int64_t row = flat ? 0 : q / runs, from = (q - row * runs) * kOrthSumRun;
+#pragma unroll
+        for (int j = 0; j < (int)kOrthSumRun / (kThreads * V); ++j) {
+            const int64_t at = from + (j * kThreads + (int)threadIdx.x) * V;
+            if (at < len)
+                f(row * ld + at, (int)min((int64_t)V, len - at));
+        }
+    }
+}
+
+template <class T, int V>
+struct Vec {
+    typedef T type __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+};
+// n <= V elements at p, zeros behind them.
+template <class T, int V>
+__device__ __forceinline__ typename Vec<T, V>::type load_some(const T *p, int n)
+{
+    typedef typename Vec<T, V>::type vec;
+    if (n == V)
+        return *reinterpret_cast<const vec *>(p);
+    vec v;
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+        v[j] = j < n ? p[j] : (T)0.f;
+    return v;
+}
+template <class T, int V>
+__device__ __forceinline__ void store_some(T *p, int n, typename Vec<T, V>::type v)
+{
+    if (n == V) {
+        *reinterpret_cast<typename Vec<T, V>::type *>(p) = v;
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            if (j < n)
+                p[j] = v[j];
+    }
+}
+
 // Partial sums of the squares of U, 64 bits: their range holds the squares of
 // every fp32 number.
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_sum(OrthBatch b)
 {
+    constexpr int V = 16 / sizeof(T);
     const OrthItem &it = b.item[blockIdx.y];
     if ((int)blockIdx.x >= it.sums)
         return;
-    const T *u = (const T *)it.u;
-    const int64_t n = (int64_t)it.rows * it.cols;
     double v = 0;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n;
-         i += (int64_t)it.sums * kThreads) {
-        const int64_t r = i / it.cols;
-        const double x = (double)(float)u[r * it.ldu + (i - r * it.cols)];
-        v += x * x;
-    }
+    for_vectors<V>(it, it.ldu, [&](int64_t at, int n) {
+        const auto x = load_some<T, V>((const T *)it.u + at, n);
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            v += (double)(float)x[j] * (double)(float)x[j];
+    });
     v = block_sum(v);
     if (threadIdx.x == 0)
         it.part[blockIdx.x] = v;
@@ -94,21 +148,35 @@ __global__ __launch_bounds__(kThreads) void k_muon_momentum(OrthBatch b, OrthGra
         return;
     const float *const *g = grads.g + blockIdx.y * per_item;
     float *u = (float *)it.u;
-    const int64_t n = (int64_t)it.rows * it.cols;
     const float inv = 1.f / (float)per_item;
     double v = 0;
-    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n;
-         i += (int64_t)it.sums * kThreads) {
-        float s = 0.f;
-        for (int m = 0; m < per_item; ++m)
-            s += g[m][i];
-        s *= inv;
-        const float mo = fmaf(beta, it.mom[i], s);
-        it.mom[i] = mo;
-        const float x = nesterov ? fmaf(beta, mo, s) : mo;
-        u[i] = x;
-        v += (double)x * (double)x;
-    }
+    for_vectors<4>(it, it.cols, [&](int64_t at, int n) {
+        auto mo = load_some<float, 4>(it.mom + at, n);
+        auto s = load_some<float, 4>(g[0] + at, n);
+        int m = 1;
+        for (; m + 4 <= per_item; m += 4) {   // four in flight, added in order
+            Vec<float, 4>::type x[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[j] = load_some<float, 4>(g[m + j] + at, n);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                s += x[j];
+        }
+        for (; m < per_item; ++m)
+            s += load_some<float, 4>(g[m] + at, n);
+        auto x = s;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float mean = s[j] * inv;
+            mo[j] = fmaf(beta, mo[j], mean);
+            x[j] = nesterov ? fmaf(beta, mo[j], mean) : mo[j];
+            if (j < n)
+                v += (double)x[j] * (double)x[j];
+        }
+        store_some<float, 4>(it.mom + at, n, mo);
+        store_some<float, 4>(u + at, n, x);
+    });
     v = block_sum(v);
     if (threadIdx.x == 0)
         it.part[blockIdx.x] = v;
@@ -127,7 +195,7 @@ __device__ __forceinline__ void split8(const float (&x)[8], _Float16 *dst)
         l[j] = (_Float16)(x[j] - (float)h[j]);
     }
     *reinterpret_cast<half8 *>(dst) = h;
-    *reinterpret_cast<half8 *>(dst + kBlockK) = l;
+    *reinterpret_cast<half8 *>(dst + kPart) = l;
 }
 
 template <class T>
@@ -140,7 +208,10 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
     // padded extents of U's rows and columns
     if (i0 >= (tall ? it.cp : it.rp) || j0 >= (tall ? it.rp : it.cp))
         return;
-    const double norm = sqrt(block_sum(threadIdx.x < it.sums ? it.part[threadIdx.x] : 0.0));
+    double sum = 0;
+    for (int i = threadIdx.x; i < it.sums; i += kThreads)
+        sum += it.part[i];
+    const double norm = sqrt(block_sum(sum));
     const double f = norm == 0 ? 0.0 : scale / norm;
     const T *u = (const T *)it.u;
     const int tj = threadIdx.x % kSplitTile;
@@ -155,7 +226,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
     _Float16 *pt = (_Float16 *)(tall ? it.X : it.Xt[0]);
     const int kp = tall ? it.rk : it.ck, kt = tall ? it.ck : it.rk;
     for (int q = threadIdx.x; q < kSplitTile * kSplitTile / 8; q += kThreads) {
-        const int row = q / (kSplitTile / 8), k = q % (kSplitTile / 8) * 8;
+        const int row = q % kSplitTile, k = q / kSplitTile * 8;   // (rows side by side)
         float x[8];
         if (j0 < kp) {
 #pragma unroll
@@ -185,7 +256,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
 enum OrthMode { kGram, kPoly, kApply, kResult, kUpdate };
 constexpr bool symmetric(int mode) { return mode == kGram || mode == kPoly; }
 
-constexpr int kLine = 8;   // 16-byte chunks of a line
+constexpr int kLineBytes = 4096;   // 32 rows, 32 k, both parts
 
 struct OrthParams {
     float alpha;         // plane products to the stored value's scale
@@ -244,51 +315,69 @@ int tiles_of(const OrthItem &it)
     return F * (j * (j + 1) / 2) + (gn - F * j) * (j + 1);
 }
 
-// Stores four products of one column n, rows m .. m + 3 (a multiple of 4), of
-// the 32 x 32 block at (mb, nb), which lies inside the padded product.
-// `mirror`: the block's transposed is nobody else's to store.
+// Stores 32 columns n from nb on and 16 rows m from mb on of the product,
+// given by rows: lane (n = lane % 32, lane / 32) holds m = 8 (lane / 32) ..
+// + 7.  `mirror`: the transposed is nobody else's to store.  `turn` is the
+// wave's own LDS.
+constexpr int kTurn = 32 * 20;
 template <int MODE, class T>
-__device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, int m, int n,
-                                    const float (&x)[4], bool mirror)
+__device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, int mb, int nb,
+                                    float (&v)[8], bool mirror, uint32_t *turn)
 {
-    float v[4];
+    const int lane = threadIdx.x % kWave;
+    const int m = mb + lane / 32 * 8, n = nb + lane % 32;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        v[e] = x[e] * pr.alpha;
+    for (int e = 0; e < 8; ++e)
+        v[e] *= pr.alpha;
     if constexpr (MODE == kPoly) {
-        // (A is symmetric: its row n holds the four side by side)
+        // (A is symmetric: its row n holds the eight side by side)
         const _Float16 *a = (const _Float16 *)it.A + plane_at(n, it.rk, m);
-        const half4 h = *reinterpret_cast<const half4 *>(a);
-        const half4 l = *reinterpret_cast<const half4 *>(a + kBlockK);
+        const half8 h = *reinterpret_cast<const half8 *>(a);
+        const half8 l = *reinterpret_cast<const half8 *>(a + kPart);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
             v[e] = fmaf((float)h[e] + (float)l[e], pr.lin, v[e]) + (m + e == n ? pr.diag : 0.f);
     }
     if constexpr (MODE == kGram || MODE == kPoly || MODE == kApply) {
-        half4 h, l;
+        union {
+            half8 v;
+            uint16_t u[8];
+        } h, l;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            h[e] = (_Float16)v[e];
-            l[e] = (_Float16)(v[e] - (float)h[e]);
+        for (int e = 0; e < 8; ++e) {
+            h.v[e] = (_Float16)v[e];
+            l.v[e] = (_Float16)(v[e] - (float)h.v[e]);
         }
         _Float16 *d = (_Float16 *)(MODE == kGram ? it.A : MODE == kPoly ? it.B : it.X);
-        const int pitch = symmetric(MODE) ? it.rk : it.ck;
+        if (mirror) {
+            _Float16 *dt = (symmetric(MODE) ? d : (_Float16 *)it.Xt[pr.from ^ 1]) +
+                           plane_at(n, it.rk, m);
+            *reinterpret_cast<half8 *>(dt) = h.v;
+            *reinterpret_cast<half8 *>(dt + kPart) = l.v;
+        }
+        // turned over in LDS: lane (m = lane % 16, lane / 16) takes n = 8 (lane / 16) .. + 7
+        // (rows 20 words apart)
+        uint4 *w = reinterpret_cast<uint4 *>(turn + lane % 32 * 20 + lane / 32 * 8);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int64_t at = plane_at(m + e, pitch, n);
-            d[at] = h[e];
-            d[at + kBlockK] = l[e];
+        for (int e = 0; e < 2; ++e)
+            w[e] = make_uint4(h.u[4 * e] | l.u[4 * e] << 16, h.u[4 * e + 1] | l.u[4 * e + 1] << 16,
+                              h.u[4 * e + 2] | l.u[4 * e + 2] << 16,
+                              h.u[4 * e + 3] | l.u[4 * e + 3] << 16);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        const uint32_t *r = turn + lane / 16 * 160 + lane % 16;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            h.u[e] = (uint16_t)r[20 * e];
+            l.u[e] = (uint16_t)(r[20 * e] >> 16);
         }
-        if (mirror) {   // four consecutive k
-            _Float16 *dt = symmetric(MODE) ? d : (_Float16 *)it.Xt[pr.from ^ 1];
-            const int64_t at = plane_at(n, it.rk, m);
-            *reinterpret_cast<half4 *>(dt + at) = h;
-            *reinterpret_cast<half4 *>(dt + at + kBlockK) = l;
-        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+        d += plane_at(mb + lane % 16, symmetric(MODE) ? it.rk : it.ck, nb + lane / 16 * 8);
+        *reinterpret_cast<half8 *>(d) = h.v;
+        *reinterpret_cast<half8 *>(d + kPart) = l.v;
     } else {
         const bool tall = it.rows > it.cols;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
+        for (int e = 0; e < 8; ++e)
             if (m + e < it.r && n < it.c) {
                 T *o = (T *)it.out + (tall ? (int64_t)n * it.ldo + m + e
                                            : (int64_t)(m + e) * it.ldo + n);
@@ -297,6 +386,22 @@ __device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, in
                 else
                     *o = (T)v[e];
             }
+    }
+}
+
+// The matrix instruction's 32 x 32 result, lane (n, lane / 32) with rows
+// 8 g + 4 (lane / 32) + e in element 4 g + e, to rows as put takes them: 16
+// rows of half s.
+__device__ __forceinline__ void rows_of(const floatx16 &x, int s, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        // the upper lanes' x[8 s + e] against the lower lanes' x[8 s + 4 + e]
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x[8 * s + e]),
+                                                        __float_as_uint(x[8 * s + 4 + e]), false,
+                                                        false);
+        v[e] = __uint_as_float(r[0]);
+        v[4 + e] = __uint_as_float(r[1]);
     }
 }
 
@@ -316,10 +421,9 @@ __device__ __forceinline__ bool stored(const OrthItem &it, int mb, int nb)
 template <int MODE, class T, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthParams pr)
 {
-    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32;
-    // [row][chunk]: chunk j of row i holds the line's chunk j ^ (i & 7), so
-    // that eight rows' reads of one chunk fall into different banks
-    __shared__ half8 lds0[(BM + BN) * kLine], lds1[(BM + BN) * kLine];
+    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, ROWS = (BM + BN) / 32;
+    // [32 rows][16 k][part][lane]: what a matrix instruction takes is 1 KB
+    __shared__ half8 lds0[ROWS * kLineBytes / 16], lds1[ROWS * kLineBytes / 16];
 
     int w = blockIdx.x, i = 0, t, part = -1;
     if (w < pr.whole) {
@@ -339,7 +443,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthPa
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
-    const int wm = wave / WN * TM * 32, wn = wave % WN * TN * 32;
+    const int wm = wave / WN * TM, wn = wave % WN * TN;   // in blocks of 32
 
     floatx16 acc[TM][TN];
 #pragma unroll
@@ -350,43 +454,35 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthPa
             for (int e = 0; e < 16; ++e)
                 acc[x][y][e] = 0.f;
 
-    // A wave's instruction takes 8 rows, 16 bytes a lane; rows past the
-    // operand repeat its last eight (their products are not stored).
-    const int64_t pitch = (int64_t)K * 4;   // bytes of a row
-    const int prow = it.rp, qrow = symmetric(MODE) ? it.rp : it.cp;
-    const int lrow = lane / kLine;
-    const uint32_t loff = (uint32_t)(lrow * pitch) + 16 * ((lane % kLine) ^ lrow);
+    // A wave's instruction takes 1 KB of a line's 4 KB for 32 rows; rows past
+    // the operand repeat its last 32 (their products are not stored).
+    const int64_t pitch = (int64_t)K * 128;   // bytes of 32 rows
+    const int prow = it.rp / 32, qrow = (symmetric(MODE) ? it.rp : it.cp) / 32;
+    const uint32_t loff = lane * 16;
     auto load = [&](int kb, half8 *dst) {
 #pragma unroll
-        for (int q = 0; q < BM / 8; q += W) {
-            const int row = 8 * (q + wave);
-            const char *src = P + min(tm * BM + row, prow - 8) * pitch + kb * 128;
-            __builtin_amdgcn_global_load_lds((global_void *)(src + loff),
-                                             (lds_void *)(&dst[row * kLine]), 16, 0, 0);
-        }
-#pragma unroll
-        for (int q = 0; q < BN / 8; q += W) {
-            const int row = 8 * (q + wave);
-            const char *src = Q + min(tn * BN + row, qrow - 8) * pitch + kb * 128;
-            __builtin_amdgcn_global_load_lds((global_void *)(src + loff),
-                                             (lds_void *)(&dst[(BM + row) * kLine]), 16, 0, 0);
+        for (int q = 0; q < 4 * ROWS; q += W) {
+            const int at = q + wave, row = at / 4;
+            const char *src = row < BM / 32 ? P + min(tm * (BM / 32) + row, prow - 1) * pitch
+                                            : Q + min(tn * (BN / 32) + row - BM / 32, qrow - 1) * pitch;
+            src += (int64_t)kb * kLineBytes + at % 4 * 1024;
+            __builtin_amdgcn_global_load_lds((global_void *)(src + loff), (lds_void *)(&dst[at * kWave]),
+                                             16, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     auto multiply = [&](const half8 *src) {
-        const int r = lane % 32;
 #pragma unroll
         for (int s = 0; s < kBlockK / 16; ++s) {
             half8 p[2][TM], q[2][TN];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int c = (4 * h + 2 * s + lane / 32) ^ (r & 7);
 #pragma unroll
                 for (int x = 0; x < TM; ++x)
-                    p[h][x] = src[(wm + 32 * x + r) * kLine + c];
+                    p[h][x] = src[((wm + x) * 4 + 2 * s + h) * kWave + lane];
 #pragma unroll
                 for (int y = 0; y < TN; ++y)
-                    q[h][y] = src[(BM + wn + 32 * y + r) * kLine + c];
+                    q[h][y] = src[((BM / 32 + wn + y) * 4 + 2 * s + h) * kWave + lane];
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k)
@@ -415,65 +511,78 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthPa
     // (what the stores need is formed here, not kept through the loop)
     int lane_out = lane;
     asm volatile("" : "+v"(lane_out));
-    // element e of a lane: row 8 (e / 4) + 4 (lane_out / 32) + e % 4, column lane % 32
-    // of its 32 x 32 block
+    static_assert(sizeof(lds0) >= W * kTurn * 4, "room to turn blocks");
+    uint32_t *turn = reinterpret_cast<uint32_t *>(lds0) + wave * kTurn;
 #pragma unroll
     for (int x = 0; x < TM; ++x)
 #pragma unroll
         for (int y = 0; y < TN; ++y) {
-            const int mb = tm * BM + wm + 32 * x, nb = tn * BN + wn + 32 * y;
+            const int mb = tm * BM + (wm + x) * 32, nb = tn * BN + (wn + y) * 32;
             if (!stored<MODE>(it, mb, nb))
                 continue;
+            if (part < 0) {
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                float v[4];
+                for (int s = 0; s < 2; ++s) {
+                    float v[8];
+                    rows_of(acc[x][y], s, v);
+                    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn);
+                }
+            } else {
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = acc[x][y][4 * g + e];
-                if (part < 0) {
-                    put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane_out / 32), nb + lane_out % 32, v,
-                                 !symmetric(MODE) || mb != nb);
-                } else {
+                for (int g = 0; g < 4; ++g) {
                     float *d = pr.partials + (int64_t)(w - pr.whole) * (BM * BN) +
                                ((((wave * TM + x) * TN + y) * 4 + g) * kWave + lane_out) * 4;
-                    *reinterpret_cast<float4 *>(d) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4 *>(d) =
+                        make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
+                                    acc[x][y][4 * g + 3]);
                 }
             }
         }
 }
 
-// Sums the parts of the tiles that were split, one wave a 32 x 32 block.
+// Sums the parts of the tiles that were split, one wave 16 rows of a block.
 template <int MODE, class T, int WM, int WN, int TM, int TN>
 __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams pr)
 {
-    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, BLOCKS = W * TM * TN;
+    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, UNITS = W * TM * TN * 2;
+    __shared__ uint32_t turn[kThreads / kWave][kTurn];
     const int lane = threadIdx.x % kWave;
     const int at = blockIdx.x * (kThreads / kWave) + wave_id();
-    int tile = pr.whole + at / BLOCKS, i = 0;
+    const int tile = pr.whole + at / UNITS;
+    int i = 0;
     while (i + 1 < b.n && tile >= pr.tile0[i + 1])
         ++i;
     const OrthItem &it = b.item[i];
     const int first = max(pr.whole, pr.tile0[i]);   // the item's first split tile
     int tm, tn;
     tile_of<symmetric(MODE), BM, BN>(it, tile - pr.tile0[i], tm, tn);
-    const int blk = at % BLOCKS, wave = blk / (TM * TN), x = blk / TN % TM, y = blk % TN;
+    const int blk = at % UNITS / 2, s = at % 2;
+    const int wave = blk / (TM * TN), x = blk / TN % TM, y = blk % TN;
     const int mb = tm * BM + (wave / WN * TM + x) * 32, nb = tn * BN + (wave % WN * TN + y) * 32;
     if (!stored<MODE>(it, mb, nb))
         return;
+    // rows 8 (lane / 32) .. + 7 of half s: element group 2 s + lane / 32 of both lane halves
     const float *src = pr.partials +
                        (int64_t)(pr.work0[i] - pr.whole + (tile - first) * pr.parts[i]) * (BM * BN) +
-                       (blk * 4 * kWave + lane) * 4;
+                       ((blk * 4 + 2 * s + lane / 32) * kWave + lane % 32) * 4;
+    float v[8] = {};
+    constexpr int U = 8;   // parts in flight
+    for (int p0 = 0; p0 < pr.parts[i]; p0 += U) {
+        float4 f[U][2];
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < pr.parts[i]; ++p) {
-            const float4 f = *reinterpret_cast<const float4 *>(src + (int64_t)p * (BM * BN) +
-                                                               g * kWave * 4);
-            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
+        for (int u = 0; u < U; ++u) {
+            const float *q = src + (int64_t)min(p0 + u, pr.parts[i] - 1) * (BM * BN);
+            f[u][0] = *reinterpret_cast<const float4 *>(q);
+            f[u][1] = *reinterpret_cast<const float4 *>(q + 128);
         }
-        put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane / 32), nb + lane % 32, v,
-                     !symmetric(MODE) || mb != nb);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (p0 + u < pr.parts[i]) {
+                v[0] += f[u][0].x, v[1] += f[u][0].y, v[2] += f[u][0].z, v[3] += f[u][0].w;
+                v[4] += f[u][1].x, v[5] += f[u][1].y, v[6] += f[u][1].z, v[7] += f[u][1].w;
+            }
     }
+    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave_id()]);
 }
 
 // The small products, bound by latency: 64 x 64 of D per workgroup, whose
@@ -486,6 +595,7 @@ template <int MODE, class T>
 __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, OrthParams pr)
 {
     __shared__ float4 sum[kSmallWaves][16][kWave];
+    __shared__ uint32_t turn[kSmallWaves][kTurn];
     int i = 0;
     const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x);
     while (i + 1 < b.n && w >= pr.tile0[i + 1])
@@ -496,10 +606,10 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
-    const int64_t pitch = (int64_t)K * 4;
-    const uint32_t loff = (uint32_t)((lane % 32) * pitch) + 16 * (lane / 32);
-    P += tm * kSmall * pitch;
-    Q += tn * kSmall * pitch;
+    const int64_t pitch = (int64_t)K * 128;
+    const uint32_t loff = lane * 16;
+    P += tm * 2 * pitch;
+    Q += tn * 2 * pitch;
 
     floatx16 acc[2][2];
 #pragma unroll
@@ -519,7 +629,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int64_t o = 32 * x * pitch + kb * 128 + 64 * h + 32 * s;
+                    const int64_t o = x * pitch + (int64_t)kb * kLineBytes + (2 * s + h) * 1024;
                     l.p[s][h][x] = *reinterpret_cast<const half8 *>(P + o + loff);
                     l.q[s][h][x] = *reinterpret_cast<const half8 *>(Q + o + loff);
                 }
@@ -551,45 +661,53 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         }
     }
     const int waves = min(kSmallWaves, nk);   // the others' sums are zero
+    if (wave < waves)
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                sum[wave][(2 * x + y) * 4 + g][lane] =
-                    make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
-                                acc[x][y][4 * g + 3]);
+                for (int g = 0; g < 4; ++g)
+                    sum[wave][(2 * x + y) * 4 + g][lane] =
+                        make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
+                                    acc[x][y][4 * g + 3]);
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 16 / kSmallWaves; ++j) {
-        const int at = wave * (16 / kSmallWaves) + j, x = at / 8, y = at / 4 % 2, g = at % 4;
-        const int mb = tm * kSmall + 32 * x, nb = tn * kSmall + 32 * y;
-        if (!stored<MODE>(it, mb, nb))
-            continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int p = 0; p < waves; ++p) {
-            const float4 f = sum[p][at][lane];
-            v[0] += f.x, v[1] += f.y, v[2] += f.z, v[3] += f.w;
-        }
-        put<MODE, T>(it, pr, mb + 8 * g + 4 * (lane / 32), nb + lane % 32, v,
-                     !symmetric(MODE) || mb != nb);
+    // a wave stores 16 rows of a block
+    static_assert(kSmallWaves == 8, "one of the eight halves of blocks a wave");
+    const int blk = wave / 2, s = wave % 2;
+    const int mb = tm * kSmall + blk / 2 * 32, nb = tn * kSmall + blk % 2 * 32;
+    if (!stored<MODE>(it, mb, nb))
+        return;
+    float v[8] = {};
+    for (int p = 0; p < waves; ++p) {
+        const float4 *f = &sum[p][blk * 4 + 2 * s + lane / 32][lane % 32];
+        v[0] += f[0].x, v[1] += f[0].y, v[2] += f[0].z, v[3] += f[0].w;
+        v[4] += f[32].x, v[5] += f[32].y, v[6] += f[32].z, v[7] += f[32].w;
     }
+    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave]);
 }
 
-// The large kernel's shape, and its workgroups on the card at a time.
-#ifndef ORTH_SHAPE
-#define ORTH_SHAPE 2, 4, 4, 2
+// The large kernel's shapes, and its workgroups on the card at a time.
+#ifndef ORTH_FULL
+#define ORTH_FULL 2, 4, 4, 2
+#define ORTH_HALF 2, 2, 4, 2
 #endif
-constexpr int kShape[4] = {ORTH_SHAPE};
-constexpr int kBM = kShape[0] * kShape[2] * 32, kBN = kShape[1] * kShape[3] * 32;
+struct ShapeOf {
+    int wm, wn, tm, tn;
+    constexpr int bm() const { return wm * tm * 32; }
+    constexpr int bn() const { return wn * tn * 32; }
+};
+constexpr ShapeOf kFull = {ORTH_FULL}, kHalf = {ORTH_HALF};
+constexpr ShapeOf shape_of(int mode) { return symmetric(mode) ? kHalf : kFull; }
 #ifndef ORTH_SLOTS
 #define ORTH_SLOTS 256
 #endif
 constexpr int kSlots = ORTH_SLOTS;
-constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each)
+#ifndef ORTH_MINCHUNK
+#define ORTH_MINCHUNK 4
+#endif
+constexpr int kMinChunk = ORTH_MINCHUNK;   // lines of a part, at least (an even number each)
 
-template <bool SYM>
 int lines_of(const OrthItem &it, int mode)
 {
     return (mode == kGram ? it.ck : it.rk) / kBlockK;
@@ -603,14 +721,14 @@ int32_t plan_tiles(const OrthBatch &b, OrthParams &pr)
     constexpr bool SYM = symmetric(MODE);
     pr.tile0[0] = 0;
     for (int i = 0; i < b.n; ++i)
-        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<SYM, kBM, kBN>(b.item[i]);
+        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<SYM, shape_of(MODE).bm(), shape_of(MODE).bn()>(b.item[i]);
     const int32_t tiles = pr.tile0[b.n];
     pr.whole = tiles - tiles % kSlots;
     auto parts = [&](int chunk) {
         int32_t n = 0;
         for (int i = 0; i < b.n; ++i) {
             const int left = pr.tile0[i + 1] - std::max(pr.whole, pr.tile0[i]);
-            const int lines = lines_of<SYM>(b.item[i], MODE);
+            const int lines = lines_of(b.item[i], MODE);
             pr.parts[i] = (lines + chunk - 1) / chunk;
             pr.work0[i] = pr.whole + n;
             if (left > 0)
@@ -621,7 +739,7 @@ int32_t plan_tiles(const OrthBatch &b, OrthParams &pr)
     };
     int most = 0;
     for (int i = 0; i < b.n; ++i)
-        most = std::max(most, lines_of<SYM>(b.item[i], MODE));
+        most = std::max(most, lines_of(b.item[i], MODE));
     pr.chunk = kMinChunk;
     while (pr.chunk < most && parts(pr.chunk) > kSlots)
         pr.chunk += std::max(2, pr.chunk / 32 * 2);
@@ -653,11 +771,12 @@ hipError_t gemm(const OrthBatch &b, OrthParams pr, hipStream_t s)
         return hipGetLastError();
     }
     n = plan_tiles<MODE>(b, pr);
-    k_orth_gemm<MODE, T, ORTH_SHAPE><<<n, kShape[0] * kShape[1] * kWave, 0, s>>>(b, pr);
+    constexpr ShapeOf S = shape_of(MODE);
+    k_orth_gemm<MODE, T, S.wm, S.wn, S.tm, S.tn><<<n, S.wm * S.wn * kWave, 0, s>>>(b, pr);
     if (pr.whole < pr.tile0[b.n])
-        k_orth_join<MODE, T, ORTH_SHAPE>
-            <<<(pr.tile0[b.n] - pr.whole) * (kBM / 32) * (kBN / 32) / (kThreads / kWave), kThreads, 0,
-               s>>>(b, pr);
+        k_orth_join<MODE, T, S.wm, S.wn, S.tm, S.tn>
+            <<<(pr.tile0[b.n] - pr.whole) * (S.bm() / 32) * (S.bn() / 32) * 2 / (kThreads / kWave),
+               kThreads, 0, s>>>(b, pr);
     return hipGetLastError();
 }
 
@@ -712,14 +831,19 @@ hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStr
 
 size_t orth_partials(const OrthBatch &b)
 {
-    OrthParams pr{};
-    auto bytes = [&](int32_t small, int32_t work) {
-        return small <= kSmallTiles ? 0 : (size_t)(work - pr.whole) * kBM * kBN * sizeof(float);
-    };
     size_t most = 0;
-    most = std::max(most, bytes(small_tiles<kGram>(b, pr), plan_tiles<kGram>(b, pr)));
-    most = std::max(most, bytes(small_tiles<kPoly>(b, pr), plan_tiles<kPoly>(b, pr)));
-    return std::max(most, bytes(small_tiles<kApply>(b, pr), plan_tiles<kApply>(b, pr)));
+    auto add = [&](auto mode) {
+        constexpr int MODE = decltype(mode)::value;
+        OrthParams pr{};
+        if (small_tiles<MODE>(b, pr) > kSmallTiles) {
+            const int32_t parts = plan_tiles<MODE>(b, pr) - pr.whole;
+            most = std::max(most, (size_t)parts * shape_of(MODE).bm() * shape_of(MODE).bn() * 4);
+        }
+    };
+    add(std::integral_constant<int, kGram>());
+    add(std::integral_constant<int, kPoly>());
+    add(std::integral_constant<int, kApply>());
+    return most;
 }
 
 hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,

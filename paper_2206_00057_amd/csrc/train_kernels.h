@@ -32,13 +32,12 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
 // X <- (a I + b A + c A^2) X with A = X X^T, for X wide (r <= c; a tall U is
 // worked on as its transpose).  X, its transpose, A and B = a I + b A + c A^2
 // lie in memory as split planes: each value times a power of two as the sum
-// of two fp16, in rows whose k runs in blocks of 32, 32 high parts and then 32
-// low parts (one 128-byte line).  Rows and k are padded to kOrthPad, with
-// zeros.
+// of two fp16, in the order in which the matrix instructions take them.  Rows
+// and k are padded to kOrthPad, with zeros.
 constexpr int kOrthItems = 16;       // matrices of one launch
 constexpr int kOrthGrads = 192;      // gradient pointers of one launch (its arguments stay below 4 KB)
 constexpr int kOrthPad = 64;
-constexpr int kOrthSumBlocks = 256;  // partial sums of |U|_F^2, at most
+constexpr int kOrthSumBlocks = 1024;  // partial sums of |U|_F^2, at most
 constexpr int64_t kOrthSumRun = 4096;
 
 struct OrthItem {
