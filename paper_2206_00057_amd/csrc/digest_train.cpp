@@ -213,17 +213,34 @@ digest_status plan_steps(int32_t steps, const float *coeffs, OrthStep *out)
     return DIGEST_OK;
 }
 
+// Every matrix of the group fits one workgroup's LDS.
+bool whole(const OrthBatch &b, int32_t steps)
+{
+    for (int32_t i = 0; i < b.n; ++i)
+        if (b.item[i].r > digest::kWholeRows || b.item[i].c > digest::kWholeCols)
+            return false;
+    return steps <= digest::kWholeSteps;
+}
+
+// From U (and, for larger matrices, its partial sums) to the result.
 digest_status run_steps(const OrthBatch &batch, const OrthStep *plan, int32_t steps, bool muon,
                         int32_t type, float keep, void *partials, hipStream_t s)
 {
+    if (whole(batch, steps))
+        return hip_check(
+            digest::launch_orth_whole(batch, plan, steps, muon, type, keep, s),
+            "orthogonalisation");
+    if (!muon)
+        if (digest_status st = hip_check(digest::launch_orth_sum(batch, type, s), "norm"))
+            return st;
     if (digest_status st = hip_check(
             digest::launch_orth_split(batch, muon ? DIGEST_F32 : type, plan[0].ex, s), "split"))
         return st;
     for (int32_t k = 0; k < steps; ++k)
-        if (digest_status st = hip_check(digest::launch_orth_step(batch, plan[k], k + 1 == steps,
-                                                                  muon, type, keep,
-                                                                  (float *)partials, s),
-                                         "orthogonalisation step"))
+        if (digest_status st = hip_check(
+                digest::launch_orth_step(batch, plan[k], k + 1 == steps, muon, type, keep,
+                                         (float *)partials, s),
+                "orthogonalisation step"))
             return st;
     return DIGEST_OK;
 }
@@ -383,8 +400,6 @@ digest_status digest_orthogonalize(int32_t count, const int32_t *rows, const int
             it.u = in[i], it.ldu = ld_in ? ld_in[i] : cols[i];
             it.out = out[i], it.ldo = ld_out ? ld_out[i] : cols[i];
         }
-        if (digest_status st = hip_check(digest::launch_orth_sum(batch, type, s), "norm"))
-            return st;
         if (digest_status st = run_steps(batch, plan, steps, false, type, 0.f, base, s))
             return st;
     }

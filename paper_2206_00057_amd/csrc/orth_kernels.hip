@@ -585,51 +585,54 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
     put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave_id()]);
 }
 
-// The small products, bound by latency: 64 x 64 of D per workgroup, whose
-// waves split k among themselves (a line in turn, straight from memory into
-// the registers that multiply) and add their sums through LDS in wave order.
+// The small products, bound by latency: TS x TS blocks of 32 x 32 of D per
+// workgroup, whose waves split k among themselves (a line in turn, straight
+// from memory into the registers that multiply, DEPTH lines in flight) and
+// add their sums through LDS in wave order.
 constexpr int kSmallWaves = 8;
-constexpr int kSmall = 64;
 
-template <int MODE, class T>
+template <int MODE, class T, int TS, int DEPTH>
 __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, OrthParams pr)
 {
-    __shared__ float4 sum[kSmallWaves][16][kWave];
-    __shared__ uint32_t turn[kSmallWaves][kTurn];
+    constexpr int TILE = 32 * TS, GROUPS = TS * TS * 4, UNITS = TS * TS * 2;
+    __shared__ float4 sum[kSmallWaves][GROUPS][kWave];
+    __shared__ uint32_t turn[UNITS][kTurn];
     int i = 0;
     const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x);
     while (i + 1 < b.n && w >= pr.tile0[i + 1])
         ++i;
     const OrthItem &it = b.item[i];
     int tm, tn, K;
-    tile_of<symmetric(MODE), kSmall, kSmall>(it, w - pr.tile0[i], tm, tn);
+    tile_of<symmetric(MODE), TILE, TILE>(it, w - pr.tile0[i], tm, tn);
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
     const int64_t pitch = (int64_t)K * 128;
     const uint32_t loff = lane * 16;
-    P += tm * 2 * pitch;
-    Q += tn * 2 * pitch;
+    P += tm * TS * pitch;
+    Q += tn * TS * pitch;
 
-    floatx16 acc[2][2];
+    floatx16 acc[TS][TS];
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+    for (int x = 0; x < TS; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int y = 0; y < TS; ++y)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
                 acc[x][y][e] = 0.f;
     struct Line {
-        half8 p[2][2][2], q[2][2][2];   // [16 k][part][block]
+        half8 p[2][2][TS], q[2][2][TS];   // [16 k][part][block]
     };
-    auto load = [&](int kb, Line &l) {
+    const int nk = K / kBlockK;
+    auto load = [&](int kb, Line &l) {   // (past the end: the last line, not multiplied)
+        const int64_t at = (int64_t)min(kb, nk - 1) * kLineBytes;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    const int64_t o = x * pitch + (int64_t)kb * kLineBytes + (2 * s + h) * 1024;
+                for (int x = 0; x < TS; ++x) {
+                    const int64_t o = x * pitch + at + (2 * s + h) * 1024;
                     l.p[s][h][x] = *reinterpret_cast<const half8 *>(P + o + loff);
                     l.q[s][h][x] = *reinterpret_cast<const half8 *>(Q + o + loff);
                 }
@@ -640,43 +643,44 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
 #pragma unroll
             for (int k = 0; k < 3; ++k)
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int x = 0; x < TS; ++x)
 #pragma unroll
-                    for (int y = 0; y < 2; ++y)
+                    for (int y = 0; y < TS; ++y)
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                             l.p[s][k == 2][x], l.q[s][k == 1][y], acc[x][y], 0, 0, 0);
     };
-    const int nk = K / kBlockK;
     if (wave < nk) {
-        Line l0, l1;
-        load(wave, l0);
-        for (int kb = wave; kb < nk; kb += 2 * kSmallWaves) {
-            // (past the end: the last line again, not multiplied)
-            load(min(kb + kSmallWaves, nk - 1), l1);
-            multiply(l0);
-            if (kb + kSmallWaves >= nk)
-                break;
-            load(min(kb + 2 * kSmallWaves, nk - 1), l0);
-            multiply(l1);
+        Line l[DEPTH];
+#pragma unroll
+        for (int u = 0; u < DEPTH; ++u)
+            load(wave + u * kSmallWaves, l[u]);
+        for (int kb = wave; kb < nk; kb += DEPTH * kSmallWaves) {
+#pragma unroll
+            for (int u = 0; u < DEPTH; ++u) {
+                if (kb + u * kSmallWaves < nk)   // uniform
+                    multiply(l[u]);
+                if (kb + DEPTH * kSmallWaves < nk)
+                    load(kb + (u + DEPTH) * kSmallWaves, l[u]);
+            }
         }
     }
     const int waves = min(kSmallWaves, nk);   // the others' sums are zero
     if (wave < waves)
 #pragma unroll
-        for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < TS; ++x)
 #pragma unroll
-            for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < TS; ++y)
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
-                    sum[wave][(2 * x + y) * 4 + g][lane] =
+                    sum[wave][(TS * x + y) * 4 + g][lane] =
                         make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
                                     acc[x][y][4 * g + 3]);
     __syncthreads();
     // a wave stores 16 rows of a block
-    static_assert(kSmallWaves == 8, "one of the eight halves of blocks a wave");
+    static_assert(UNITS <= kSmallWaves, "a wave for each half of a block");
     const int blk = wave / 2, s = wave % 2;
-    const int mb = tm * kSmall + blk / 2 * 32, nb = tn * kSmall + blk % 2 * 32;
-    if (!stored<MODE>(it, mb, nb))
+    const int mb = tm * TILE + blk / TS * 32, nb = tn * TILE + blk % TS * 32;
+    if (wave >= UNITS || !stored<MODE>(it, mb, nb))
         return;
     float v[8] = {};
     for (int p = 0; p < waves; ++p) {
@@ -685,6 +689,250 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         v[4] += f[32].x, v[5] += f[32].y, v[6] += f[32].z, v[7] += f[32].w;
     }
     put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave]);
+}
+
+// Small matrices as a whole: X, its transpose and A (then B in its place) stay
+// in the LDS of one workgroup through all steps, so that a call is one launch
+// instead of three a step.
+constexpr int kWholeWaves = 8;
+constexpr int kWholeThreads = kWholeWaves * kWave;
+
+struct WholeParams {
+    int32_t steps;
+    double scale;    // X_0's
+    float keep;
+    struct {
+        float gram, poly, lin, diag, apply;   // as OrthParams has them
+    } st[kWholeSteps];
+};
+
+// A plane in LDS: [part][row / 32][k / 8][row % 32][8], the 32 rows followed by
+// 16 bytes that set the next k / 8 off by four banks.
+struct LdsPlane {
+    half8 *p;
+    int rows, k8;   // blocks of 32 rows, of 8 k
+    __device__ __forceinline__ int size() const { return rows * k8 * 33; }
+    // the operand of a matrix instruction: 32 rows, 16 k
+    __device__ __forceinline__ half8 frag(int rb, int k16, int part, int lane) const
+    {
+        return p[part * size() + (rb * k8 + 2 * k16 + lane / 32) * 33 + lane % 32];
+    }
+    __device__ __forceinline__ half8 *at(int row, int k, int part) const
+    {
+        return p + part * size() + (row / 32 * k8 + k / 8) * 33 + row % 32;
+    }
+    // 8 consecutive k of a row
+    __device__ __forceinline__ void store8(int row, int k, half8 h, half8 l) const
+    {
+        *at(row, k, 0) = h;
+        *at(row, k, 1) = l;
+    }
+    __device__ __forceinline__ void store1(int row, int k, _Float16 h, _Float16 l) const
+    {
+        reinterpret_cast<_Float16 *>(at(row, k, 0))[k % 8] = h;
+        reinterpret_cast<_Float16 *>(at(row, k, 1))[k % 8] = l;
+    }
+};
+
+__device__ __forceinline__ void split_parts(const float (&v)[8], half8 &h, half8 &l)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        h[e] = (_Float16)v[e];
+        l[e] = (_Float16)(v[e] - (float)h[e]);
+    }
+}
+
+__device__ __forceinline__ floatx16 zero16()
+{
+    floatx16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        z[e] = 0.f;
+    return z;
+}
+
+// A 32 x 32 block of P Q^T over k16 in [from, to).
+__device__ __forceinline__ floatx16 block_product(const LdsPlane &P, int pr, const LdsPlane &Q,
+                                                  int qr, int from, int to, int lane)
+{
+    floatx16 acc = zero16();
+    for (int k = from; k < to; ++k) {
+        const half8 p0 = P.frag(pr, k, 0, lane), p1 = P.frag(pr, k, 1, lane);
+        const half8 q0 = Q.frag(qr, k, 0, lane), q1 = Q.frag(qr, k, 1, lane);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p0, q0, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p0, q1, acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p1, q0, acc, 0, 0, 0);
+    }
+    return acc;
+}
+
+template <bool UPDATE, class T>
+__global__ __launch_bounds__(kWholeThreads) void k_orth_whole(OrthBatch b, WholeParams pr)
+{
+    // X and X^T of 64 x 256, A of 64 x 64
+    __shared__ half8 lds[2 * 2 * (kWholeRows / 32) * (kWholeCols / 8) * 33 +
+                         2 * (kWholeRows / 32) * (kWholeRows / 8) * 33];
+    __shared__ double sums[kWholeWaves];
+    const OrthItem &it = b.item[blockIdx.x];
+    const int lane = threadIdx.x % kWave, wave = wave_id();
+    const bool tall = it.rows > it.cols;
+    constexpr int R = kWholeRows;
+    const int C = it.ck;
+    const LdsPlane X = {lds, R / 32, C / 8};
+    const LdsPlane Xt = {lds + 2 * X.size(), C / 32, R / 8};
+    const LdsPlane A = {Xt.p + 2 * Xt.size(), R / 32, R / 8};
+
+    // U, eight consecutive elements of a row at a time
+    constexpr int N = kWholeRows * kWholeCols / 8 / kWholeThreads;
+    const int wide = (tall ? R : C) / 8;   // eights in a padded row of U
+    float u[N][8];
+    double sum = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int q = threadIdx.x + j * kWholeThreads;
+        const int i = q / wide, k = q % wide * 8;
+        const T *src = (const T *)it.u + (int64_t)i * it.ldu + k;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            u[j][e] = i < it.rows && k + e < it.cols ? (float)src[e] : 0.f;
+            sum += (double)u[j][e] * (double)u[j][e];
+        }
+    }
+#pragma unroll
+    for (int off = kWave / 2; off > 0; off >>= 1)
+        sum += __shfl_xor(sum, off);
+    if (lane == 0)
+        sums[wave] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < kWholeWaves; ++w)
+        sum += sums[w];
+    const double f = sum == 0 ? 0.0 : pr.scale / sqrt(sum);
+    const LdsPlane &P = tall ? Xt : X, &Pt = tall ? X : Xt;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        const int q = threadIdx.x + j * kWholeThreads;
+        const int i = q / wide, k = q % wide * 8;
+        if (i >= (tall ? C : R))
+            continue;
+        half8 h, l;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            v[e] = (float)((double)u[j][e] * f);
+        split_parts(v, h, l);
+        P.store8(i, k, h, l);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            Pt.store1(k + e, i, h[e], l[e]);
+    }
+    __syncthreads();
+
+    // the three blocks of a symmetric product, one a wave
+    const int sx = wave % 3 == 2, sy = wave % 3 != 0;
+    const int half = C / 32;   // k16 of half of X's k
+    for (int st = 0; st < pr.steps; ++st) {
+        const auto &p = pr.st[st];
+        floatx16 acc = zero16();
+        // A = X X^T: each block by two waves, half of the k each, the second's
+        // sum handed over where A will be
+        float4 *hand = reinterpret_cast<float4 *>(A.p) + wave % 3 * 4 * kWave + lane;
+        if (wave < 6)
+            acc = block_product(X, sx, X, sy, wave / 3 * half, (wave / 3 + 1) * half, lane);
+        if (wave >= 3 && wave < 6)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                hand[g * kWave] = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2],
+                                              acc[4 * g + 3]);
+        __syncthreads();
+        if (wave < 3)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 o = hand[g * kWave];
+                acc[4 * g] += o.x, acc[4 * g + 1] += o.y;
+                acc[4 * g + 2] += o.z, acc[4 * g + 3] += o.w;
+            }
+        __syncthreads();
+        auto keep = [&](float (&v)[8], const LdsPlane &D, const LdsPlane &Dt, int m, int n,
+                        bool mirror) {
+            half8 h, l;
+            split_parts(v, h, l);
+            if (mirror)
+                Dt.store8(n, m, h, l);
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                D.store1(m + e, n, h[e], l[e]);
+        };
+        const int n = 32 * sy + lane % 32;
+        if (wave < 3)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float v[8];
+                rows_of(acc, s, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[e] *= p.gram;
+                keep(v, A, A, 32 * sx + 16 * s + lane / 32 * 8, n, sx != sy);
+            }
+        __syncthreads();
+        // B = a I + b A + c A A
+        float v[2][8];
+        if (wave < 3) {
+            acc = block_product(A, sx, A, sy, 0, R / 16, lane);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int m = 32 * sx + 16 * s + lane / 32 * 8;
+                rows_of(acc, s, v[s]);
+                const half8 h = *A.at(n, m, 0), l = *A.at(n, m, 1);
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    v[s][e] = fmaf((float)h[e] + (float)l[e], p.lin, v[s][e] * p.poly) +
+                              (m + e == n ? p.diag : 0.f);
+            }
+        }
+        __syncthreads();
+        if (wave < 3)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+                keep(v[s], A, A, 32 * sx + 16 * s + lane / 32 * 8, n, sx != sy);
+        __syncthreads();
+        // X <- B X: block column x of X, both of its blocks a wave
+        const bool mine = wave < C / 32;
+        floatx16 out[2];
+        if (mine)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+                out[x] = block_product(A, x, Xt, wave, 0, R / 16, lane);
+        __syncthreads();
+        if (mine)
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    rows_of(out[x], s, v[s]);
+                    const int m = 32 * x + 16 * s + lane / 32 * 8, c = 32 * wave + lane % 32;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        v[s][e] *= p.apply;
+                    if (st + 1 < pr.steps) {
+                        keep(v[s], X, Xt, m, c, true);
+                        continue;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (m + e < it.r && c < it.c) {
+                            T *o = (T *)it.out + (tall ? (int64_t)c * it.ldo + m + e
+                                                       : (int64_t)(m + e) * it.ldo + c);
+                            if constexpr (UPDATE)
+                                *o = (T)(pr.keep * (float)*o - it.scale * v[s][e]);
+                            else
+                                *o = (T)v[s][e];
+                        }
+                }
+        __syncthreads();
+    }
 }
 
 // The large kernel's shapes, and its workgroups on the card at a time.
@@ -751,23 +999,31 @@ int32_t plan_tiles(const OrthBatch &b, OrthParams &pr)
     return pr.whole + n;
 }
 
-// 64 x 64 tiles up to which the small kernel is the faster one.
-constexpr int kSmallTiles = 512;
-template <int MODE>
+// 32 x 32 and 64 x 64 tiles up to which the small kernel is the faster one.
+#ifndef ORTH_T32
+#define ORTH_T32 512
+#endif
+constexpr int kTiles32 = ORTH_T32, kTiles64 = 512;
+template <int MODE, int TILE>
 int32_t small_tiles(const OrthBatch &b, OrthParams &pr)
 {
     pr.tile0[0] = 0;
     for (int i = 0; i < b.n; ++i)
-        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<symmetric(MODE), kSmall, kSmall>(b.item[i]);
+        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<symmetric(MODE), TILE, TILE>(b.item[i]);
     return pr.tile0[b.n];
 }
 
 template <int MODE, class T>
 hipError_t gemm(const OrthBatch &b, OrthParams pr, hipStream_t s)
 {
-    int32_t n = small_tiles<MODE>(b, pr);
-    if (n <= kSmallTiles) {
-        k_orth_small<MODE, T><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
+    int32_t n = small_tiles<MODE, 32>(b, pr);
+    if (n <= kTiles32) {
+        k_orth_small<MODE, T, 1, 4><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
+        return hipGetLastError();
+    }
+    n = small_tiles<MODE, 64>(b, pr);
+    if (n <= kTiles64) {
+        k_orth_small<MODE, T, 2, 2><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
         return hipGetLastError();
     }
     n = plan_tiles<MODE>(b, pr);
@@ -829,13 +1085,40 @@ hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStr
     return hipGetLastError();
 }
 
+hipError_t launch_orth_whole(const OrthBatch &b, const OrthStep *st, int32_t steps, bool muon,
+                             int32_t type, float keep, hipStream_t s)
+{
+    WholeParams pr{};
+    pr.steps = steps;
+    pr.keep = keep;
+    pr.scale = std::ldexp(1.0, st[0].ex);
+    for (int32_t k = 0; k < steps; ++k) {
+        pr.st[k].gram = std::ldexp(1.f, st[k].ea - 2 * st[k].ex);
+        pr.st[k].poly = std::ldexp(st[k].c, st[k].eb - 2 * st[k].ea);
+        pr.st[k].lin = std::ldexp(st[k].b, st[k].eb - st[k].ea);
+        pr.st[k].diag = std::ldexp(st[k].a, st[k].eb);
+        pr.st[k].apply = std::ldexp(1.f, (k + 1 == steps ? 0 : st[k].en) - st[k].eb - st[k].ex);
+    }
+    if (muon) {
+        k_orth_whole<true, float><<<b.n, kWholeThreads, 0, s>>>(b, pr);
+        return hipGetLastError();
+    }
+    switch (type) {
+    case kF32: k_orth_whole<false, float><<<b.n, kWholeThreads, 0, s>>>(b, pr); break;
+    case kBF16: k_orth_whole<false, __bf16><<<b.n, kWholeThreads, 0, s>>>(b, pr); break;
+    case kF16: k_orth_whole<false, _Float16><<<b.n, kWholeThreads, 0, s>>>(b, pr); break;
+    default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
 size_t orth_partials(const OrthBatch &b)
 {
     size_t most = 0;
     auto add = [&](auto mode) {
         constexpr int MODE = decltype(mode)::value;
         OrthParams pr{};
-        if (small_tiles<MODE>(b, pr) > kSmallTiles) {
+        if (small_tiles<MODE, 64>(b, pr) > kTiles64) {
             const int32_t parts = plan_tiles<MODE>(b, pr) - pr.whole;
             most = std::max(most, (size_t)parts * shape_of(MODE).bm() * shape_of(MODE).bn() * 4);
         }

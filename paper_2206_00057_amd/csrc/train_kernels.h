@@ -75,6 +75,11 @@ hipError_t launch_muon_momentum(const OrthBatch &b, const OrthGrads &g, int32_t 
 hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStream_t s);
 // Bytes of the steps' partial sums (joined), 16-byte aligned.
 size_t orth_partials(const OrthBatch &b);
+// Matrices that one workgroup holds in its LDS: everything from U (after
+// launch_muon_momentum) to the result in one launch.
+constexpr int kWholeRows = 64, kWholeCols = 256, kWholeSteps = 16;
+hipError_t launch_orth_whole(const OrthBatch &b, const OrthStep *st, int32_t steps, bool muon,
+                             int32_t type, float keep, hipStream_t s);
 // One step.  last: the result goes to out, as `type`, or (muon) into the
 // weights: out <- keep out - scale O.
 hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
