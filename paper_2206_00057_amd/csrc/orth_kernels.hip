@@ -26,6 +26,7 @@ namespace {
 
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 
 constexpr int kThreads = 256;
@@ -712,59 +713,53 @@ struct LdsPlane {
     half8 *p;
     int rows, k8;   // blocks of 32 rows, of 8 k
     __device__ __forceinline__ int size() const { return rows * k8 * 33; }
-    // the operand of a matrix instruction: 32 rows, 16 k
-    __device__ __forceinline__ half8 frag(int rb, int k16, int part, int lane) const
-    {
-        return p[part * size() + (rb * k8 + 2 * k16 + lane / 32) * 33 + lane % 32];
-    }
     __device__ __forceinline__ half8 *at(int row, int k, int part) const
     {
         return p + part * size() + (row / 32 * k8 + k / 8) * 33 + row % 32;
     }
-    // 8 consecutive k of a row
-    __device__ __forceinline__ void store8(int row, int k, half8 h, half8 l) const
+    // the operand of a matrix instruction: 16 rows, 32 k
+    __device__ __forceinline__ half8 frag(int row, int k, int part, int lane) const
     {
-        *at(row, k, 0) = h;
-        *at(row, k, 1) = l;
+        return *at(row + lane % 16, k + lane / 16 * 8, part);
     }
-    __device__ __forceinline__ void store1(int row, int k, _Float16 h, _Float16 l) const
+    // 4 consecutive k of a row
+    __device__ __forceinline__ half4 *at4(int row, int k, int part) const
     {
-        reinterpret_cast<_Float16 *>(at(row, k, 0))[k % 8] = h;
-        reinterpret_cast<_Float16 *>(at(row, k, 1))[k % 8] = l;
+        return reinterpret_cast<half4 *>(at(row, k, part)) + k / 4 % 2;
+    }
+    __device__ __forceinline__ _Float16 *at1(int row, int k, int part) const
+    {
+        return reinterpret_cast<_Float16 *>(at(row, k, part)) + k % 8;
     }
 };
 
-__device__ __forceinline__ void split_parts(const float (&v)[8], half8 &h, half8 &l)
+// 16 x 16 blocks of P Q^T (rows m of P, n of Q) over k in [0, K), K a multiple
+// of 32: for each lane (n = lane % 16) rows m = 4 (lane / 16) .. + 3.
+template <int BLOCKS>
+__device__ __forceinline__ void block_products(const LdsPlane &P, const int (&m)[BLOCKS],
+                                               const LdsPlane &Q, const int (&n)[BLOCKS], int K,
+                                               int lane, floatx4 (&acc)[BLOCKS])
 {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        h[e] = (_Float16)v[e];
-        l[e] = (_Float16)(v[e] - (float)h[e]);
-    }
-}
-
-__device__ __forceinline__ floatx16 zero16()
-{
-    floatx16 z;
+    for (int i = 0; i < BLOCKS; ++i)
+        acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+    for (int k = 0; k < K; k += 32) {
+        half8 p[BLOCKS][2], q[BLOCKS][2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-        z[e] = 0.f;
-    return z;
-}
-
-// A 32 x 32 block of P Q^T over k16 in [from, to).
-__device__ __forceinline__ floatx16 block_product(const LdsPlane &P, int pr, const LdsPlane &Q,
-                                                  int qr, int from, int to, int lane)
-{
-    floatx16 acc = zero16();
-    for (int k = from; k < to; ++k) {
-        const half8 p0 = P.frag(pr, k, 0, lane), p1 = P.frag(pr, k, 1, lane);
-        const half8 q0 = Q.frag(qr, k, 0, lane), q1 = Q.frag(qr, k, 1, lane);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p0, q0, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p0, q1, acc, 0, 0, 0);
-        acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(p1, q0, acc, 0, 0, 0);
+        for (int i = 0; i < BLOCKS; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                p[i][h] = P.frag(m[i], k, h, lane);
+                q[i][h] = Q.frag(n[i], k, h, lane);
+            }
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+#pragma unroll
+            for (int i = 0; i < BLOCKS; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i][t == 2], q[i][t == 1], acc[i],
+                                                                0, 0, 0);
     }
-    return acc;
 }
 
 template <bool UPDATE, class T>
@@ -783,19 +778,19 @@ __global__ __launch_bounds__(kWholeThreads) void k_orth_whole(OrthBatch b, Whole
     const LdsPlane Xt = {lds + 2 * X.size(), C / 32, R / 8};
     const LdsPlane A = {Xt.p + 2 * Xt.size(), R / 32, R / 8};
 
-    // U, eight consecutive elements of a row at a time
+    // U, eight consecutive elements of a row a thread, the rows side by side
     constexpr int N = kWholeRows * kWholeCols / 8 / kWholeThreads;
-    const int wide = (tall ? R : C) / 8;   // eights in a padded row of U
+    const int ui = tall ? C : R, uk = (tall ? R : C) / 8;   // padded rows, eights of a row
     float u[N][8];
     double sum = 0;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        const int q = threadIdx.x + j * kWholeThreads;
-        const int i = q / wide, k = q % wide * 8;
-        const T *src = (const T *)it.u + (int64_t)i * it.ldu + k;
+        const int q = threadIdx.x + j * kWholeThreads, i = q % ui, k = q / ui * 8;
+        const int n = i < it.rows ? max(0, min(8, it.cols - k)) : 0;
+        const auto x = load_some<T, 8>((const T *)it.u + (int64_t)i * it.ldu + k, n);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            u[j][e] = i < it.rows && k + e < it.cols ? (float)src[e] : 0.f;
+            u[j][e] = (float)x[e];
             sum += (double)u[j][e] * (double)u[j][e];
         }
     }
@@ -810,127 +805,122 @@ __global__ __launch_bounds__(kWholeThreads) void k_orth_whole(OrthBatch b, Whole
     for (int w = 0; w < kWholeWaves; ++w)
         sum += sums[w];
     const double f = sum == 0 ? 0.0 : pr.scale / sqrt(sum);
-    const LdsPlane &P = tall ? Xt : X, &Pt = tall ? X : Xt;
+    const LdsPlane P = tall ? Xt : X, Pt = tall ? X : Xt;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-        const int q = threadIdx.x + j * kWholeThreads;
-        const int i = q / wide, k = q % wide * 8;
-        if (i >= (tall ? C : R))
+        const int q = threadIdx.x + j * kWholeThreads, i = q % ui, k = q / ui * 8;
+        if (k >= 8 * uk)
             continue;
         half8 h, l;
-        float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] = (float)((double)u[j][e] * f);
-        split_parts(v, h, l);
-        P.store8(i, k, h, l);
+        for (int e = 0; e < 8; ++e) {
+            const float v = (float)((double)u[j][e] * f);
+            h[e] = (_Float16)v;
+            l[e] = (_Float16)(v - (float)h[e]);
+        }
+        *P.at(i, k, 0) = h;
+        *P.at(i, k, 1) = l;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            Pt.store1(k + e, i, h[e], l[e]);
+        for (int e = 0; e < 8; ++e) {
+            *Pt.at1(k + e, i, 0) = h[e];
+            *Pt.at1(k + e, i, 1) = l[e];
+        }
     }
     __syncthreads();
 
-    // the three blocks of a symmetric product, one a wave
-    const int sx = wave % 3 == 2, sy = wave % 3 != 0;
-    const int half = C / 32;   // k16 of half of X's k
+    // 16 x 16 blocks: two of the 16 of A and B a wave, in one row of blocks
+    // (all of them: a block is stored transposed, which is its mirror's place)
+    const int am[2] = {wave / 2 * 16, wave / 2 * 16};
+    const int an[2] = {wave % 2 * 32, wave % 2 * 32 + 16};
+    const int lm = lane / 16 * 4, ln = lane % 16;
+    auto split4 = [](const float (&v)[4], half4 &h, half4 &l) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            h[e] = (_Float16)v[e];
+            l[e] = (_Float16)(v[e] - (float)h[e]);
+        }
+    };
     for (int st = 0; st < pr.steps; ++st) {
-        const auto &p = pr.st[st];
-        floatx16 acc = zero16();
-        // A = X X^T: each block by two waves, half of the k each, the second's
-        // sum handed over where A will be
-        float4 *hand = reinterpret_cast<float4 *>(A.p) + wave % 3 * 4 * kWave + lane;
-        if (wave < 6)
-            acc = block_product(X, sx, X, sy, wave / 3 * half, (wave / 3 + 1) * half, lane);
-        if (wave >= 3 && wave < 6)
+        const auto p = pr.st[st];
+        floatx4 acc[2];
+        half4 h[2], l[2];
+        // A = X X^T
+        block_products<2>(X, am, X, an, C, lane, acc);
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                hand[g * kWave] = make_float4(acc[4 * g], acc[4 * g + 1], acc[4 * g + 2],
-                                              acc[4 * g + 3]);
-        __syncthreads();
-        if (wave < 3)
+        for (int i = 0; i < 2; ++i) {
+            float v[4];
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 o = hand[g * kWave];
-                acc[4 * g] += o.x, acc[4 * g + 1] += o.y;
-                acc[4 * g + 2] += o.z, acc[4 * g + 3] += o.w;
-            }
-        __syncthreads();
-        auto keep = [&](float (&v)[8], const LdsPlane &D, const LdsPlane &Dt, int m, int n,
-                        bool mirror) {
-            half8 h, l;
-            split_parts(v, h, l);
-            if (mirror)
-                Dt.store8(n, m, h, l);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                D.store1(m + e, n, h[e], l[e]);
-        };
-        const int n = 32 * sy + lane % 32;
-        if (wave < 3)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float v[8];
-                rows_of(acc, s, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[e] *= p.gram;
-                keep(v, A, A, 32 * sx + 16 * s + lane / 32 * 8, n, sx != sy);
-            }
-        __syncthreads();
-        // B = a I + b A + c A A
-        float v[2][8];
-        if (wave < 3) {
-            acc = block_product(A, sx, A, sy, 0, R / 16, lane);
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const int m = 32 * sx + 16 * s + lane / 32 * 8;
-                rows_of(acc, s, v[s]);
-                const half8 h = *A.at(n, m, 0), l = *A.at(n, m, 1);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    v[s][e] = fmaf((float)h[e] + (float)l[e], p.lin, v[s][e] * p.poly) +
-                              (m + e == n ? p.diag : 0.f);
-            }
+            for (int e = 0; e < 4; ++e)
+                v[e] = acc[i][e] * p.gram;
+            split4(v, h[i], l[i]);
+            *A.at4(an[i] + ln, am[i] + lm, 0) = h[i];
+            *A.at4(an[i] + ln, am[i] + lm, 1) = l[i];
         }
         __syncthreads();
-        if (wave < 3)
+        // B = a I + b A + c A A, over A once every wave has read it
+        block_products<2>(A, am, A, an, R, lane, acc);
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
-                keep(v[s], A, A, 32 * sx + 16 * s + lane / 32 * 8, n, sx != sy);
+        for (int i = 0; i < 2; ++i) {
+            float v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = fmaf((float)h[i][e] + (float)l[i][e], p.lin, acc[i][e] * p.poly) +
+                       (am[i] + lm + e == an[i] + ln ? p.diag : 0.f);
+            split4(v, h[i], l[i]);
+        }
         __syncthreads();
-        // X <- B X: block column x of X, both of its blocks a wave
-        const bool mine = wave < C / 32;
-        floatx16 out[2];
-        if (mine)
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
-                out[x] = block_product(A, x, Xt, wave, 0, R / 16, lane);
+        for (int i = 0; i < 2; ++i) {
+            *A.at4(an[i] + ln, am[i] + lm, 0) = h[i];
+            *A.at4(an[i] + ln, am[i] + lm, 1) = l[i];
+        }
         __syncthreads();
-        if (mine)
+        // X <- B X: two 16-wide columns of blocks of X a wave, over X once every
+        // wave has read it
+        floatx4 out[2][4];
+        const int xm[4] = {0, 16, 32, 48};
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+        for (int j = 0; j < 2; ++j) {
+            const int c = 16 * (wave + kWholeWaves * j), xn[4] = {c, c, c, c};
+            if (c < C)
+                block_products<4>(A, xm, Xt, xn, R, lane, out[j]);
+        }
+        __syncthreads();
 #pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    rows_of(out[x], s, v[s]);
-                    const int m = 32 * x + 16 * s + lane / 32 * 8, c = 32 * wave + lane % 32;
+        for (int j = 0; j < 2; ++j) {
+            const int c = 16 * (wave + kWholeWaves * j) + ln;
+            if (c - ln >= C)
+                continue;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[s][e] *= p.apply;
-                    if (st + 1 < pr.steps) {
-                        keep(v[s], X, Xt, m, c, true);
-                        continue;
+            for (int i = 0; i < 4; ++i) {
+                const int m = 16 * i + lm;
+                float v[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    v[e] = out[j][i][e] * p.apply;
+                if (st + 1 < pr.steps) {
+                    split4(v, h[0], l[0]);
+                    *Xt.at4(c, m, 0) = h[0];
+                    *Xt.at4(c, m, 1) = l[0];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        *X.at1(m + e, c, 0) = h[0][e];
+                        *X.at1(m + e, c, 1) = l[0][e];
                     }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (m + e < it.r && c < it.c) {
-                            T *o = (T *)it.out + (tall ? (int64_t)c * it.ldo + m + e
-                                                       : (int64_t)(m + e) * it.ldo + c);
-                            if constexpr (UPDATE)
-                                *o = (T)(pr.keep * (float)*o - it.scale * v[s][e]);
-                            else
-                                *o = (T)v[s][e];
-                        }
+                    continue;
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (m + e < it.r && c < it.c) {
+                        T *o = (T *)it.out + (tall ? (int64_t)c * it.ldo + m + e
+                                                   : (int64_t)(m + e) * it.ldo + c);
+                        if constexpr (UPDATE)
+                            *o = (T)(pr.keep * (float)*o - it.scale * v[e]);
+                        else
+                            *o = (T)v[e];
+                    }
+            }
+        }
         __syncthreads();
     }
 }
