@@ -236,13 +236,9 @@ digest_status run_steps(const OrthBatch &batch, const OrthStep *plan, int32_t st
     if (digest_status st = hip_check(
             digest::launch_orth_split(batch, muon ? DIGEST_F32 : type, plan[0].ex, s), "split"))
         return st;
-    for (int32_t k = 0; k < steps; ++k)
-        if (digest_status st = hip_check(
-                digest::launch_orth_step(batch, plan[k], k + 1 == steps, muon, type, keep,
-                                         (float *)partials, s),
-                "orthogonalisation step"))
-            return st;
-    return DIGEST_OK;
+    return hip_check(digest::launch_orth_steps(batch, plan, steps, muon, type, keep,
+                                               (float *)partials, s),
+                     "orthogonalisation");
 }
 
 }  // namespace

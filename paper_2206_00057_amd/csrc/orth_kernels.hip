@@ -16,7 +16,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "device.h"
 #include "train_kernels.h"
@@ -209,19 +208,23 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
     // padded extents of U's rows and columns
     if (i0 >= (tall ? it.cp : it.rp) || j0 >= (tall ? it.rp : it.cp))
         return;
+    const T *u = (const T *)it.u;
+    constexpr int N = kSplitTile * kSplitTile / kThreads;
+    const int tj = threadIdx.x % kSplitTile, t0 = threadIdx.x / kSplitTile;
+    float x[N];   // (on their way while the norm is formed)
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const int i = i0 + t0 + q * (kThreads / kSplitTile), j = j0 + tj;
+        x[q] = i < it.rows && j < it.cols ? (float)u[(int64_t)i * it.ldu + j] : 0.f;
+    }
     double sum = 0;
     for (int i = threadIdx.x; i < it.sums; i += kThreads)
         sum += it.part[i];
     const double norm = sqrt(block_sum(sum));
     const double f = norm == 0 ? 0.0 : scale / norm;
-    const T *u = (const T *)it.u;
-    const int tj = threadIdx.x % kSplitTile;
-    for (int ti = threadIdx.x / kSplitTile; ti < kSplitTile; ti += kThreads / kSplitTile) {
-        const int i = i0 + ti, j = j0 + tj;
-        tile[ti][tj] = i < it.rows && j < it.cols
-                           ? (float)((double)(float)u[(int64_t)i * it.ldu + j] * f)
-                           : 0.f;
-    }
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+        tile[t0 + q * (kThreads / kSplitTile)][tj] = (float)((double)x[q] * f);
     __syncthreads();
     _Float16 *p = (_Float16 *)(tall ? it.Xt[0] : it.X);
     _Float16 *pt = (_Float16 *)(tall ? it.X : it.Xt[0]);
@@ -267,7 +270,7 @@ struct OrthParams {
     // Workgroups: the whole tiles [0, whole), then the parts of the others
     // (chunk lines of k each, item i's parts from work0[i] on).
     int32_t whole, chunk;
-    int32_t tile0[kOrthItems + 1], work0[kOrthItems + 1], parts[kOrthItems];
+    int32_t tile0[kOrthItems + 1], work0[kOrthItems], parts[kOrthItems];
     float *partials;
 };
 
@@ -283,37 +286,28 @@ __device__ __forceinline__ void operands(const OrthItem &it, const OrthParams &p
     Q = (const char *)(MODE == kGram ? it.X : MODE == kPoly ? it.A : it.Xt[pr.from]);
 }
 
-// Tile t of an item, tiles of BM x BN.  Symmetric products: the tiles that
-// reach above the diagonal (BM = f BN), by column.
-template <bool SYM, int BM, int BN>
+// Tile t of an item, TILE x TILE.  Symmetric products: the tiles on and above
+// the diagonal, by column.
+template <bool SYM, int TILE>
 __device__ __forceinline__ void tile_of(const OrthItem &it, int t, int &tm, int &tn)
 {
     if constexpr (SYM) {
-        constexpr int F = BM / BN;
-        // columns F j .. F j + F - 1 have j + 1 tiles each: F j (j + 1) / 2 before them
-        int j = (int)((sqrtf(8.f * (float)t / F + 1.f) - 1.f) * 0.5f);
-        while (F * (j * (j + 1) / 2) > t)
-            --j;
-        while (F * ((j + 1) * (j + 2) / 2) <= t)
-            ++j;
-        t -= F * (j * (j + 1) / 2);
-        tn = F * j + t / (j + 1);
-        tm = t % (j + 1);
+        tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+        while (tn * (tn + 1) / 2 > t)
+            --tn;
+        while ((tn + 1) * (tn + 2) / 2 <= t)
+            ++tn;
+        tm = t - tn * (tn + 1) / 2;
     } else {
-        const int gm = (it.rp + BM - 1) / BM;
+        const int gm = (it.rp + TILE - 1) / TILE;
         tm = t % gm;
         tn = t / gm;
     }
 }
-template <bool SYM, int BM, int BN>
-int tiles_of(const OrthItem &it)
+int32_t tiles_of(const OrthItem &it, bool sym, int tile)
 {
-    const int gm = (it.rp + BM - 1) / BM;
-    if (!SYM)
-        return gm * ((it.cp + BN - 1) / BN);
-    constexpr int F = BM / BN;
-    const int gn = (it.rp + BN - 1) / BN, j = gn / F;
-    return F * (j * (j + 1) / 2) + (gn - F * j) * (j + 1);
+    const int32_t gm = (it.rp + tile - 1) / tile;
+    return sym ? gm * (gm + 1) / 2 : gm * ((it.cp + tile - 1) / tile);
 }
 
 // Stores 32 columns n from nb on and 16 rows m from mb on of the product,
@@ -416,13 +410,20 @@ __device__ __forceinline__ bool stored(const OrthItem &it, int mb, int nb)
     return mb < it.rp && nb < it.cp;
 }
 
-// The large products: BM x BN of D per workgroup, WM x WN waves of TM x TN
-// blocks of 32 x 32.  One line (32 k) of both operands' rows at a time in LDS,
-// the next one on its way there.
-template <int MODE, class T, int WM, int WN, int TM, int TN>
-__global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthParams pr)
+// The large products: a TILE x TILE tile of D per workgroup, 128 (4 waves of
+// 64 x 64, two workgroups a CU) or 256 (8 waves of 128 x 64, which read each
+// line of LDS fewer times).  One line (32 k) of both operands' rows at a time
+// in LDS, the next one on its way there.
+template <int TILE>
+struct Waves {
+    static constexpr int WM = 2, WN = TILE / 64, TM = TILE / 64, TN = 2, W = WM * WN;
+    static_assert(WN * TN * 32 == TILE && WM * TM * 32 == TILE, "the waves cover the tile");
+};
+template <int MODE, class T, int TILE>
+__global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b, OrthParams pr)
 {
-    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, ROWS = (BM + BN) / 32;
+    constexpr int WN = Waves<TILE>::WN, TM = Waves<TILE>::TM, TN = Waves<TILE>::TN;
+    constexpr int W = Waves<TILE>::W, BM = TILE, BN = TILE, ROWS = (BM + BN) / 32;
     // [32 rows][16 k][part][lane]: what a matrix instruction takes is 1 KB
     __shared__ half8 lds0[ROWS * kLineBytes / 16], lds1[ROWS * kLineBytes / 16];
 
@@ -440,7 +441,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthPa
     }
     const OrthItem &it = b.item[i];
     int tm, tn, K;
-    tile_of<symmetric(MODE), BM, BN>(it, t, tm, tn);
+    tile_of<symmetric(MODE), TILE>(it, t, tm, tn);
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
@@ -542,10 +543,11 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_orth_gemm(OrthBatch b, OrthPa
 }
 
 // Sums the parts of the tiles that were split, one wave 16 rows of a block.
-template <int MODE, class T, int WM, int WN, int TM, int TN>
+template <int MODE, class T, int TILE>
 __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams pr)
 {
-    constexpr int W = WM * WN, BM = WM * TM * 32, BN = WN * TN * 32, UNITS = W * TM * TN * 2;
+    constexpr int WN = Waves<TILE>::WN, TM = Waves<TILE>::TM, TN = Waves<TILE>::TN;
+    constexpr int BM = TILE, BN = TILE, UNITS = Waves<TILE>::W * TM * TN * 2;
     __shared__ uint32_t turn[kThreads / kWave][kTurn];
     const int lane = threadIdx.x % kWave;
     const int at = blockIdx.x * (kThreads / kWave) + wave_id();
@@ -556,7 +558,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
     const OrthItem &it = b.item[i];
     const int first = max(pr.whole, pr.tile0[i]);   // the item's first split tile
     int tm, tn;
-    tile_of<symmetric(MODE), BM, BN>(it, tile - pr.tile0[i], tm, tn);
+    tile_of<symmetric(MODE), TILE>(it, tile - pr.tile0[i], tm, tn);
     const int blk = at % UNITS / 2, s = at % 2;
     const int wave = blk / (TM * TN), x = blk / TN % TM, y = blk % TN;
     const int mb = tm * BM + (wave / WN * TM + x) * 32, nb = tn * BN + (wave % WN * TN + y) * 32;
@@ -604,7 +606,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         ++i;
     const OrthItem &it = b.item[i];
     int tm, tn, K;
-    tile_of<symmetric(MODE), TILE, TILE>(it, w - pr.tile0[i], tm, tn);
+    tile_of<symmetric(MODE), TILE>(it, w - pr.tile0[i], tm, tn);
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
@@ -925,104 +927,134 @@ __global__ __launch_bounds__(kWholeThreads) void k_orth_whole(OrthBatch b, Whole
     }
 }
 
-// The large kernel's shapes, and its workgroups on the card at a time.
-#ifndef ORTH_FULL
-#define ORTH_FULL 2, 4, 4, 2
-#define ORTH_HALF 2, 2, 4, 2
-#endif
-struct ShapeOf {
-    int wm, wn, tm, tn;
-    constexpr int bm() const { return wm * tm * 32; }
-    constexpr int bn() const { return wn * tn * 32; }
+// How the products of one kind run: the kernel, by its tile, and its
+// workgroups.
+struct OrthPlan {
+    OrthParams pr;
+    int32_t tile, blocks;   // 32 and 64: k_orth_small, 128 and 256: k_orth_gemm
+    int32_t joins;          // split tiles, for k_orth_join
 };
-constexpr ShapeOf kFull = {ORTH_FULL}, kHalf = {ORTH_HALF};
-constexpr ShapeOf shape_of(int mode) { return symmetric(mode) ? kHalf : kFull; }
-#ifndef ORTH_SLOTS
-#define ORTH_SLOTS 256
-#endif
-constexpr int kSlots = ORTH_SLOTS;
-#ifndef ORTH_MINCHUNK
-#define ORTH_MINCHUNK 4
-#endif
-constexpr int kMinChunk = ORTH_MINCHUNK;   // lines of a part, at least (an even number each)
 
-int lines_of(const OrthItem &it, int mode)
-{
-    return (mode == kGram ? it.ck : it.rk) / kBlockK;
-}
+constexpr int kSlots = 256;    // CUs
+constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each)
 
-// Splits the k of the tiles that are left over when the whole ones have
-// filled the card's slots evenly: into as many parts as there are slots.
+// The fastest of the kernels by their times in us, as measured (MI355X, fp32
+// 256 x 256 to 4,096 x 4,096; lines are 32 k):
+//   32    5.5 + 0.6 a line of a wave, 3 + 5.3e-3 for each line of each tile's
+//         waves once the card is full
+//   64    1 + (4.5 + 1.65 a line of a wave) for each 256 tiles
+//   128   5.5 + 0.78 a line with one workgroup a CU, 1.54 with two
+//   256   8 + 2.7 a line (3.1 for the four tiles of 128 with two a CU)
+// A tile's k may be split where tiles are few or left over by the whole ones:
+// the join takes 4 and 0.013 (128) or 0.052 (256) for each part that it reads.
 template <int MODE>
-int32_t plan_tiles(const OrthBatch &b, OrthParams &pr)
+OrthPlan plan_products(const OrthBatch &b)
 {
     constexpr bool SYM = symmetric(MODE);
-    pr.tile0[0] = 0;
-    for (int i = 0; i < b.n; ++i)
-        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<SYM, shape_of(MODE).bm(), shape_of(MODE).bn()>(b.item[i]);
-    const int32_t tiles = pr.tile0[b.n];
-    pr.whole = tiles - tiles % kSlots;
-    auto parts = [&](int chunk) {
-        int32_t n = 0;
-        for (int i = 0; i < b.n; ++i) {
-            const int left = pr.tile0[i + 1] - std::max(pr.whole, pr.tile0[i]);
-            const int lines = lines_of(b.item[i], MODE);
-            pr.parts[i] = (lines + chunk - 1) / chunk;
-            pr.work0[i] = pr.whole + n;
-            if (left > 0)
-                n += left * pr.parts[i];
-        }
-        pr.work0[b.n] = pr.whole + n;
-        return n;
-    };
-    int most = 0;
-    for (int i = 0; i < b.n; ++i)
-        most = std::max(most, lines_of(b.item[i], MODE));
-    pr.chunk = kMinChunk;
-    while (pr.chunk < most && parts(pr.chunk) > kSlots)
-        pr.chunk += std::max(2, pr.chunk / 32 * 2);
-    const int32_t n = parts(pr.chunk);
-    if (n == tiles - pr.whole) {   // nothing to split
-        pr.whole = tiles;
-        return tiles;
+    OrthPlan best{};
+    double time = 1e300;
+    int32_t lines[kOrthItems], most = 0;
+    for (int i = 0; i < b.n; ++i) {
+        lines[i] = (MODE == kGram ? b.item[i].ck : b.item[i].rk) / kBlockK;
+        most = std::max(most, lines[i]);
     }
-    return pr.whole + n;
+    auto start = [&](int tile) {
+        OrthPlan p{};
+        p.tile = tile;
+        for (int i = 0; i < b.n; ++i)
+            p.pr.tile0[i + 1] = p.pr.tile0[i] + tiles_of(b.item[i], SYM, tile);
+        p.blocks = p.pr.whole = p.pr.tile0[b.n];
+        return p;
+    };
+    auto consider = [&](const OrthPlan &p, double t) {
+        if (t < time) {
+            time = t;
+            best = p;
+        }
+    };
+    const double waves = (most + kSmallWaves - 1) / kSmallWaves;
+    {
+        const OrthPlan p = start(32);
+        double all = 0;
+        for (int i = 0; i < b.n; ++i)
+            all += (double)(p.pr.tile0[i + 1] - p.pr.tile0[i]) *
+                   ((lines[i] + kSmallWaves - 1) / kSmallWaves);
+        consider(p, std::max(5.5 + 0.6 * waves, 3 + 5.3e-3 * all));
+    }
+    {
+        const OrthPlan p = start(64);
+        consider(p, 1 + (p.blocks + kSlots - 1) / kSlots * (4.5 + 1.65 * waves));
+    }
+    for (int tile = 128; tile <= 256; tile *= 2) {
+        const OrthPlan all = start(tile);
+        const int per_cu = tile == 128 ? 2 : 1;
+        const double full = tile == 128 ? 1.54 : 2.7, alone = tile == 128 ? 0.78 : 2.7;
+        const double base = tile == 128 ? 5.5 : 8, part = tile == 128 ? 0.013 : 0.052;
+        const int32_t tiles = all.blocks;
+        // workgroups of `c` lines on their own
+        auto run = [&](double n, double c) {
+            const double rounds = std::floor(n / (per_cu * kSlots)), left = n - rounds * per_cu * kSlots;
+            return c * (rounds * full + (left > kSlots ? full : left > 0 ? alone : 0));
+        };
+        consider(all, base + run(tiles, most));
+        for (int w = 0; w <= per_cu; ++w) {   // whole tiles: none, or all but what is left over
+            OrthPlan p = all;
+            p.pr.whole = w ? tiles - tiles % (w * kSlots) : 0;
+            if (p.pr.whole == tiles || (w && p.pr.whole == 0))
+                continue;
+            for (int split = 2; split <= 16; split += split < 4 ? 1 : split / 4 * 2) {
+                p.pr.chunk = ((most + split - 1) / split + 1) / 2 * 2;
+                if (p.pr.chunk < kMinChunk)
+                    break;
+                p.joins = tiles - p.pr.whole;
+                int32_t n = 0;
+                for (int i = 0; i < b.n; ++i) {
+                    const int32_t left = p.pr.tile0[i + 1] - std::max(p.pr.whole, p.pr.tile0[i]);
+                    p.pr.parts[i] = (lines[i] + p.pr.chunk - 1) / p.pr.chunk;
+                    p.pr.work0[i] = p.pr.whole + n;
+                    n += std::max(0, left) * p.pr.parts[i];
+                }
+                p.blocks = p.pr.whole + n;
+                double t = base + 4 + part * n;
+                if (p.pr.whole % (per_cu * kSlots) == 0) {
+                    t += run(p.pr.whole, most) + run(n, p.pr.chunk);
+                } else {
+                    // one whole tile on each CU, parts beside it in turn
+                    const double beside = (n + kSlots - 1) / kSlots * (double)p.pr.chunk;
+                    t += run(p.pr.whole - kSlots, most) + std::min<double>(beside, most) * full +
+                         std::max<double>(0, most - beside) * alone +
+                         std::max<double>(0, beside - most) * full / 2;
+                }
+                consider(p, t);
+            }
+        }
+    }
+    return best;
 }
 
-// 32 x 32 and 64 x 64 tiles up to which the small kernel is the faster one.
-#ifndef ORTH_T32
-#define ORTH_T32 512
-#endif
-constexpr int kTiles32 = ORTH_T32, kTiles64 = 512;
-template <int MODE, int TILE>
-int32_t small_tiles(const OrthBatch &b, OrthParams &pr)
+template <int MODE, class T, int TILE>
+void gemm(const OrthBatch &b, const OrthPlan &p, hipStream_t s)
 {
-    pr.tile0[0] = 0;
-    for (int i = 0; i < b.n; ++i)
-        pr.tile0[i + 1] = pr.tile0[i] + tiles_of<symmetric(MODE), TILE, TILE>(b.item[i]);
-    return pr.tile0[b.n];
+    k_orth_gemm<MODE, T, TILE><<<p.blocks, Waves<TILE>::W * kWave, 0, s>>>(b, p.pr);
+    if (p.joins > 0)
+        k_orth_join<MODE, T, TILE>
+            <<<p.joins * (TILE / 32) * (TILE / 32) * 2 / (kThreads / kWave), kThreads, 0, s>>>(b, p.pr);
 }
 
 template <int MODE, class T>
-hipError_t gemm(const OrthBatch &b, OrthParams pr, hipStream_t s)
+hipError_t product(const OrthBatch &b, const OrthPlan &p, hipStream_t s)
 {
-    int32_t n = small_tiles<MODE, 32>(b, pr);
-    if (n <= kTiles32) {
-        k_orth_small<MODE, T, 1, 4><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
-        return hipGetLastError();
+    switch (p.tile) {
+    case 32:
+        k_orth_small<MODE, T, 1, 4><<<p.blocks, kSmallWaves * kWave, 0, s>>>(b, p.pr);
+        break;
+    case 64:
+        k_orth_small<MODE, T, 2, 2><<<p.blocks, kSmallWaves * kWave, 0, s>>>(b, p.pr);
+        break;
+    case 128: gemm<MODE, T, 128>(b, p, s); break;
+    case 256: gemm<MODE, T, 256>(b, p, s); break;
+    default: return hipErrorInvalidValue;
     }
-    n = small_tiles<MODE, 64>(b, pr);
-    if (n <= kTiles64) {
-        k_orth_small<MODE, T, 2, 2><<<n, kSmallWaves * kWave, 0, s>>>(b, pr);
-        return hipGetLastError();
-    }
-    n = plan_tiles<MODE>(b, pr);
-    constexpr ShapeOf S = shape_of(MODE);
-    k_orth_gemm<MODE, T, S.wm, S.wn, S.tm, S.tn><<<n, S.wm * S.wn * kWave, 0, s>>>(b, pr);
-    if (pr.whole < pr.tile0[b.n])
-        k_orth_join<MODE, T, S.wm, S.wn, S.tm, S.tn>
-            <<<(pr.tile0[b.n] - pr.whole) * (S.bm() / 32) * (S.bn() / 32) * 2 / (kThreads / kWave),
-               kThreads, 0, s>>>(b, pr);
     return hipGetLastError();
 }
 
@@ -1105,46 +1137,46 @@ hipError_t launch_orth_whole(const OrthBatch &b, const OrthStep *st, int32_t ste
 size_t orth_partials(const OrthBatch &b)
 {
     size_t most = 0;
-    auto add = [&](auto mode) {
-        constexpr int MODE = decltype(mode)::value;
-        OrthParams pr{};
-        if (small_tiles<MODE, 64>(b, pr) > kTiles64) {
-            const int32_t parts = plan_tiles<MODE>(b, pr) - pr.whole;
-            most = std::max(most, (size_t)parts * shape_of(MODE).bm() * shape_of(MODE).bn() * 4);
-        }
-    };
-    add(std::integral_constant<int, kGram>());
-    add(std::integral_constant<int, kPoly>());
-    add(std::integral_constant<int, kApply>());
+    for (const OrthPlan &p : {plan_products<kGram>(b), plan_products<kPoly>(b), plan_products<kApply>(b)})
+        most = std::max(most, (size_t)(p.blocks - p.pr.whole) * p.tile * p.tile * sizeof(float));
     return most;
 }
 
-hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
-                            int32_t type, float keep, float *partials, hipStream_t s)
+hipError_t launch_orth_steps(const OrthBatch &b, const OrthStep *steps, int32_t n, bool muon,
+                             int32_t type, float keep, float *partials, hipStream_t s)
 {
-    OrthParams pr{};
-    pr.partials = partials;
-    pr.keep = keep;
-    pr.from = st.from;
-    pr.alpha = std::ldexp(1.f, st.ea - 2 * st.ex);
-    if (hipError_t e = gemm<kGram, float>(b, pr, s))
-        return e;
-    pr.alpha = std::ldexp(st.c, st.eb - 2 * st.ea);
-    pr.lin = std::ldexp(st.b, st.eb - st.ea);
-    pr.diag = std::ldexp(st.a, st.eb);
-    if (hipError_t e = gemm<kPoly, float>(b, pr, s))
-        return e;
-    pr.alpha = std::ldexp(1.f, (last ? 0 : st.en) - st.eb - st.ex);
-    if (!last)
-        return gemm<kApply, float>(b, pr, s);
-    if (muon)
-        return gemm<kUpdate, float>(b, pr, s);
-    switch (type) {
-    case kF32: return gemm<kResult, float>(b, pr, s);
-    case kBF16: return gemm<kResult, __bf16>(b, pr, s);
-    case kF16: return gemm<kResult, _Float16>(b, pr, s);
+    OrthPlan gram = plan_products<kGram>(b), poly = plan_products<kPoly>(b),
+             apply = plan_products<kApply>(b);
+    gram.pr.partials = poly.pr.partials = apply.pr.partials = partials;
+    apply.pr.keep = keep;
+    for (int32_t k = 0; k < n; ++k) {
+        const OrthStep &st = steps[k];
+        const bool last = k + 1 == n;
+        gram.pr.alpha = std::ldexp(1.f, st.ea - 2 * st.ex);
+        poly.pr.alpha = std::ldexp(st.c, st.eb - 2 * st.ea);
+        poly.pr.lin = std::ldexp(st.b, st.eb - st.ea);
+        poly.pr.diag = std::ldexp(st.a, st.eb);
+        apply.pr.alpha = std::ldexp(1.f, (last ? 0 : st.en) - st.eb - st.ex);
+        apply.pr.from = st.from;
+        if (hipError_t e = product<kGram, float>(b, gram, s))
+            return e;
+        if (hipError_t e = product<kPoly, float>(b, poly, s))
+            return e;
+        hipError_t e = hipErrorInvalidValue;
+        if (!last)
+            e = product<kApply, float>(b, apply, s);
+        else if (muon)
+            e = product<kUpdate, float>(b, apply, s);
+        else if (type == kF32)
+            e = product<kResult, float>(b, apply, s);
+        else if (type == kBF16)
+            e = product<kResult, __bf16>(b, apply, s);
+        else if (type == kF16)
+            e = product<kResult, _Float16>(b, apply, s);
+        if (e != hipSuccess)
+            return e;
     }
-    return hipErrorInvalidValue;
+    return hipSuccess;
 }
 
 }  // namespace digest

@@ -59,7 +59,7 @@ struct OrthBatch {
 struct OrthGrads {
     const float *g[kOrthGrads];      // item i: g[i * per_item ..]
 };
-// Scale exponents of one step: planes hold value * 2^e.
+// One step: its coefficients, and scale exponents (planes hold value * 2^e).
 struct OrthStep {
     float a, b, c;
     int32_t ex, ea, eb, en;          // X, A, B, and X after the step
@@ -80,9 +80,9 @@ size_t orth_partials(const OrthBatch &b);
 constexpr int kWholeRows = 64, kWholeCols = 256, kWholeSteps = 16;
 hipError_t launch_orth_whole(const OrthBatch &b, const OrthStep *st, int32_t steps, bool muon,
                              int32_t type, float keep, hipStream_t s);
-// One step.  last: the result goes to out, as `type`, or (muon) into the
-// weights: out <- keep out - scale O.
-hipError_t launch_orth_step(const OrthBatch &b, const OrthStep &st, bool last, bool muon,
-                            int32_t type, float keep, float *partials, hipStream_t s);
+// The steps.  The result goes to out, as `type`, or (muon) into the weights:
+// out <- keep out - scale O.
+hipError_t launch_orth_steps(const OrthBatch &b, const OrthStep *steps, int32_t n, bool muon,
+                             int32_t type, float keep, float *partials, hipStream_t s);
 
 }  // namespace digest
