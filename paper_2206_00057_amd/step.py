@@ -1,6 +1,7 @@
 """One DIGEST training round of one partition on the GPU, as a sequence of
 library calls (Algorithm 1's inner loop for a single subgraph), for the GCN
-layer of Eq. 5 or the GAT layer over stale halo rows:
+layer of Eq. 5 or the GAT layer over stale halo rows, with a layer norm behind
+the hidden layers if asked for:
 
     for l = 1..L:   pull level l-1 if the schedule says so (levels >= 1),
                     layer forward, push level l if the schedule says so
@@ -29,9 +30,12 @@ from . import digest as D
 
 class GpuPartition:
     def __init__(self, n_global, part, widths, device="cuda", overlap_io=False, model="gcn",
-                 atts=None, pull_mode=None):
+                 atts=None, pull_mode=None, norms=None):
         """model "gcn" (Eq. 5) or "gat" (the attention layer over stale halo
         rows; atts are its per-layer [d_l, 2] attention matrices).
+        norms: None, or for each hidden layer 1..L-1 its (gain, shift), device
+        float32 [d_l]: a layer norm between the layer and its ReLU, so that
+        H[l] = relu(norm(Z[l])) with Z[l] the layer's own output.
         pull_mode: what a pull keeps (D.PULL_ROWS or D.PULL_AGGREGATE); by
         default the halo aggregate alone for the GCN layer, the halo rows
         for the GAT layer, which reads them."""
@@ -39,7 +43,9 @@ class GpuPartition:
             raise ValueError("model is gcn or gat")
         if model == "gat" and (atts is None or len(atts) != len(widths) - 1):
             raise ValueError("a GAT model needs one attention matrix per layer")
-        self.model, self.atts = model, atts
+        if norms is not None and len(norms) != len(widths) - 2:
+            raise ValueError("a normalised model needs (gain, shift) for each hidden layer")
+        self.model, self.atts, self.norms = model, atts, norms
         self.widths = [int(w) for w in widths]
         self.L = len(self.widths) - 1
         self.device = device
@@ -65,6 +71,16 @@ class GpuPartition:
                             for l in range(1, self.L + 1)]
         self.dAtt = ([None] + [torch.empty(self.widths[l], 2, **f32) for l in range(1, self.L + 1)]
                      if model == "gat" else None)
+        if norms is not None:
+            # layer outputs before the norm, rows' (mean, 1/std), parameter gradients
+            hidden = range(1, self.L)
+            self.Z = [None] + [torch.empty(n, self.widths[l], **f32) for l in hidden]
+            self.stats = [None] + [torch.empty(n, 2, **f32) for l in hidden]
+            self.dGain = [None] + [torch.empty(self.widths[l], **f32) for l in hidden]
+            self.dShift = [None] + [torch.empty(self.widths[l], **f32) for l in hidden]
+            self.norm_workspace = torch.empty(
+                max([D.digest_layer_norm_query(n, self.widths[l]) for l in hidden] + [256]),
+                dtype=torch.uint8, device=device)
         self.loss = torch.zeros(1, **f32)
         self.graphs = {}
         # pulls and pushes: on their own stream (default priority) next to the
@@ -76,12 +92,40 @@ class GpuPartition:
     def act(self, layer):
         return D.ACT_RELU if layer < self.L else D.ACT_IDENTITY
 
-    def _layer(self, l, h, W, stream=None):
+    def normed(self, layer):
+        return self.norms is not None and layer < self.L
+
+    def layer_forward(self, l, h, W, stream=None):
+        """H[l] from the rows h of level l-1."""
+        normed = self.normed(l)
+        out, act = (self.Z[l], D.ACT_IDENTITY) if normed else (self.H[l], self.act(l))
         if self.model == "gat":
-            D.digest_gat_forward(self.p, l, h, W, self.atts[l - 1], self.H[l], self.act(l),
-                                 stream=stream)
+            D.digest_gat_forward(self.p, l, h, W, self.atts[l - 1], out, act, stream=stream)
         else:
-            D.digest_layer_forward(self.p, l, h, W, self.H[l], self.act(l), stream=stream)
+            D.digest_layer_forward(self.p, l, h, W, out, act, stream=stream)
+        if normed:
+            gain, shift = self.norms[l - 1]
+            D.digest_layer_norm_forward(out, gain, shift, self.H[l], self.stats[l],
+                                        act=self.act(l), stream=stream)
+
+    def layer_backward(self, l, h_in, W, dh_in, dh_halo=None):
+        """dW[l] (with the norm's and the attention's gradients) and dh_in, if
+        not None, from dH[l], which a normalised layer replaces by dZ[l];
+        dh_halo: also the halo rows' gradient (GCN layers)."""
+        out = self.H[l]
+        if self.normed(l):
+            out = self.Z[l]
+            D.digest_layer_norm_backward(out, self.norms[l - 1][0], self.H[l], self.dH[l],
+                                         self.stats[l], self.dH[l], self.dGain[l],
+                                         self.dShift[l], self.norm_workspace, self.act(l))
+        if self.model == "gat":
+            D.digest_gat_backward(self.p, l, h_in, out, self.dH[l], W, self.atts[l - 1],
+                                  self.dW[l], self.dAtt[l], dh_in)
+        elif dh_halo is not None:
+            D.digest_layer_backward_halo(self.p, l, h_in, out, self.dH[l], W, self.dW[l], dh_in,
+                                         dh_halo)
+        else:
+            D.digest_layer_backward(self.p, l, h_in, out, self.dH[l], W, self.dW[l], dh_in)
 
     def pull_all(self, stores):
         """Initial pull of every level (level 0 = features)."""
@@ -105,7 +149,7 @@ class GpuPartition:
         for l in range(1, self.L + 1):
             if pulled and l >= 2:
                 main.wait_event(self.pull_done[l - 1])
-            self._layer(l, h, Ws[l - 1])
+            self.layer_forward(l, h, Ws[l - 1])
             if do_push and l <= self.L - 1:
                 self.io.wait_stream(main)
                 with torch.cuda.stream(self.io):
@@ -120,7 +164,7 @@ class GpuPartition:
         for l in range(1, self.L + 1):
             if do_pull and l >= 2:
                 D.digest_pull(self.p, l - 1, stores[l - 1])
-            self._layer(l, h, Ws[l - 1])
+            self.layer_forward(l, h, Ws[l - 1])
             if do_push and l <= self.L - 1:
                 D.digest_push(self.p, l, self.H[l], stores[l])
             h = self.H[l]
@@ -131,12 +175,7 @@ class GpuPartition:
         for l in range(self.L, 0, -1):
             dh_in = self.dH[l - 1] if l > 1 else None
             h_in = self.H[l - 1] if l > 1 else self.x_own
-            if self.model == "gat":
-                D.digest_gat_backward(self.p, l, h_in, self.H[l], self.dH[l], Ws[l - 1],
-                                      self.atts[l - 1], self.dW[l], self.dAtt[l], dh_in)
-            else:
-                D.digest_layer_backward(self.p, l, h_in, self.H[l], self.dH[l], Ws[l - 1],
-                                        self.dW[l], dh_in)
+            self.layer_backward(l, h_in, Ws[l - 1], dh_in)
 
     def round(self, r, K, x_own, Ws, stores, labels):
         """Round r (1-based) with sync interval K, eagerly."""

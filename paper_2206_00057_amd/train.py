@@ -32,6 +32,11 @@ rows as constants.
 model="gat" trains GAT layers over stale halo rows instead of Eq. 5; AGG
 then averages the attention matrices as well as W.
 
+norms puts a layer norm between each hidden layer and its ReLU (the pushed
+rows are the normalised ones); optimizer="muon" replaces the plain step of
+the weight matrices by digest_muon_average, whose momenta are global
+parameters' state (`momenta`, zero at the start).
+
 All arithmetic runs in libdigest.so (the layers, pulls, pushes, loss heads
 and the parameter averaging); this module owns the buffers and orders the
 calls.  ``capture`` records one round per pull/push pattern into a HIP graph.
@@ -59,19 +64,27 @@ def boundary_push_mode(gps, parts):
 
 class DigestTrainer:
     def __init__(self, n_global, parts, widths, x, labels, weights, lr, K, device="cuda",
-                 grad_exchange="none", model="gcn", atts=None):
+                 grad_exchange="none", model="gcn", atts=None, norms=None, optimizer="sgd",
+                 beta=0.95, decay=0.0):
         """parts: synth-style partitions (owned, halo, CSR rows) covering the
         graph; x: device [n_global, d_0] features; labels: device int32
         [n_global]; weights: device float32 tensors W_1..W_L (the global
-        parameters, updated in place by every round)."""
+        parameters, updated in place by every round); norms: None, or (gain,
+        shift) of a layer norm for each hidden layer, updated likewise.
+        optimizer "muon" steps the weight matrices by the orthogonalised
+        momentum (decay, beta) of their mean gradients; attention matrices,
+        gains and shifts take the plain step at every setting."""
         if not 1 <= len(parts) <= 64:
             raise ValueError("between 1 and 64 subgraphs")
         if grad_exchange not in ("none", "fresh", "stale"):
             raise ValueError("grad_exchange is none, fresh or stale")
         if model == "gat" and grad_exchange != "none":
             raise ValueError("the halo-gradient exchange is defined for GCN layers")
+        if optimizer not in ("sgd", "muon"):
+            raise ValueError("optimizer is sgd or muon")
         self.grad_exchange = grad_exchange
-        self.model = model
+        self.model, self.norms = model, norms
+        self.optimizer, self.beta, self.decay = optimizer, float(beta), float(decay)
         self.att = atts   # GAT: device [d_l, 2] attention matrices, updated in place
         self.widths = [int(w) for w in widths]
         self.L = len(self.widths) - 1
@@ -80,7 +93,8 @@ class DigestTrainer:
         self.W = weights
         # pulls keep the halo aggregate alone for GCN layers, the halo rows
         # for GAT layers (GpuPartition's default)
-        self.gps = [GpuPartition(n_global, p, widths, device=device, model=model, atts=atts)
+        self.gps = [GpuPartition(n_global, p, widths, device=device, model=model, atts=atts,
+                                 norms=norms)
                     for p in parts]
         self.push_mode = boundary_push_mode(self.gps, parts)
         idx = [torch.from_numpy(p.owned).to(device) for p in parts]
@@ -91,6 +105,14 @@ class DigestTrainer:
         self.stores = [x] + [torch.zeros(n_global, self.widths[l], **f32)
                              for l in range(1, self.L)]
         self.losses = torch.zeros(len(parts), **f32)
+        if optimizer == "muon":
+            shapes = [tuple(w.shape) for w in weights]
+            self.momenta = [torch.zeros_like(w) for w in weights]
+            # each singular direction of the step has the same effect on a row
+            # whatever the layer's widths
+            self.scales = [max(1.0, d_out / d_in) ** 0.5 for d_in, d_out in shapes]
+            self.muon_workspace = torch.empty(D.digest_orthogonalize_query(shapes),
+                                              dtype=torch.uint8, device=device)
         if grad_exchange != "none":
             # gradient stores (levels 1..L-1) and each subgraph's halo gradients
             self.gstores = [None] + [torch.zeros(n_global, self.widths[l], **f32)
@@ -109,12 +131,6 @@ class DigestTrainer:
     def act(self, layer):
         return D.ACT_RELU if layer < self.L else D.ACT_IDENTITY
 
-    def _fwd(self, gp, l, h):
-        if self.model == "gat":
-            D.digest_gat_forward(gp.p, l, h, self.W[l - 1], self.att[l - 1], gp.H[l], self.act(l))
-        else:
-            D.digest_layer_forward(gp.p, l, h, self.W[l - 1], gp.H[l], self.act(l))
-
     def init_stores(self):
         """Fill the store with one forward of all subgraphs at the current W
         with fresh halo rows (a round-0 pass that pulls before and pushes
@@ -126,7 +142,7 @@ class DigestTrainer:
             for m, gp in enumerate(self.gps):
                 if l >= 2:
                     D.digest_pull(gp.p, l - 1, self.stores[l - 1])
-                self._fwd(gp, l, h[m])
+                gp.layer_forward(l, h[m], self.W[l - 1])
             for gp in self.gps:
                 D.digest_push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
             h = [gp.H[l] for gp in self.gps]
@@ -141,7 +157,7 @@ class DigestTrainer:
                 for gp in self.gps:
                     D.digest_pull(gp.p, l - 1, self.stores[l - 1])
             for m, gp in enumerate(self.gps):
-                self._fwd(gp, l, h[m])
+                gp.layer_forward(l, h[m], self.W[l - 1])
             if do_push and l <= self.L - 1:
                 for gp in self.gps:
                     D.digest_push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
@@ -154,23 +170,29 @@ class DigestTrainer:
             for m, gp in enumerate(self.gps):
                 dh_in = gp.dH[l - 1] if l > 1 else None
                 h_in = gp.H[l - 1] if l > 1 else self.x_own[m]
-                if self.model == "gat":
-                    D.digest_gat_backward(gp.p, l, h_in, gp.H[l], gp.dH[l], self.W[l - 1],
-                                          self.att[l - 1], gp.dW[l], gp.dAtt[l], dh_in)
-                elif exch and l > 1:
-                    # the halo gradient comes out of the backward's own products
-                    D.digest_layer_backward_halo(gp.p, l, h_in, gp.H[l], gp.dH[l],
-                                                 self.W[l - 1], gp.dW[l], dh_in,
-                                                 self.dh_halo[m][l - 1])
-                else:
-                    D.digest_layer_backward(gp.p, l, h_in, gp.H[l], gp.dH[l], self.W[l - 1],
-                                            gp.dW[l], dh_in)
+                # (with the exchange the halo gradient comes out of the
+                # backward's own products)
+                gp.layer_backward(l, h_in, self.W[l - 1], dh_in,
+                                  self.dh_halo[m][l - 1] if exch and l > 1 else None)
             if exch and l > 1:
                 self._exchange(l)
-        for l in range(1, self.L + 1):
-            D.digest_sgd_average(self.W[l - 1], [gp.dW[l] for gp in self.gps], self.lr)
+        self._update()
+
+    def _update(self):
+        """AGG: the global parameters from the subgraphs' gradients."""
+        layers = range(1, self.L + 1)
+        if self.optimizer == "muon":
+            D.digest_muon_average(self.W, self.momenta,
+                                  [[gp.dW[l] for gp in self.gps] for l in layers],
+                                  self.muon_workspace, self.lr, self.beta, self.decay, self.scales)
+        for l in layers:
+            if self.optimizer == "sgd":
+                D.digest_sgd_average(self.W[l - 1], [gp.dW[l] for gp in self.gps], self.lr)
             if self.model == "gat":
                 D.digest_sgd_average(self.att[l - 1], [gp.dAtt[l] for gp in self.gps], self.lr)
+            if self.norms is not None and l < self.L:
+                for v, g in zip(self.norms[l - 1], ("dGain", "dShift")):
+                    D.digest_sgd_average(v, [getattr(gp, g)[l] for gp in self.gps], self.lr)
 
     def _exchange(self, l):
         """The halo gradients of layer l (from the backward) into the level
