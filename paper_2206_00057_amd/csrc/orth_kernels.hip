@@ -277,6 +277,17 @@ struct OrthParams {
 typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 
+// The item whose range of `first` (ascending; entries past the last item are
+// beyond every v) holds v: all of it read at once, no search.
+__device__ __forceinline__ int item_of(const int32_t *first, int v)
+{
+    int i = 0;
+#pragma unroll
+    for (int j = 1; j < kOrthItems; ++j)
+        i += v >= first[j];
+    return i;
+}
+
 template <int MODE>
 __device__ __forceinline__ void operands(const OrthItem &it, const OrthParams &pr, int &K,
                                          const char *&P, const char *&Q)
@@ -315,9 +326,21 @@ int32_t tiles_of(const OrthItem &it, bool sym, int tile)
 // + 7.  `mirror`: the transposed is nobody else's to store.  `turn` is the
 // wave's own LDS.
 constexpr int kTurn = 32 * 20;
+// kPoly's elements of A there: A is symmetric, row n holds the eight side by side.
+struct Eights {
+    half8 h, l;
+    __device__ __forceinline__ void load(const OrthItem &it, int mb, int nb)
+    {
+        const int lane = threadIdx.x % kWave;
+        const _Float16 *a = (const _Float16 *)it.A +
+                            plane_at(nb + lane % 32, it.rk, mb + lane / 32 * 8);
+        h = *reinterpret_cast<const half8 *>(a);
+        l = *reinterpret_cast<const half8 *>(a + kPart);
+    }
+};
 template <int MODE, class T>
 __device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, int mb, int nb,
-                                    float (&v)[8], bool mirror, uint32_t *turn)
+                                    float (&v)[8], const Eights &a, bool mirror, uint32_t *turn)
 {
     const int lane = threadIdx.x % kWave;
     const int m = mb + lane / 32 * 8, n = nb + lane % 32;
@@ -325,13 +348,10 @@ __device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, in
     for (int e = 0; e < 8; ++e)
         v[e] *= pr.alpha;
     if constexpr (MODE == kPoly) {
-        // (A is symmetric: its row n holds the eight side by side)
-        const _Float16 *a = (const _Float16 *)it.A + plane_at(n, it.rk, m);
-        const half8 h = *reinterpret_cast<const half8 *>(a);
-        const half8 l = *reinterpret_cast<const half8 *>(a + kPart);
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-            v[e] = fmaf((float)h[e] + (float)l[e], pr.lin, v[e]) + (m + e == n ? pr.diag : 0.f);
+            v[e] = fmaf((float)a.h[e] + (float)a.l[e], pr.lin, v[e]) +
+                   (m + e == n ? pr.diag : 0.f);
     }
     if constexpr (MODE == kGram || MODE == kPoly || MODE == kApply) {
         union {
@@ -427,15 +447,13 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
     // [32 rows][16 k][part][lane]: what a matrix instruction takes is 1 KB
     __shared__ half8 lds0[ROWS * kLineBytes / 16], lds1[ROWS * kLineBytes / 16];
 
-    int w = blockIdx.x, i = 0, t, part = -1;
+    int w = blockIdx.x, i, t, part = -1;
     if (w < pr.whole) {
         w = (int)xcd_contiguous(w, pr.whole);
-        while (i + 1 < b.n && w >= pr.tile0[i + 1])
-            ++i;
+        i = item_of(pr.tile0, w);
         t = w - pr.tile0[i];
     } else {
-        while (i + 1 < b.n && w >= pr.work0[i + 1])
-            ++i;
+        i = item_of(pr.work0, w);
         part = (w - pr.work0[i]) % pr.parts[i];
         t = max(pr.whole - pr.tile0[i], 0) + (w - pr.work0[i]) / pr.parts[i];
     }
@@ -526,8 +544,11 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
                     float v[8];
+                    Eights a;
+                    if constexpr (MODE == kPoly)
+                        a.load(it, mb + 16 * s, nb);
                     rows_of(acc[x][y], s, v);
-                    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn);
+                    put<MODE, T>(it, pr, mb + 16 * s, nb, v, a, !symmetric(MODE) || mb != nb, turn);
                 }
             } else {
 #pragma unroll
@@ -552,9 +573,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
     const int lane = threadIdx.x % kWave;
     const int at = blockIdx.x * (kThreads / kWave) + wave_id();
     const int tile = pr.whole + at / UNITS;
-    int i = 0;
-    while (i + 1 < b.n && tile >= pr.tile0[i + 1])
-        ++i;
+    const int i = item_of(pr.tile0, tile);
     const OrthItem &it = b.item[i];
     const int first = max(pr.whole, pr.tile0[i]);   // the item's first split tile
     int tm, tn;
@@ -568,6 +587,9 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
     const float *src = pr.partials +
                        (int64_t)(pr.work0[i] - pr.whole + (tile - first) * pr.parts[i]) * (BM * BN) +
                        ((blk * 4 + 2 * s + lane / 32) * kWave + lane % 32) * 4;
+    Eights a;
+    if constexpr (MODE == kPoly)
+        a.load(it, mb + 16 * s, nb);
     float v[8] = {};
     constexpr int U = 8;   // parts in flight
     for (int p0 = 0; p0 < pr.parts[i]; p0 += U) {
@@ -585,7 +607,7 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
                 v[4] += f[u][1].x, v[5] += f[u][1].y, v[6] += f[u][1].z, v[7] += f[u][1].w;
             }
     }
-    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave_id()]);
+    put<MODE, T>(it, pr, mb + 16 * s, nb, v, a, !symmetric(MODE) || mb != nb, turn[wave_id()]);
 }
 
 // The small products, bound by latency: TS x TS blocks of 32 x 32 of D per
@@ -600,10 +622,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     constexpr int TILE = 32 * TS, GROUPS = TS * TS * 4, UNITS = TS * TS * 2;
     __shared__ float4 sum[kSmallWaves][GROUPS][kWave];
     __shared__ uint32_t turn[UNITS][kTurn];
-    int i = 0;
-    const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x);
-    while (i + 1 < b.n && w >= pr.tile0[i + 1])
-        ++i;
+    const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x), i = item_of(pr.tile0, w);
     const OrthItem &it = b.item[i];
     int tm, tn, K;
     tile_of<symmetric(MODE), TILE>(it, w - pr.tile0[i], tm, tn);
@@ -614,6 +633,16 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     const uint32_t loff = lane * 16;
     P += tm * TS * pitch;
     Q += tn * TS * pitch;
+
+    // at the end a wave stores 16 rows of a block
+    static_assert(UNITS <= kSmallWaves, "a wave for each half of a block");
+    const int blk = wave / 2, s = wave % 2;
+    const int mb = tm * TILE + blk / TS * 32, nb = tn * TILE + blk % TS * 32;
+    const bool stores = wave < UNITS && stored<MODE>(it, mb, nb);
+    Eights a;
+    if constexpr (MODE == kPoly)
+        if (stores)
+            a.load(it, mb + 16 * s, nb);
 
     floatx16 acc[TS][TS];
 #pragma unroll
@@ -679,11 +708,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
                         make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
                                     acc[x][y][4 * g + 3]);
     __syncthreads();
-    // a wave stores 16 rows of a block
-    static_assert(UNITS <= kSmallWaves, "a wave for each half of a block");
-    const int blk = wave / 2, s = wave % 2;
-    const int mb = tm * TILE + blk / TS * 32, nb = tn * TILE + blk % TS * 32;
-    if (wave >= UNITS || !stored<MODE>(it, mb, nb))
+    if (!stores)
         return;
     float v[8] = {};
     for (int p = 0; p < waves; ++p) {
@@ -691,7 +716,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         v[0] += f[0].x, v[1] += f[0].y, v[2] += f[0].z, v[3] += f[0].w;
         v[4] += f[32].x, v[5] += f[32].y, v[6] += f[32].z, v[7] += f[32].w;
     }
-    put<MODE, T>(it, pr, mb + 16 * s, nb, v, !symmetric(MODE) || mb != nb, turn[wave]);
+    put<MODE, T>(it, pr, mb + 16 * s, nb, v, a, !symmetric(MODE) || mb != nb, turn[wave]);
 }
 
 // Small matrices as a whole: X, its transpose and A (then B in its place) stay
@@ -963,6 +988,8 @@ OrthPlan plan_products(const OrthBatch &b)
         p.tile = tile;
         for (int i = 0; i < b.n; ++i)
             p.pr.tile0[i + 1] = p.pr.tile0[i] + tiles_of(b.item[i], SYM, tile);
+        for (int i = b.n + 1; i <= kOrthItems; ++i)
+            p.pr.tile0[i] = INT32_MAX;
         p.blocks = p.pr.whole = p.pr.tile0[b.n];
         return p;
     };
@@ -1014,6 +1041,8 @@ OrthPlan plan_products(const OrthBatch &b)
                     p.pr.work0[i] = p.pr.whole + n;
                     n += std::max(0, left) * p.pr.parts[i];
                 }
+                for (int i = b.n; i < kOrthItems; ++i)
+                    p.pr.work0[i] = INT32_MAX;
                 p.blocks = p.pr.whole + n;
                 double t = base + 4 + part * n;
                 if (p.pr.whole % (per_cu * kSlots) == 0) {

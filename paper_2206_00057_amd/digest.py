@@ -127,7 +127,8 @@ def _np(a, dtype):
 def _stream(stream):
     if stream is None:
         import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        # (the handle alone: building a torch.cuda.Stream takes longer than a launch)
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -506,57 +507,82 @@ def digest_profile_model(p, model=MODEL_GCN):
 
 # Operators that belong to no partition: layer norm, orthogonalised updates.
 
-def _here(t, name):
-    """t is a tensor on the current device (where the kernels run)."""
+_TYPES = {}
+
+
+def _elem_types():
+    """torch dtype -> DIGEST_F32, ..."""
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16})
+    return _TYPES
+
+
+def _device():
+    """The current device, where the kernels run."""
     import torch
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    return torch.cuda.current_device()
+
+
+def _here(t, dev, name):
+    if getattr(t, "is_cuda", False) is not True:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is "
-                         f"cuda:{torch.cuda.current_device()}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{dev}")
 
 
-def _elem_type(t, name):
-    import torch
-    types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-    if t.dtype not in types:
-        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
-    return types[t.dtype]
-
-
-def _rows(t, like, name):
-    """(pointer, row stride) of a 2-D tensor of the shape and type of ``like``
-    whose rows are contiguous."""
-    _here(t, name)
-    if t.dim() != 2 or t.shape != like.shape:
-        raise ValueError(f"{name} must be {list(like.shape)}, got {list(t.shape)}")
-    if t.dtype != like.dtype:
-        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    n, d = t.shape
-    if d > 1 and t.stride(1) != 1:
+def _rows(t, shape, dtype, dev, name):
+    """(pointer, row stride) of a 2-D tensor of this shape and type whose rows
+    are contiguous."""
+    _here(t, dev, name)
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    n, d = shape
+    if t.is_contiguous():
+        return t.data_ptr(), d
+    ld, step = t.stride()
+    if d > 1 and step != 1:
         raise ValueError(f"{name}: the elements of a row must be contiguous")
-    ld = t.stride(0) if n > 1 else d
+    if n <= 1:
+        ld = d
     if ld < d:
         raise ValueError(f"{name}: rows must not overlap")
-    return ctypes.c_void_p(t.data_ptr()), ld
+    return t.data_ptr(), ld
 
 
-def _vector(t, numel, name):
-    import torch
+def _matrix(t, dev, name):
+    """The (shape, dtype) of a 2-D tensor of one of the element types."""
+    _here(t, dev, name)
+    if t.dim() != 2:
+        raise ValueError(f"{name} must be 2-D")
+    if t.dtype not in _elem_types():
+        raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    return t.shape, t.dtype
+
+
+def _floats(t, numel, dev, name):
+    """Pointer of a contiguous float32 tensor of numel elements, None for None."""
     if t is None:
         return None
-    _here(t, name)
-    return _dev(t, torch.float32, numel, name)
+    _here(t, dev, name)
+    if _elem_types().get(t.dtype) != F32:
+        raise TypeError(f"{name} must be torch.float32, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.numel() != numel:
+        raise ValueError(f"{name} has {t.numel()} elements, expected {numel}")
+    return t.data_ptr()
 
 
-def _workspace(t):
-    import torch
+def _workspace(t, dev):
     if t is None:
         return None, 0
-    _here(t, "workspace")
+    _here(t, dev, "workspace")
     if not t.is_contiguous():
         raise ValueError("workspace must be contiguous")
-    return ctypes.c_void_p(t.data_ptr()), t.numel() * t.element_size()
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def digest_layer_norm_query(n_rows, width):
@@ -570,15 +596,15 @@ def digest_layer_norm_forward(x, gain, shift, y, stats=None, eps=1e-5, act=ACT_I
                               stream=None):
     """y = act(layer norm of each row of x [n, d]); gain, shift float32 [d] or
     None; stats float32 [n, 2] keeps (mean, rstd) for the backward."""
-    _here(x, "x")
-    if x.dim() != 2:
-        raise ValueError("x must be [n, d]")
-    n, d = x.shape
-    px, ldx = _rows(x, x, "x")
-    py, ldy = _rows(y, x, "y")
+    dev = _device()
+    shape, dtype = _matrix(x, dev, "x")
+    n, d = shape
+    px, ldx = _rows(x, shape, dtype, dev, "x")
+    py, ldy = _rows(y, shape, dtype, dev, "y")
     _check(_train_lib().digest_layer_norm_forward(
-        n, d, _elem_type(x, "x"), px, ldx, _vector(gain, d, "gain"), _vector(shift, d, "shift"),
-        float(eps), int(act), py, ldy, _vector(stats, 2 * n, "stats"), _stream(stream)))
+        n, d, _TYPES[dtype], px, ldx, _floats(gain, d, dev, "gain"),
+        _floats(shift, d, dev, "shift"), eps, act, py, ldy, _floats(stats, 2 * n, dev, "stats"),
+        _stream(stream)))
 
 
 def digest_layer_norm_backward(x, gain, y, dy, stats, dx, dgain, dshift, workspace,
@@ -586,21 +612,20 @@ def digest_layer_norm_backward(x, gain, y, dy, stats, dx, dgain, dshift, workspa
     """dx, dgain, dshift of digest_layer_norm_forward (each may be None); y, its
     output, is read with ACT_RELU only; workspace: a CUDA tensor of at least
     digest_layer_norm_query(n, d) bytes (None without dgain and dshift)."""
-    _here(x, "x")
-    if x.dim() != 2:
-        raise ValueError("x must be [n, d]")
-    n, d = x.shape
-    px, ldx = _rows(x, x, "x")
-    py, ldy = _rows(y, x, "y") if act == ACT_RELU else (None, 0)
-    pdy, lddy = _rows(dy, x, "dy")
-    pdx, lddx = _rows(dx, x, "dx") if dx is not None else (None, 0)
-    ws, nbytes = _workspace(workspace)
+    dev = _device()
+    shape, dtype = _matrix(x, dev, "x")
+    n, d = shape
+    px, ldx = _rows(x, shape, dtype, dev, "x")
+    py, ldy = _rows(y, shape, dtype, dev, "y") if act == ACT_RELU else (None, 0)
+    pdy, lddy = _rows(dy, shape, dtype, dev, "dy")
+    pdx, lddx = _rows(dx, shape, dtype, dev, "dx") if dx is not None else (None, 0)
+    ws, nbytes = _workspace(workspace, dev)
     if stats is None:
         raise ValueError("stats is required")
     _check(_train_lib().digest_layer_norm_backward(
-        n, d, _elem_type(x, "x"), px, ldx, _vector(gain, d, "gain"), int(act), py, ldy, pdy, lddy,
-        _vector(stats, 2 * n, "stats"), pdx, lddx, _vector(dgain, d, "dgain"),
-        _vector(dshift, d, "dshift"), ws, nbytes, _stream(stream)))
+        n, d, _TYPES[dtype], px, ldx, _floats(gain, d, dev, "gain"), act, py, ldy, pdy, lddy,
+        _floats(stats, 2 * n, dev, "stats"), pdx, lddx, _floats(dgain, d, dev, "dgain"),
+        _floats(dshift, d, dev, "dshift"), ws, nbytes, _stream(stream)))
 
 
 MUON_COEFFS = (3.4445, -4.7750, 2.0315)   # the default odd polynomial of each step
@@ -642,23 +667,23 @@ def digest_orthogonalize(mats, outs, workspace, steps=5, coeffs=None, stream=Non
     n = len(mats)
     if n < 1 or len(outs) != n:
         raise ValueError("need as many outputs as matrices, and one at least")
-    _here(mats[0], "mats[0]")
-    kind = _elem_type(mats[0], "mats[0]")
+    dev = _device()
+    dtype = _matrix(mats[0], dev, "mats[0]")[1]
     ins, outp = [], []
     for i, (m, o) in enumerate(zip(mats, outs)):
-        _here(m, f"mats[{i}]")
-        if m.dim() != 2 or 0 in m.shape:
-            raise ValueError(f"mats[{i}] must be a matrix with rows and columns")
-        if m.dtype != mats[0].dtype:
-            raise TypeError(f"mats[{i}] must be {mats[0].dtype}, got {m.dtype}")
-        ins.append(_rows(m, m, f"mats[{i}]"))
-        outp.append(_rows(o, m, f"outs[{i}]"))
+        shape, t = _matrix(m, dev, f"mats[{i}]")
+        if 0 in shape:
+            raise ValueError(f"mats[{i}] has no elements")
+        if t != dtype:
+            raise TypeError(f"mats[{i}] must be {dtype}, got {t}")
+        ins.append(_rows(m, shape, dtype, dev, f"mats[{i}]"))
+        outp.append(_rows(o, shape, dtype, dev, f"outs[{i}]"))
     rows, cols = _sides([m.shape for m in mats])
     ptrs, lds = ctypes.c_void_p * n, ctypes.c_int64 * n
-    ws, nbytes = _workspace(workspace)
+    ws, nbytes = _workspace(workspace, dev)
     _check(_train_lib().digest_orthogonalize(
-        n, rows, cols, kind, ptrs(*[p.value for p, _ in ins]), lds(*[l for _, l in ins]),
-        ptrs(*[p.value for p, _ in outp]), lds(*[l for _, l in outp]), int(steps),
+        n, rows, cols, _TYPES[dtype], ptrs(*[p for p, _ in ins]), lds(*[l for _, l in ins]),
+        ptrs(*[p for p, _ in outp]), lds(*[l for _, l in outp]), int(steps),
         _coeffs(coeffs, steps), ws, nbytes, _stream(stream)))
 
 
@@ -667,7 +692,6 @@ def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0,
     """The Muon update of the weight matrices ws (with their momenta, float32,
     in place) by the mean of each one's gradients: grads[i] lists the M
     gradients of ws[i]."""
-    import torch
     n = len(ws)
     if n < 1 or len(momenta) != n or len(grads) != n:
         raise ValueError("need a momentum and a list of gradients for each matrix, and one at "
@@ -677,20 +701,20 @@ def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0,
         raise ValueError("need the same number of gradients for each matrix, and one at least")
     if scales is not None and len(scales) != n:
         raise ValueError("need one scale for each matrix")
+    dev = _device()
     flat = {"ws": [], "momenta": [], "grads": []}
-    for i, w in enumerate(ws):
-        _here(w, f"ws[{i}]")
-        if w.dim() != 2 or 0 in w.shape:
+    shapes = [w.shape for w in ws]
+    for i, shape in enumerate(shapes):
+        if len(shape) != 2 or 0 in shape:
             raise ValueError(f"ws[{i}] must be a matrix with rows and columns")
-        for name, ts in (("ws", [w]), ("momenta", [momenta[i]]), ("grads", grads[i])):
+        for name, ts in (("ws", [ws[i]]), ("momenta", [momenta[i]]), ("grads", grads[i])):
             for t in ts:
-                _here(t, f"{name}[{i}]")
-                if t.shape != w.shape:
-                    raise ValueError(f"{name}[{i}] must be {list(w.shape)}, got {list(t.shape)}")
-                flat[name].append(_dev(t, torch.float32, w.numel(), f"{name}[{i}]").value)
-    rows, cols = _sides([w.shape for w in ws])
+                if t.shape != shape:
+                    raise ValueError(f"{name}[{i}] must be {list(shape)}, got {list(t.shape)}")
+                flat[name].append(_floats(t, t.numel(), dev, f"{name}[{i}]"))
+    rows, cols = _sides(shapes)
     arr = lambda v: (ctypes.c_void_p * len(v))(*v)
-    work, nbytes = _workspace(workspace)
+    work, nbytes = _workspace(workspace, dev)
     _check(_train_lib().digest_muon_average(
         n, rows, cols, arr(flat["ws"]), arr(flat["momenta"]), arr(flat["grads"]), M, float(lr),
         float(beta), float(decay),
