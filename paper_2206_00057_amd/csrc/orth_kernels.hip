@@ -300,7 +300,7 @@ __device__ __forceinline__ void operands(const OrthItem &it, const OrthParams &p
 // Tile t of an item, TILE x TILE.  Symmetric products: the tiles on and above
 // the diagonal, by column.
 template <bool SYM, int TILE>
-__device__ __forceinline__ void tile_of(const OrthItem &it, int t, int &tm, int &tn)
+__device__ __forceinline__ void tile_of(int rp, int t, int &tm, int &tn)
 {
     if constexpr (SYM) {
         tn = (int)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
@@ -310,7 +310,7 @@ __device__ __forceinline__ void tile_of(const OrthItem &it, int t, int &tm, int 
             ++tn;
         tm = t - tn * (tn + 1) / 2;
     } else {
-        const int gm = (it.rp + TILE - 1) / TILE;
+        const int gm = (rp + TILE - 1) / TILE;
         tm = t % gm;
         tn = t / gm;
     }
@@ -423,11 +423,11 @@ __device__ __forceinline__ void rows_of(const floatx16 &x, int s, float (&v)[8])
 // A symmetric product's 32 x 32 block at (mb, nb): blocks below the diagonal
 // are the mirror of those above.
 template <int MODE>
-__device__ __forceinline__ bool stored(const OrthItem &it, int mb, int nb)
+__device__ __forceinline__ bool stored(int rp, int cp, int mb, int nb)
 {
     if (symmetric(MODE))
-        return mb <= nb && nb < it.rk;
-    return mb < it.rp && nb < it.cp;
+        return mb <= nb && nb < rp;
+    return mb < rp && nb < cp;
 }
 
 // The large products: a TILE x TILE tile of D per workgroup, 128 (4 waves of
@@ -459,7 +459,7 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
     }
     const OrthItem &it = b.item[i];
     int tm, tn, K;
-    tile_of<symmetric(MODE), TILE>(it, t, tm, tn);
+    tile_of<symmetric(MODE), TILE>(it.rp, t, tm, tn);
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
     const int lane = threadIdx.x % kWave, wave = wave_id();
@@ -538,7 +538,7 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
 #pragma unroll
         for (int y = 0; y < TN; ++y) {
             const int mb = tm * BM + (wm + x) * 32, nb = tn * BN + (wn + y) * 32;
-            if (!stored<MODE>(it, mb, nb))
+            if (!stored<MODE>(it.rp, it.cp, mb, nb))
                 continue;
             if (part < 0) {
 #pragma unroll
@@ -577,11 +577,11 @@ __global__ __launch_bounds__(kThreads) void k_orth_join(OrthBatch b, OrthParams 
     const OrthItem &it = b.item[i];
     const int first = max(pr.whole, pr.tile0[i]);   // the item's first split tile
     int tm, tn;
-    tile_of<symmetric(MODE), TILE>(it, tile - pr.tile0[i], tm, tn);
+    tile_of<symmetric(MODE), TILE>(it.rp, tile - pr.tile0[i], tm, tn);
     const int blk = at % UNITS / 2, s = at % 2;
     const int wave = blk / (TM * TN), x = blk / TN % TM, y = blk % TN;
     const int mb = tm * BM + (wave / WN * TM + x) * 32, nb = tn * BN + (wave % WN * TN + y) * 32;
-    if (!stored<MODE>(it, mb, nb))
+    if (!stored<MODE>(it.rp, it.cp, mb, nb))
         return;
     // rows 8 (lane / 32) .. + 7 of half s: element group 2 s + lane / 32 of both lane halves
     const float *src = pr.partials +
@@ -622,12 +622,15 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     constexpr int TILE = 32 * TS, GROUPS = TS * TS * 4, UNITS = TS * TS * 2;
     __shared__ float4 sum[kSmallWaves][GROUPS][kWave];
     __shared__ uint32_t turn[UNITS][kTurn];
-    const int w = (int)xcd_contiguous(blockIdx.x, gridDim.x), i = item_of(pr.tile0, w);
+    const int w = blockIdx.x, i = item_of(pr.tile0, w);
     const OrthItem &it = b.item[i];
     int tm, tn, K;
-    tile_of<symmetric(MODE), TILE>(it, w - pr.tile0[i], tm, tn);
     const char *P, *Q;
     operands<MODE>(it, pr, K, P, Q);
+    int t = w - pr.tile0[i], rp = it.rp, cp = it.cp;
+    // (everything that the loads need is fetched here, at once)
+    asm volatile("" : "+s"(K), "+s"(P), "+s"(Q), "+s"(t), "+s"(rp), "+s"(cp));
+    tile_of<symmetric(MODE), TILE>(rp, t, tm, tn);
     const int lane = threadIdx.x % kWave, wave = wave_id();
     const int64_t pitch = (int64_t)K * 128;
     const uint32_t loff = lane * 16;
@@ -638,7 +641,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     static_assert(UNITS <= kSmallWaves, "a wave for each half of a block");
     const int blk = wave / 2, s = wave % 2;
     const int mb = tm * TILE + blk / TS * 32, nb = tn * TILE + blk % TS * 32;
-    const bool stores = wave < UNITS && stored<MODE>(it, mb, nb);
+    const bool stores = wave < UNITS && stored<MODE>(rp, cp, mb, nb);
     Eights a;
     if constexpr (MODE == kPoly)
         if (stores)
@@ -656,8 +659,10 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         half8 p[2][2][TS], q[2][2][TS];   // [16 k][part][block]
     };
     const int nk = K / kBlockK;
-    auto load = [&](int kb, Line &l) {   // (past the end: the last line, not multiplied)
-        const int64_t at = (int64_t)min(kb, nk - 1) * kLineBytes;
+    auto load = [&](int kb, Line &l) {
+        if (kb >= nk)   // uniform
+            return;
+        const int64_t at = (int64_t)kb * kLineBytes;
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -691,8 +696,7 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
             for (int u = 0; u < DEPTH; ++u) {
                 if (kb + u * kSmallWaves < nk)   // uniform
                     multiply(l[u]);
-                if (kb + DEPTH * kSmallWaves < nk)
-                    load(kb + (u + DEPTH) * kSmallWaves, l[u]);
+                load(kb + (u + DEPTH) * kSmallWaves, l[u]);
             }
         }
     }
