@@ -16,6 +16,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "device.h"
 #include "train_kernels.h"
@@ -430,10 +431,10 @@ __device__ __forceinline__ bool stored(int rp, int cp, int mb, int nb)
     return mb < rp && nb < cp;
 }
 
-// The large products: a TILE x TILE tile of D per workgroup, 128 (4 waves of
-// 64 x 64, two workgroups a CU) or 256 (8 waves of 128 x 64, which read each
-// line of LDS fewer times).  One line (32 k) of both operands' rows at a time
-// in LDS, the next one on its way there.
+// The large products: a TILE x TILE tile of D per workgroup and CU, 128 (4
+// waves of 64 x 64) or 256 (8 waves of 128 x 64, which read each line of LDS
+// and of memory fewer times).  Lines (32 k) of both operands' rows come into a
+// ring of BUFS places in LDS.
 template <int TILE>
 struct Waves {
     static constexpr int WM = 2, WN = TILE / 64, TM = TILE / 64, TN = 2, W = WM * WN;
@@ -442,10 +443,16 @@ struct Waves {
 template <int MODE, class T, int TILE>
 __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b, OrthParams pr)
 {
+    constexpr int BUFS = TILE == 128 ? 4 : 2;   // 128 KB either way
     constexpr int WN = Waves<TILE>::WN, TM = Waves<TILE>::TM, TN = Waves<TILE>::TN;
     constexpr int W = Waves<TILE>::W, BM = TILE, BN = TILE, ROWS = (BM + BN) / 32;
-    // [32 rows][16 k][part][lane]: what a matrix instruction takes is 1 KB
+    // [32 rows][16 k][part][lane]: what a matrix instruction takes is 1 KB.  A
+    // ring of BUFS lines (arrays of their own: the compiler then knows which
+    // one a load fills).
     __shared__ half8 lds0[ROWS * kLineBytes / 16], lds1[ROWS * kLineBytes / 16];
+    static_assert(BUFS == 2 || BUFS == 4, "places for lines");
+    __shared__ half8 lds2[BUFS > 2 ? ROWS * kLineBytes / 16 : 1];
+    __shared__ half8 lds3[BUFS > 2 ? ROWS * kLineBytes / 16 : 1];
 
     int w = blockIdx.x, i, t, part = -1;
     if (w < pr.whole) {
@@ -479,54 +486,103 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
     const int64_t pitch = (int64_t)K * 128;   // bytes of 32 rows
     const int prow = it.rp / 32, qrow = (symmetric(MODE) ? it.rp : it.cp) / 32;
     const uint32_t loff = lane * 16;
+    constexpr int L = 4 * ROWS / W;   // its loads of a line
+    auto load_one = [&](int kb, half8 *dst, int q) {
+        const int at = q * W + wave, row = at / 4;
+        const char *src = row < BM / 32
+                              ? P + min(tm * (BM / 32) + row, prow - 1) * pitch
+                              : Q + min(tn * (BN / 32) + row - BM / 32, qrow - 1) * pitch;
+        src += (int64_t)kb * kLineBytes + at % 4 * 1024;
+        __builtin_amdgcn_global_load_lds((global_void *)(src + loff),
+                                         (lds_void *)(&dst[at * kWave]), 16, 0, 0);
+    };
     auto load = [&](int kb, half8 *dst) {
 #pragma unroll
-        for (int q = 0; q < 4 * ROWS; q += W) {
-            const int at = q + wave, row = at / 4;
-            const char *src = row < BM / 32 ? P + min(tm * (BM / 32) + row, prow - 1) * pitch
-                                            : Q + min(tn * (BN / 32) + row - BM / 32, qrow - 1) * pitch;
-            src += (int64_t)kb * kLineBytes + at % 4 * 1024;
-            __builtin_amdgcn_global_load_lds((global_void *)(src + loff), (lds_void *)(&dst[at * kWave]),
-                                             16, 0, 0);
-        }
-        __builtin_amdgcn_sched_barrier(0);
+        for (int q = 0; q < L; ++q)
+            load_one(kb, dst, q);
     };
-    auto multiply = [&](const half8 *src) {
+    struct Frags {   // the operands of 16 k
+        half8 p[2][TM], q[2][TN];
+    };
+    constexpr int F = 2 * (TM + TN);   // reads of a Frags
+    auto fetch_one = [&](const half8 *src, int s, Frags &f, int i) {
+        const int h = i % 2, x = i / 2;
+        if (x < TM)
+            f.p[h][x] = src[((wm + x) * 4 + 2 * s + h) * kWave + lane];
+        else
+            f.q[h][x - TM] = src[((BM / 32 + wn + x - TM) * 4 + 2 * s + h) * kWave + lane];
+    };
+    // f's products, `beside(i)` issued behind the i-th: reads and loads take
+    // their turn while the matrix instructions run
+    auto multiply = [&](const Frags &f, auto beside) {
 #pragma unroll
-        for (int s = 0; s < kBlockK / 16; ++s) {
-            half8 p[2][TM], q[2][TN];
+        for (int k = 0; k < 3; ++k)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int x = 0; x < TM; ++x)
 #pragma unroll
-                for (int x = 0; x < TM; ++x)
-                    p[h][x] = src[((wm + x) * 4 + 2 * s + h) * kWave + lane];
-#pragma unroll
-                for (int y = 0; y < TN; ++y)
-                    q[h][y] = src[((BM / 32 + wn + y) * 4 + 2 * s + h) * kWave + lane];
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-#pragma unroll
-                for (int x = 0; x < TM; ++x)
-#pragma unroll
-                    for (int y = 0; y < TN; ++y)
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                            p[k == 2][x], q[k == 1][y], acc[x][y], 0, 0, 0);
-        }
+                for (int y = 0; y < TN; ++y) {
+                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                        f.p[k == 2][x], f.q[k == 1][y], acc[x][y], 0, 0, 0);
+                    beside((k * TM + x) * TN + y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+    };
+    static_assert(F <= 3 * TM * TN && L <= 3 * TM * TN, "a place behind a product for each");
+    // Waits until all but the wave's newest `lines` lines are in LDS and its
+    // reads are done, then for the other waves.  (A barrier of the compiler's
+    // would wait for every load.)
+    static_assert((BUFS - 1) * L < 64, "vmcnt holds six bits");
+    auto sync = [&](auto lines) {
+        constexpr int n = decltype(lines)::value * L;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((n & 15) | 7 << 4 | (n >> 4) << 14);
+        asm volatile("s_barrier" ::: "memory");
     };
     const int k0 = part < 0 ? 0 : part * pr.chunk;
     const int k1 = part < 0 ? K / kBlockK : min(K / kBlockK, k0 + pr.chunk);
+    // One line: its first half is in f0 already.  The second half is read while
+    // the first is multiplied, the next line's first half while the second is;
+    // between them the line's place in LDS is free for the line BUFS further.
+    // (Past the last line it is loaded again, so that the waits count alike.)
+    Frags f0, f1;
+    auto step = [&](int kb, half8 *now, const half8 *next) {
+        __builtin_amdgcn_s_waitcnt(15 | 7 << 4 | 3 << 14);   // f0, before f1 is asked for
+        multiply(f0, [&](int i) {
+            if (i < F)
+                fetch_one(now, 1, f1, i);
+        });
+        sync(std::integral_constant<int, BUFS - 2>());
+        const int further = min(kb + BUFS, k1 - 1);
+        multiply(f1, [&](int i) {
+            if (i < F)
+                fetch_one(next, 0, f0, i);
+            if (i < L)
+                load_one(further, now, i);
+        });
+    };
     load(k0, lds0);
-    __syncthreads();
-    for (int kb = k0; kb < k1; kb += 2) {   // (an even number of lines)
-        load(kb + 1, lds1);
-        multiply(lds0);
-        __syncthreads();
-        if (kb + 2 < k1)
-            load(kb + 2, lds0);
-        multiply(lds1);
-        __syncthreads();
+    load(min(k0 + 1, k1 - 1), lds1);
+    if constexpr (BUFS == 4) {
+        load(min(k0 + 2, k1 - 1), lds2);
+        load(min(k0 + 3, k1 - 1), lds3);
     }
+    sync(std::integral_constant<int, BUFS - 1>());
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+        fetch_one(lds0, 0, f0, i);
+    int kb = k0;
+    if constexpr (BUFS == 4)
+        for (; kb + 4 <= k1; kb += 4) {
+            step(kb, lds0, lds1);
+            step(kb + 1, lds1, lds2);
+            step(kb + 2, lds2, lds3);
+            step(kb + 3, lds3, lds0);
+        }
+    for (; kb < k1; kb += 2) {   // (an even number of lines)
+        step(kb, lds0, lds1);
+        step(kb + 1, lds1, BUFS == 4 ? lds2 : lds0);
+    }
+    __syncthreads();
 
     // (what the stores need is formed here, not kept through the loop)
     int lane_out = lane;
@@ -968,14 +1024,17 @@ constexpr int kSlots = 256;    // CUs
 constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each)
 
 // The fastest of the kernels by their times in us, as measured (MI355X, fp32
-// 256 x 256 to 4,096 x 4,096; lines are 32 k):
-//   32    5.5 + 0.6 a line of a wave, 3 + 5.3e-3 for each line of each tile's
-//         waves once the card is full
-//   64    1 + (4.5 + 1.65 a line of a wave) for each 256 tiles
-//   128   5.5 + 0.78 a line with one workgroup a CU, 1.54 with two
-//   256   8 + 2.7 a line (3.1 for the four tiles of 128 with two a CU)
-// A tile's k may be split where tiles are few or left over by the whole ones:
-// the join takes 4 and 0.013 (128) or 0.052 (256) for each part that it reads.
+// 64 x 512 to 4,096 x 4,096; w is the lines, 32 k each, of one of the eight
+// waves that share a small tile's k, n the workgroups of a round of 256):
+//   32    3.9 + 0.7 w, or 2 + 3.2e-3 a tile + 4.2e-3 w a tile where that is more
+//   64    1 + (4.5 + 1.65 w) for each 256 tiles
+//   128   5.5 + (0.58 + 0.2 n / 256) a line of each round
+//   256   8 + (2.0 + 0.6 n / 256) a line of each round
+// A tile's k may be split where tiles are few or left over by whole rounds:
+// the join takes 3.5 + 0.015 (128) or 4 + 0.045 (256) a part.  (1,024 x 4,096:
+// X X^T 35 us with 64, 20 and 6 with 128 in seven parts each; B X 48 and 30;
+// 256 x 256: 4.6 us with 32, 6.3 with 64, 12 with 128; 4,096 x 4,096: B X 412
+// with 128, 344 with 256.)
 template <int MODE>
 OrthPlan plan_products(const OrthBatch &b)
 {
@@ -1003,63 +1062,52 @@ OrthPlan plan_products(const OrthBatch &b)
             best = p;
         }
     };
-    const double waves = (most + kSmallWaves - 1) / kSmallWaves;
+    auto shared = [](int n) { return (n + kSmallWaves - 1) / kSmallWaves; };
     {
         const OrthPlan p = start(32);
         double all = 0;
         for (int i = 0; i < b.n; ++i)
-            all += (double)(p.pr.tile0[i + 1] - p.pr.tile0[i]) *
-                   ((lines[i] + kSmallWaves - 1) / kSmallWaves);
-        consider(p, std::max(5.5 + 0.6 * waves, 3 + 5.3e-3 * all));
+            all += (p.pr.tile0[i + 1] - p.pr.tile0[i]) * (3.2e-3 + 4.2e-3 * shared(lines[i]));
+        consider(p, std::max(3.9 + 0.7 * shared(most), 2 + all));
     }
     {
         const OrthPlan p = start(64);
-        consider(p, 1 + (p.blocks + kSlots - 1) / kSlots * (4.5 + 1.65 * waves));
+        consider(p, 1 + (p.blocks + kSlots - 1) / kSlots * (4.5 + 1.65 * shared(most)));
     }
     for (int tile = 128; tile <= 256; tile *= 2) {
         const OrthPlan all = start(tile);
-        const int per_cu = tile == 128 ? 2 : 1;
-        const double full = tile == 128 ? 1.54 : 2.7, alone = tile == 128 ? 0.78 : 2.7;
-        const double base = tile == 128 ? 5.5 : 8, part = tile == 128 ? 0.013 : 0.052;
         const int32_t tiles = all.blocks;
-        // workgroups of `c` lines on their own
-        auto run = [&](double n, double c) {
-            const double rounds = std::floor(n / (per_cu * kSlots)), left = n - rounds * per_cu * kSlots;
-            return c * (rounds * full + (left > kSlots ? full : left > 0 ? alone : 0));
+        const bool wide = tile == 256;
+        // n workgroups of c lines each
+        auto run = [&](int32_t n, int32_t c) {
+            const double left = n % kSlots / (double)kSlots;
+            return c * (wide ? n / kSlots * 2.6 + (left > 0 ? 2.0 + 0.6 * left : 0)
+                             : n / kSlots * 0.78 + (left > 0 ? 0.58 + 0.2 * left : 0));
         };
+        const double base = wide ? 8 : 5.5;
         consider(all, base + run(tiles, most));
-        for (int w = 0; w <= per_cu; ++w) {   // whole tiles: none, or all but what is left over
+        if (tiles % kSlots == 0)
+            continue;
+        // the tiles that whole rounds leave over, in `split` parts each
+        for (int split = 2; split <= 16; split += split < 4 ? 1 : split / 4 * 2) {
             OrthPlan p = all;
-            p.pr.whole = w ? tiles - tiles % (w * kSlots) : 0;
-            if (p.pr.whole == tiles || (w && p.pr.whole == 0))
-                continue;
-            for (int split = 2; split <= 16; split += split < 4 ? 1 : split / 4 * 2) {
-                p.pr.chunk = ((most + split - 1) / split + 1) / 2 * 2;
-                if (p.pr.chunk < kMinChunk)
-                    break;
-                p.joins = tiles - p.pr.whole;
-                int32_t n = 0;
-                for (int i = 0; i < b.n; ++i) {
-                    const int32_t left = p.pr.tile0[i + 1] - std::max(p.pr.whole, p.pr.tile0[i]);
-                    p.pr.parts[i] = (lines[i] + p.pr.chunk - 1) / p.pr.chunk;
-                    p.pr.work0[i] = p.pr.whole + n;
-                    n += std::max(0, left) * p.pr.parts[i];
-                }
-                for (int i = b.n; i < kOrthItems; ++i)
-                    p.pr.work0[i] = INT32_MAX;
-                p.blocks = p.pr.whole + n;
-                double t = base + 4 + part * n;
-                if (p.pr.whole % (per_cu * kSlots) == 0) {
-                    t += run(p.pr.whole, most) + run(n, p.pr.chunk);
-                } else {
-                    // one whole tile on each CU, parts beside it in turn
-                    const double beside = (n + kSlots - 1) / kSlots * (double)p.pr.chunk;
-                    t += run(p.pr.whole - kSlots, most) + std::min<double>(beside, most) * full +
-                         std::max<double>(0, most - beside) * alone +
-                         std::max<double>(0, beside - most) * full / 2;
-                }
-                consider(p, t);
+            p.pr.whole = tiles - tiles % kSlots;
+            p.pr.chunk = ((most + split - 1) / split + 1) / 2 * 2;
+            if (p.pr.chunk < kMinChunk)
+                break;
+            p.joins = tiles - p.pr.whole;
+            int32_t n = 0;
+            for (int i = 0; i < b.n; ++i) {
+                const int32_t left = p.pr.tile0[i + 1] - std::max(p.pr.whole, p.pr.tile0[i]);
+                p.pr.parts[i] = (lines[i] + p.pr.chunk - 1) / p.pr.chunk;
+                p.pr.work0[i] = p.pr.whole + n;
+                n += std::max(0, left) * p.pr.parts[i];
             }
+            for (int i = b.n; i < kOrthItems; ++i)
+                p.pr.work0[i] = INT32_MAX;
+            p.blocks = p.pr.whole + n;
+            consider(p, base + run(p.pr.whole, most) + run(n, p.pr.chunk) +
+                            (wide ? 4 + 0.045 * n : 3.5 + 0.015 * n));
         }
     }
     return best;
