@@ -404,9 +404,21 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
     const int64_t c = (int64_t)blockIdx.x * kWave + lane;
     const int64_t width = 2 * (int64_t)d;
     float v = 0.f;
-    if (c < width)
-        for (int b = w; b < blocks; b += kSumWaves)
+    if (c < width) {
+        constexpr int U = 16;   // in flight, added in order
+        int b = w;
+        for (; b + (U - 1) * kSumWaves < blocks; b += U * kSumWaves) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                x[u] = part[(b + u * kSumWaves) * width + c];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                v += x[u];
+        }
+        for (; b < blocks; b += kSumWaves)
             v += part[b * width + c];
+    }
     sum[w][lane] = v;
     lds_barrier();
     if (w == 0 && c < width) {

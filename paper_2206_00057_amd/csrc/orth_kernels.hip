@@ -219,9 +219,18 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
         x[q] = i < it.rows && j < it.cols ? (float)u[(int64_t)i * it.ldu + j] : 0.f;
     }
     double sum = 0;
-    for (int i = threadIdx.x; i < it.sums; i += kThreads)
-        sum += it.part[i];
-    const double norm = sqrt(block_sum(sum));
+    if (it.sums <= kWave) {   // (uniform; every wave adds them itself)
+        if ((int)threadIdx.x % kWave < it.sums)
+            sum = it.part[threadIdx.x % kWave];
+#pragma unroll
+        for (int off = kWave / 2; off > 0; off >>= 1)
+            sum += __shfl_xor(sum, off);
+    } else {
+        for (int i = threadIdx.x; i < it.sums; i += kThreads)
+            sum += it.part[i];
+        sum = block_sum(sum);
+    }
+    const double norm = sqrt(sum);
     const double f = norm == 0 ? 0.0 : scale / norm;
 #pragma unroll
     for (int q = 0; q < N; ++q)
@@ -322,6 +331,37 @@ int32_t tiles_of(const OrthItem &it, bool sym, int tile)
     return sym ? gm * (gm + 1) / 2 : gm * ((it.cp + tile - 1) / tile);
 }
 
+// Rows m .. m + N - 1 of column n of the result, into the caller's matrix or
+// (UPDATE) into the weights: out <- keep out - scale v, all of them read
+// before the first is written.
+template <bool UPDATE, int N, class T>
+__device__ __forceinline__ void put_result(const OrthItem &it, float keep, int m, int n,
+                                           const float (&v)[N], T *out)
+{
+    const int count = n < it.c ? max(0, min(N, it.r - m)) : 0;
+    if (it.rows > it.cols) {   // (tall: side by side)
+        T *o = out + (int64_t)n * it.ldo + m;
+        typename Vec<T, N>::type x;
+        if constexpr (UPDATE)
+            x = load_some<T, N>(o, count);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            x[e] = (T)(UPDATE ? keep * (float)x[e] - it.scale * v[e] : v[e]);
+        store_some<T, N>(o, count, x);
+    } else {
+        T *o = out + (int64_t)m * it.ldo + n, x[N];
+        if constexpr (UPDATE)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (e < count)
+                    x[e] = o[e * it.ldo];
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < count)
+                o[e * it.ldo] = (T)(UPDATE ? keep * (float)x[e] - it.scale * v[e] : v[e]);
+    }
+}
+
 // Stores 32 columns n from nb on and 16 rows m from mb on of the product,
 // given by rows: lane (n = lane % 32, lane / 32) holds m = 8 (lane / 32) ..
 // + 7.  `mirror`: the transposed is nobody else's to store.  `turn` is the
@@ -391,17 +431,7 @@ __device__ __forceinline__ void put(const OrthItem &it, const OrthParams &pr, in
         *reinterpret_cast<half8 *>(d) = h.v;
         *reinterpret_cast<half8 *>(d + kPart) = l.v;
     } else {
-        const bool tall = it.rows > it.cols;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (m + e < it.r && n < it.c) {
-                T *o = (T *)it.out + (tall ? (int64_t)n * it.ldo + m + e
-                                           : (int64_t)(m + e) * it.ldo + n);
-                if constexpr (MODE == kUpdate)
-                    *o = (T)(pr.keep * (float)*o - it.scale * v[e]);
-                else
-                    *o = (T)v[e];
-            }
+        put_result<MODE == kUpdate, 8>(it, pr.keep, m, n, v, (T *)it.out);
     }
 }
 
@@ -779,6 +809,113 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
     put<MODE, T>(it, pr, mb + 16 * s, nb, v, a, !symmetric(MODE) || mb != nb, turn[wave]);
 }
 
+// X' = (a I + b A + c A A) X for up to 128 rows, 32 x 32 of X' per workgroup,
+// in one launch instead of two: wave j forms B's 32 x 32 block of the tile's
+// rows and k in [32 j, 32 j + 32) itself, whose layout as a result is the
+// matrix instruction's layout as an operand, and multiplies it by its 32 k of
+// X.  The waves' sums meet in LDS.  B is formed again for every 32 columns of
+// X: 100 x 256 6.0 us a step where B and B X take 4.2 and 4.4, but 256 x 256
+// (eight waves) 9.5 where they take 4.6 each, so it stops at 128.
+constexpr int kFuseWaves = 4;
+constexpr int kFuseRows = 32 * kFuseWaves;
+
+template <int MODE, class T>
+__global__ __launch_bounds__(kFuseWaves *kWave) void k_orth_poly_apply(OrthBatch b, OrthParams poly,
+                                                                        OrthParams pr)
+{
+    __shared__ float4 sum[kFuseWaves][4][kWave];
+    __shared__ uint32_t turn[2][kTurn];
+    const int w = blockIdx.x, i = item_of(pr.tile0, w);
+    const OrthItem &it = b.item[i];
+    int K = it.rk, t = w - pr.tile0[i], rp = it.rp;
+    const char *A = (const char *)it.A, *Q = (const char *)it.Xt[pr.from];
+    // (everything that the loads need is fetched here, at once)
+    asm volatile("" : "+s"(K), "+s"(A), "+s"(Q), "+s"(t), "+s"(rp));
+    int tm, tn;
+    tile_of<false, 32>(rp, t, tm, tn);
+    const int lane = threadIdx.x % kWave, wave = wave_id(), nk = K / kBlockK;
+    const int64_t pitch = (int64_t)K * 128;
+    const uint32_t loff = lane * 16;
+    if (wave < nk) {
+        half8 x[2][2];   // X's line of the wave's k: [16 k][part]
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                x[s][h] = *reinterpret_cast<const half8 *>(Q + tn * pitch + wave * kLineBytes +
+                                                           (2 * s + h) * 1024 + loff);
+        Eights a[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            a[s].load(it, 32 * wave + 16 * s, 32 * tm);
+        const char *p = A + wave * pitch + loff, *q = A + tm * pitch + loff;
+        floatx16 acc, low;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            acc[e] = low[e] = 0.f;
+        half8 f[kFuseWaves][2][2], g[kFuseWaves][2][2];
+#pragma unroll
+        for (int k = 0; k < kFuseWaves; ++k)
+            if (k < nk)   // uniform
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int64_t o = (int64_t)k * kLineBytes + (2 * s + h) * 1024;
+                        f[k][s][h] = *reinterpret_cast<const half8 *>(p + o);
+                        g[k][s][h] = *reinterpret_cast<const half8 *>(q + o);
+                    }
+#pragma unroll
+        for (int k = 0; k < kFuseWaves; ++k)
+            if (k < nk)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[k][s][0], g[k][s][0], acc, 0, 0, 0);
+                    low = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[k][s][0], g[k][s][1], low, 0, 0, 0);
+                    low = __builtin_amdgcn_mfma_f32_32x32x16_f16(f[k][s][1], g[k][s][0], low, 0, 0, 0);
+                }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            acc[e] += low[e];
+        floatx16 out;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            out[e] = 0.f;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            // row n = lane % 32 of the tile, k = m .. m + 7
+            float v[8];
+            rows_of(acc, s, v);
+            const int m = 32 * wave + 16 * s + lane / 32 * 8, n = 32 * tm + lane % 32;
+            half8 h, l;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                v[e] = fmaf((float)a[s].h[e] + (float)a[s].l[e], poly.lin, v[e] * poly.alpha) +
+                       (m + e == n ? poly.diag : 0.f);
+                h[e] = (_Float16)v[e];
+                l[e] = (_Float16)(v[e] - (float)h[e]);
+            }
+            out = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, x[s][0], out, 0, 0, 0);
+            out = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, x[s][1], out, 0, 0, 0);
+            out = __builtin_amdgcn_mfma_f32_32x32x16_f16(l, x[s][0], out, 0, 0, 0);
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            sum[wave][g][lane] = make_float4(out[4 * g], out[4 * g + 1], out[4 * g + 2], out[4 * g + 3]);
+    }
+    __syncthreads();
+    if (wave >= 2)
+        return;
+    // a wave stores 16 rows
+    float v[8] = {};
+    for (int p = 0; p < nk; ++p) {
+        const float4 *f = &sum[p][2 * wave + lane / 32][lane % 32];
+        v[0] += f[0].x, v[1] += f[0].y, v[2] += f[0].z, v[3] += f[0].w;
+        v[4] += f[32].x, v[5] += f[32].y, v[6] += f[32].z, v[7] += f[32].w;
+    }
+    put<MODE, T>(it, pr, 32 * tm + 16 * wave, 32 * tn, v, Eights{}, true, turn[wave]);
+}
+
 // Small matrices as a whole: X, its transpose and A (then B in its place) stay
 // in the LDS of one workgroup through all steps, so that a call is one launch
 // instead of three a step.
@@ -996,16 +1133,7 @@ __global__ __launch_bounds__(kWholeThreads) void k_orth_whole(OrthBatch b, Whole
                     }
                     continue;
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    if (m + e < it.r && c < it.c) {
-                        T *o = (T *)it.out + (tall ? (int64_t)c * it.ldo + m + e
-                                                   : (int64_t)(m + e) * it.ldo + c);
-                        if constexpr (UPDATE)
-                            *o = (T)(pr.keep * (float)*o - it.scale * v[e]);
-                        else
-                            *o = (T)v[e];
-                    }
+                put_result<UPDATE, 4>(it, pr.keep, m, c, v, (T *)it.out);
             }
         }
         __syncthreads();
@@ -1122,6 +1250,22 @@ void gemm(const OrthBatch &b, const OrthPlan &p, hipStream_t s)
             <<<p.joins * (TILE / 32) * (TILE / 32) * 2 / (kThreads / kWave), kThreads, 0, s>>>(b, p.pr);
 }
 
+// The product with X and the polynomial before it, together or one by one.
+template <int MODE, class T>
+hipError_t product(const OrthBatch &b, const OrthPlan &p, hipStream_t s);
+template <int MODE, class T>
+hipError_t poly_apply(const OrthBatch &b, const OrthPlan &poly, const OrthPlan &apply, bool fuse,
+                      hipStream_t s)
+{
+    if (fuse) {
+        k_orth_poly_apply<MODE, T><<<apply.blocks, kFuseWaves * kWave, 0, s>>>(b, poly.pr, apply.pr);
+        return hipGetLastError();
+    }
+    if (hipError_t e = product<kPoly, float>(b, poly, s))
+        return e;
+    return product<MODE, T>(b, apply, s);
+}
+
 template <int MODE, class T>
 hipError_t product(const OrthBatch &b, const OrthPlan &p, hipStream_t s)
 {
@@ -1228,6 +1372,9 @@ hipError_t launch_orth_steps(const OrthBatch &b, const OrthStep *steps, int32_t 
 {
     OrthPlan gram = plan_products<kGram>(b), poly = plan_products<kPoly>(b),
              apply = plan_products<kApply>(b);
+    bool fuse = apply.tile == 32;
+    for (int i = 0; i < b.n; ++i)
+        fuse = fuse && b.item[i].rk <= kFuseRows;
     gram.pr.partials = poly.pr.partials = apply.pr.partials = partials;
     apply.pr.keep = keep;
     for (int32_t k = 0; k < n; ++k) {
@@ -1241,19 +1388,17 @@ hipError_t launch_orth_steps(const OrthBatch &b, const OrthStep *steps, int32_t 
         apply.pr.from = st.from;
         if (hipError_t e = product<kGram, float>(b, gram, s))
             return e;
-        if (hipError_t e = product<kPoly, float>(b, poly, s))
-            return e;
         hipError_t e = hipErrorInvalidValue;
         if (!last)
-            e = product<kApply, float>(b, apply, s);
+            e = poly_apply<kApply, float>(b, poly, apply, fuse, s);
         else if (muon)
-            e = product<kUpdate, float>(b, apply, s);
+            e = poly_apply<kUpdate, float>(b, poly, apply, fuse, s);
         else if (type == kF32)
-            e = product<kResult, float>(b, apply, s);
+            e = poly_apply<kResult, float>(b, poly, apply, fuse, s);
         else if (type == kBF16)
-            e = product<kResult, __bf16>(b, apply, s);
+            e = poly_apply<kResult, __bf16>(b, poly, apply, fuse, s);
         else if (type == kF16)
-            e = product<kResult, _Float16>(b, apply, s);
+            e = poly_apply<kResult, _Float16>(b, poly, apply, fuse, s);
         if (e != hipSuccess)
             return e;
     }
