@@ -437,9 +437,6 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
 // a 16-wave workgroup).
 constexpr int kHeldWidth = 16384;
 constexpr int kFusedWidth = 8192;
-// Workgroups of the row kernels: several per CU, each a run of many rows.
-constexpr int kMaxBlocks = 1024;
-
 // Lanes of a row of d elements of V to a vector, and elements a lane.
 struct Shape {
     int gl, waves, e;
@@ -460,10 +457,17 @@ Shape shape_of(int d, int V)
 
 int rows_at_a_time(const Shape &s) { return s.waves == 1 ? kThreads / s.gl : 1; }
 
-int32_t blocks_of(int32_t n, const Shape &s)
+// Workgroups of the row kernels, each a run of rows: whole rounds of the CUs,
+// at most 2,048 forward and 1,024 backward, whose workgroups each leave a row of
+// partial sums (of rows of up to 1,024 elements; wider rows take more waves
+// each, and half or a quarter as many workgroups).  Measured with 1,024,
+// 2,048 and 8,192: forward 306,250 x 256 float32 127, 119 and 117 us,
+// 16,384 x 4,096 bfloat16 61, 45 and 44; backward 29,125 x 602 bfloat16 39, 48
+// and 95 us, 16,384 x 4,096 bfloat16 102, 133 and 186.
+int32_t blocks_of(int32_t n, const Shape &s, bool backward)
 {
     const int r = rows_at_a_time(s);
-    const int cap = s.waves == 16 ? kMaxBlocks / 4 : s.waves == 4 ? kMaxBlocks / 2 : kMaxBlocks;
+    const int cap = (backward ? 1024 : 2048) / (s.waves == 16 ? 4 : s.waves == 4 ? 2 : 1);
     return (int32_t)std::min<int64_t>(cap, ((int64_t)n + r - 1) / r);
 }
 
@@ -570,7 +574,7 @@ int32_t norm_partials(int32_t n, int32_t d)
 {
     // (the lanes of a row, and so the workgroups, go by the element type: the
     // larger of the two counts)
-    return std::max(blocks_of(n, shape_of(d, 4)), blocks_of(n, shape_of(d, 8)));
+    return std::max(blocks_of(n, shape_of(d, 4), true), blocks_of(n, shape_of(d, 8), true));
 }
 
 hipError_t launch_norm_forward(int32_t type, int32_t n, int32_t d, const void *x, int64_t ldx,
@@ -580,7 +584,7 @@ hipError_t launch_norm_forward(int32_t type, int32_t n, int32_t d, const void *x
     if (n <= 0)
         return hipSuccess;
     const Shape sh = shape_of(d, vec_of(type));
-    const int32_t blocks = blocks_of(n, sh);
+    const int32_t blocks = blocks_of(n, sh, false);
     switch (type) {
     case kF32:
         return with_shape<float>(
@@ -603,7 +607,7 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
 {
     const bool params = dgain || dshift;
     const Shape sh = shape_of(d, vec_of(type));
-    const int32_t blocks = blocks_of(n, sh);
+    const int32_t blocks = blocks_of(n, sh, true);
     if (!relu)
         y = nullptr;
     if (n > 0 && (dx || params)) {
