@@ -27,79 +27,109 @@ struct VecOf {
     typedef T type __attribute__((ext_vector_type(kVecOf<T>), aligned(sizeof(T))));
 };
 
-// A row's elements as lane `l` of L lanes holds them: vector q starts at
-// column (q L + l) V.  Past the row's end: zero, and not stored.
-template <class T, int E>
+// How the elements behind a row's last whole vector are held: there are none,
+// one a lane by the row's first lanes (one more element each), or by the lane
+// whose vector they begin, element by element (rows of too few lanes).
+enum Rest { kNone, kLanes, kVector };
+
+// The columns that lane l of L lanes holds: vector q starts at (q L + l) V.
+template <class T, int E, Rest REST>
+struct Columns {
+    static constexpr int V = kVecOf<T>, N = E + (REST == kLanes);
+    static_assert(E % V == 0, "whole vectors");
+    int d, l, L;
+    __device__ __forceinline__ int operator()(int e) const
+    {
+        return REST == kLanes && e == E ? d / V * V + l : ((e / V) * L + l) * V + e % V;
+    }
+    // element e is one of the row's
+    __device__ __forceinline__ bool in(int e) const
+    {
+        if (REST == kVector)
+            return (*this)(e) < d;
+        return REST == kLanes && e == E ? l < d % V : (*this)(e / V * V) + V <= d;
+    }
+    // f[e] = p ? p[column] : dflt, zero past the row's end
+    __device__ __forceinline__ void read(const float *__restrict__ p, float dflt, float (&f)[N]) const
+    {
+#pragma unroll
+        for (int q = 0; q < E / V; ++q) {
+            const int c = (*this)(q * V);
+            if (c + V <= d) {
+#pragma unroll
+                for (int j = 0; j < V; j += 4) {
+                    typename VecOf<float>::type v = {dflt, dflt, dflt, dflt};
+                    if (p)
+                        v = *reinterpret_cast<const typename VecOf<float>::type *>(p + c + j);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        f[q * V + j + i] = v[i];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    f[q * V + j] = REST == kVector && c + j < d ? (p ? p[c + j] : dflt) : 0.f;
+            }
+        }
+        if constexpr (REST == kLanes)
+            f[E] = in(E) ? (p ? p[(*this)(E)] : dflt) : 0.f;
+    }
+};
+
+// A row's elements as its lane holds them; zero past the row's end, and not
+// stored there.
+template <class T, int E, Rest REST>
 struct Row {
     static constexpr int V = kVecOf<T>, Q = E / V;
-    static_assert(E % V == 0, "whole vectors");
     typename VecOf<T>::type v[Q];
+    T rest;
 
-    __device__ __forceinline__ void load(const T *p, int d, int l, int L)
+    __device__ __forceinline__ void load(const T *p, const Columns<T, E, REST> &at)
     {
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int c = (q * L + l) * V;
-            if (c + V <= d) {
+            const int c = at(q * V);
+            if (c + V <= at.d) {
                 v[q] = *reinterpret_cast<const typename VecOf<T>::type *>(p + c);
             } else {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    v[q][j] = c + j < d ? p[c + j] : (T)0.f;
+                    v[q][j] = REST == kVector && c + j < at.d ? p[c + j] : (T)0.f;
             }
         }
+        if constexpr (REST == kLanes)
+            rest = at.in(E) ? p[at(E)] : (T)0.f;
     }
-    __device__ __forceinline__ float at(int e) const { return (float)v[e / V][e % V]; }
-    __device__ __forceinline__ void set(int e, float x) { v[e / V][e % V] = (T)x; }
-    __device__ __forceinline__ void store(T *p, int d, int l, int L) const
+    __device__ __forceinline__ float operator[](int e) const
+    {
+        return (float)(e < E ? v[e / V][e % V] : rest);
+    }
+    __device__ __forceinline__ void set(int e, float x)
+    {
+        if (e < E)
+            v[e / V][e % V] = (T)x;
+        else
+            rest = (T)x;
+    }
+    __device__ __forceinline__ void store(T *p, const Columns<T, E, REST> &at) const
     {
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
-            const int c = (q * L + l) * V;
-            if (c + V <= d) {
+            const int c = at(q * V);
+            if (c + V <= at.d) {
                 *reinterpret_cast<typename VecOf<T>::type *>(p + c) = v[q];
-            } else {
+            } else if constexpr (REST == kVector) {
 #pragma unroll
                 for (int j = 0; j < V; ++j)
-                    if (c + j < d)
+                    if (c + j < at.d)
                         p[c + j] = v[q][j];
             }
         }
+        if constexpr (REST == kLanes)
+            if (at.in(E))
+                p[at(E)] = rest;
     }
 };
-
-// Column of element e of a lane's row, for parameter arrays.
-template <class T>
-__device__ __forceinline__ int column(int e, int l, int L)
-{
-    constexpr int V = kVecOf<T>;
-    return ((e / V) * L + l) * V + e % V;
-}
-
-// f[e] = p ? p[column of element e] : dflt, zero past the row's end.
-template <class T, int E>
-__device__ __forceinline__ void load_params(const float *__restrict__ p, float dflt, int d, int l,
-                                            int L, float (&f)[E])
-{
-    constexpr int V = kVecOf<T>;
-#pragma unroll
-    for (int q = 0; q < E / V; ++q) {
-        const int c = (q * L + l) * V;
-        if (p && c + V <= d) {
-#pragma unroll
-            for (int j = 0; j < V; j += 4) {
-                const auto v = *reinterpret_cast<const VecOf<float>::type *>(p + c + j);
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    f[q * V + j + i] = v[i];
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                f[q * V + j] = c + j < d ? (p ? p[c + j] : dflt) : 0.f;
-        }
-    }
-}
 
 // Sums of K values over the row's lanes, to all of them.  Rows of one
 // workgroup's waves add theirs through `red`, two halves used in turn, so
@@ -130,7 +160,7 @@ __device__ __forceinline__ void row_sum(float (&x)[K], float (*red)[16 * 2], int
     }
 }
 
-template <class T, int GL, int WAVES, int E>
+template <class T, int GL, int WAVES, int E, Rest REST>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_forward(
     int32_t n, int32_t d, const T *x, int64_t ldx, const float *__restrict__ gain,
     const float *__restrict__ shift, float eps, bool relu, T *y, int64_t ldy,
@@ -142,36 +172,38 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_f
     int half = 0;
     const int l = threadIdx.x % L;
     const int64_t step = (int64_t)gridDim.x * R;
-    float g[E], b[E];
-    load_params<T, E>(gain, 1.f, d, l, L, g);
-    load_params<T, E>(shift, 0.f, d, l, L, b);
+    const Columns<T, E, REST> at{d, l, L};
+    constexpr int N = at.N;
+    float g[N], b[N];
+    at.read(gain, 1.f, g);
+    at.read(shift, 0.f, b);
     const float inv = 1.f / (float)d;
     for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < n; r += step) {
-        Row<T, E> in;
-        in.load(x + r * ldx, d, l, L);
+        Row<T, E, REST> in;
+        in.load(x + r * ldx, at);
         float s[1] = {0.f};
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            s[0] += in.at(e);
+        for (int e = 0; e < N; ++e)
+            s[0] += in[e];
         row_sum<GL, WAVES, 1>(s, red, half);
         const float mean = s[0] * inv;
         s[0] = 0.f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float c = column<T>(e, l, L) < d ? in.at(e) - mean : 0.f;
+        for (int e = 0; e < N; ++e) {
+            const float c = at.in(e) ? in[e] - mean : 0.f;
             s[0] = fmaf(c, c, s[0]);
         }
         row_sum<GL, WAVES, 1>(s, red, half);
         const float rstd = 1.f / sqrtf(fmaf(s[0], inv, eps));
-        Row<T, E> out;
+        Row<T, E, REST> out;
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            float z = fmaf((in.at(e) - mean) * rstd, g[e], b[e]);
+        for (int e = 0; e < N; ++e) {
+            float z = fmaf((in[e] - mean) * rstd, g[e], b[e]);
             if (relu)
                 z = z <= 0.f ? 0.f : z;   // (a NaN stays one)
             out.set(e, z);
         }
-        out.store(y + r * ldy, d, l, L);
+        out.store(y + r * ldy, at);
         if (stats && l == 0)
             *reinterpret_cast<float2 *>(stats + 2 * r) = make_float2(mean, rstd);
     }
@@ -180,7 +212,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_f
 // dx of each row, and the workgroup's partial sums of dgain and dshift: a
 // lane adds its columns over its rows in registers, the rows side by side in
 // the workgroup are added through LDS at the end.
-template <class T, int GL, int WAVES, int E, bool PARAMS>
+template <class T, int GL, int WAVES, int E, Rest REST, bool PARAMS>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_backward(
     int32_t n, int32_t d, const T *__restrict__ x, int64_t ldx, const float *__restrict__ gain,
     const T *__restrict__ y, int64_t ldy, const T *dy, int64_t lddy,
@@ -192,29 +224,31 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
     int half = 0;
     const int l = threadIdx.x % L;
     const int64_t step = (int64_t)gridDim.x * R;
-    float g[E], dg[PARAMS ? E : 1], db[PARAMS ? E : 1];
-    load_params<T, E>(gain, 1.f, d, l, L, g);
+    const Columns<T, E, REST> at{d, l, L};
+    constexpr int N = at.N;
+    float g[N], dg[PARAMS ? N : 1], db[PARAMS ? N : 1];
+    at.read(gain, 1.f, g);
     if constexpr (PARAMS)
 #pragma unroll
-        for (int e = 0; e < E; ++e)
+        for (int e = 0; e < N; ++e)
             dg[e] = db[e] = 0.f;
     const float inv = 1.f / (float)d;
     for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < n; r += step) {
-        Row<T, E> in, up, out;
-        in.load(x + r * ldx, d, l, L);
-        up.load(dy + r * lddy, d, l, L);
+        Row<T, E, REST> in, up, out;
+        in.load(x + r * ldx, at);
+        up.load(dy + r * lddy, at);
         if (y) {   // the ReLU mask of the forward's output
-            out.load(y + r * ldy, d, l, L);
+            out.load(y + r * ldy, at);
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                if (!(out.at(e) > 0.f))
+            for (int e = 0; e < N; ++e)
+                if (!(out[e] > 0.f))
                     up.set(e, 0.f);
         }
         const float2 st = *reinterpret_cast<const float2 *>(stats + 2 * r);
         float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float xh = (in.at(e) - st.x) * st.y, D = up.at(e), ge = D * g[e];
+        for (int e = 0; e < N; ++e) {
+            const float xh = (in[e] - st.x) * st.y, D = up[e], ge = D * g[e];
             s[0] += ge;
             s[1] = fmaf(ge, xh, s[1]);
             if constexpr (PARAMS) {
@@ -226,11 +260,11 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
             row_sum<GL, WAVES, 2>(s, red, half);
             const float c0 = s[0] * inv, c1 = s[1] * inv;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float xh = (in.at(e) - st.x) * st.y;
-                out.set(e, st.y * (up.at(e) * g[e] - c0 - xh * c1));
+            for (int e = 0; e < N; ++e) {
+                const float xh = (in[e] - st.x) * st.y;
+                out.set(e, st.y * (up[e] * g[e] - c0 - xh * c1));
             }
-            out.store(dx + r * lddx, d, l, L);
+            out.store(dx + r * lddx, at);
         }
     }
     if constexpr (PARAMS) {
@@ -238,8 +272,8 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
         // the R rows of the workgroup, one column set a time
         __shared__ float sum[R > 1 ? kThreads : 1];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int c = column<T>(e, l, L);
+        for (int e = 0; e < N; ++e) {
+            const int c = at(e);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 float v = k ? db[e] : dg[e];
@@ -252,7 +286,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
                             v += sum[i * L + l];
                     lds_barrier();
                 }
-                if (threadIdx.x < L && c < d)
+                if (threadIdx.x < L && at.in(e))
                     p[k * d + c] = v;
             }
         }
@@ -278,40 +312,40 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_forward_wide(
         const T *row = x + r * ldx;
         float s[1] = {0.f};
         for (int c = threadIdx.x * V; c < d; c += kWideThreads * V) {
-            Row<T, V> in;
-            in.load(row + c, d - c, 0, 1);
+            Row<T, V, kVector> in;
+            in.load(row + c, {d - c, 0, 1});
 #pragma unroll
             for (int e = 0; e < V; ++e)
-                s[0] += in.at(e);
+                s[0] += in[e];
         }
         row_sum<kWave, kWideWaves, 1>(s, red, half);
         const float mean = s[0] * inv;
         s[0] = 0.f;
         for (int c = threadIdx.x * V; c < d; c += kWideThreads * V) {
-            Row<T, V> in;
-            in.load(row + c, d - c, 0, 1);
+            Row<T, V, kVector> in;
+            in.load(row + c, {d - c, 0, 1});
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const float z = c + e < d ? in.at(e) - mean : 0.f;
+                const float z = c + e < d ? in[e] - mean : 0.f;
                 s[0] = fmaf(z, z, s[0]);
             }
         }
         row_sum<kWave, kWideWaves, 1>(s, red, half);
         const float rstd = 1.f / sqrtf(fmaf(s[0], inv, eps));
         for (int c = threadIdx.x * V; c < d; c += kWideThreads * V) {
-            Row<T, V> in;
-            in.load(row + c, d - c, 0, 1);
+            Row<T, V, kVector> in;
+            in.load(row + c, {d - c, 0, 1});
             float g[V], b[V];
-            load_params<T, V>(gain ? gain + c : nullptr, 1.f, d - c, 0, 1, g);
-            load_params<T, V>(shift ? shift + c : nullptr, 0.f, d - c, 0, 1, b);
+            Columns<T, V, kVector>{d - c, 0, 1}.read(gain ? gain + c : nullptr, 1.f, g);
+            Columns<T, V, kVector>{d - c, 0, 1}.read(shift ? shift + c : nullptr, 0.f, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                float z = fmaf((in.at(e) - mean) * rstd, g[e], b[e]);
+                float z = fmaf((in[e] - mean) * rstd, g[e], b[e]);
                 if (relu)
                     z = z <= 0.f ? 0.f : z;
                 in.set(e, z);
             }
-            in.store(y + r * ldy + c, d - c, 0, 1);
+            in.store(y + r * ldy + c, {d - c, 0, 1});
         }
         if (stats && threadIdx.x == 0)
             *reinterpret_cast<float2 *>(stats + 2 * r) = make_float2(mean, rstd);
@@ -332,16 +366,16 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(
         const float2 st = *reinterpret_cast<const float2 *>(stats + 2 * r);
         // e = D gain and xh of the vector at column c
         auto terms = [&](int c, float (&ge)[V], float (&xh)[V]) {
-            Row<T, V> in, up, out;
-            in.load(x + r * ldx + c, d - c, 0, 1);
-            up.load(dy + r * lddy + c, d - c, 0, 1);
-            load_params<T, V>(gain ? gain + c : nullptr, 1.f, d - c, 0, 1, ge);
+            Row<T, V, kVector> in, up, out;
+            in.load(x + r * ldx + c, {d - c, 0, 1});
+            up.load(dy + r * lddy + c, {d - c, 0, 1});
+            Columns<T, V, kVector>{d - c, 0, 1}.read(gain ? gain + c : nullptr, 1.f, ge);
             if (y)
-                out.load(y + r * ldy + c, d - c, 0, 1);
+                out.load(y + r * ldy + c, {d - c, 0, 1});
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                xh[e] = (in.at(e) - st.x) * st.y;
-                ge[e] = y && !(out.at(e) > 0.f) ? 0.f : up.at(e) * ge[e];
+                xh[e] = (in[e] - st.x) * st.y;
+                ge[e] = y && !(out[e] > 0.f) ? 0.f : up[e] * ge[e];
             }
         };
         float s[2] = {0.f, 0.f}, ge[V], xh[V];
@@ -357,11 +391,11 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(
         const float c0 = s[0] * inv, c1 = s[1] * inv;
         for (int c = threadIdx.x * V; c < d; c += kWideThreads * V) {
             terms(c, ge, xh);
-            Row<T, V> out;
+            Row<T, V, kVector> out;
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 out.set(e, st.y * (ge[e] - c0 - xh[e] * c1));
-            out.store(dx + r * lddx + c, d - c, 0, 1);
+            out.store(dx + r * lddx + c, {d - c, 0, 1});
         }
     }
 }
@@ -473,12 +507,17 @@ int32_t blocks_of(int32_t n, const Shape &s, bool backward)
 
 // Calls f with the row shape as template arguments.
 template <class T, class F>
-hipError_t with_shape(const Shape &s, F f)
+hipError_t with_shape(const Shape &s, int32_t d, F f)
 {
     constexpr int V = kVecOf<T>;
 #define DIGEST_SHAPE(GL, W, E) \
-    if (s.gl == GL && s.waves == W && s.e == E) \
-        return f.template operator()<GL, W, E>();
+    if (s.gl == GL && s.waves == W && s.e == E) { \
+        if constexpr (GL < V) \
+            return f.template operator()<GL, W, E, kVector>(); \
+        else \
+            return d % V ? f.template operator()<GL, W, E, kLanes>() \
+                         : f.template operator()<GL, W, E, kNone>(); \
+    }
     DIGEST_SHAPE(2, 1, V)
     DIGEST_SHAPE(4, 1, V)
     DIGEST_SHAPE(8, 1, V)
@@ -509,14 +548,14 @@ struct Forward {
     float *stats;
     int32_t blocks;
     hipStream_t s;
-    template <int GL, int W, int E>
+    template <int GL, int W, int E, Rest REST>
     hipError_t operator()() const
     {
         if (d > kHeldWidth)
             k_norm_forward_wide<T><<<blocks, kWideThreads, 0, s>>>(
                 n, d, (const T *)x, ldx, gain, shift, eps, relu, (T *)y, ldy, stats);
         else
-            k_norm_forward<T, GL, W, E><<<blocks, W == 1 ? kThreads : W * kWave, 0, s>>>(
+            k_norm_forward<T, GL, W, E, REST><<<blocks, W == 1 ? kThreads : W * kWave, 0, s>>>(
                 n, d, (const T *)x, ldx, gain, shift, eps, relu, (T *)y, ldy, stats);
         return hipGetLastError();
     }
@@ -538,13 +577,13 @@ struct Backward {
     float *part;   // null: no sums
     int32_t blocks;
     hipStream_t s;
-    template <int GL, int W, int E>
+    template <int GL, int W, int E, Rest REST>
     hipError_t operator()() const
     {
         constexpr int threads = W == 1 ? kThreads : W * kWave;
         if constexpr (GL * W * E <= kFusedWidth)   // (never rows past kHeldWidth)
             if (part) {
-                k_norm_backward<T, GL, W, E, true><<<blocks, threads, 0, s>>>(
+                k_norm_backward<T, GL, W, E, REST, true><<<blocks, threads, 0, s>>>(
                     n, d, (const T *)x, ldx, gain, (const T *)y, ldy, (const T *)dy, lddy, stats,
                     (T *)dx, lddx, part);
                 return hipGetLastError();
@@ -559,7 +598,7 @@ struct Backward {
                 n, d, (const T *)x, ldx, gain, (const T *)y, ldy, (const T *)dy, lddy, stats,
                 (T *)dx, lddx);
         else if (dx)
-            k_norm_backward<T, GL, W, E, false><<<blocks, threads, 0, s>>>(
+            k_norm_backward<T, GL, W, E, REST, false><<<blocks, threads, 0, s>>>(
                 n, d, (const T *)x, ldx, gain, (const T *)y, ldy, (const T *)dy, lddy, stats,
                 (T *)dx, lddx, nullptr);
         return hipGetLastError();
@@ -588,13 +627,14 @@ hipError_t launch_norm_forward(int32_t type, int32_t n, int32_t d, const void *x
     switch (type) {
     case kF32:
         return with_shape<float>(
-            sh, Forward<float>{n, d, x, ldx, gain, shift, eps, relu, y, ldy, stats, blocks, s});
+            sh, d, Forward<float>{n, d, x, ldx, gain, shift, eps, relu, y, ldy, stats, blocks, s});
     case kBF16:
         return with_shape<__bf16>(
-            sh, Forward<__bf16>{n, d, x, ldx, gain, shift, eps, relu, y, ldy, stats, blocks, s});
+            sh, d, Forward<__bf16>{n, d, x, ldx, gain, shift, eps, relu, y, ldy, stats, blocks, s});
     case kF16:
-        return with_shape<_Float16>(
-            sh, Forward<_Float16>{n, d, x, ldx, gain, shift, eps, relu, y, ldy, stats, blocks, s});
+        return with_shape<_Float16>(sh, d,
+                                    Forward<_Float16>{n, d, x, ldx, gain, shift, eps, relu, y, ldy,
+                                                      stats, blocks, s});
     }
     return hipErrorInvalidValue;
 }
@@ -615,17 +655,16 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
         hipError_t e = hipErrorInvalidValue;
         switch (type) {
         case kF32:
-            e = with_shape<float>(sh, Backward<float>{n, d, x, ldx, gain, y, ldy, dy, lddy,
-                                                            stats, dx, lddx, p, blocks, s});
+            e = with_shape<float>(sh, d, Backward<float>{n, d, x, ldx, gain, y, ldy, dy, lddy, stats,
+                                                   dx, lddx, p, blocks, s});
             break;
         case kBF16:
-            e = with_shape<__bf16>(sh, Backward<__bf16>{n, d, x, ldx, gain, y, ldy, dy, lddy,
-                                                              stats, dx, lddx, p, blocks, s});
+            e = with_shape<__bf16>(sh, d, Backward<__bf16>{n, d, x, ldx, gain, y, ldy, dy, lddy, stats,
+                                                   dx, lddx, p, blocks, s});
             break;
         case kF16:
-            e = with_shape<_Float16>(sh,
-                                           Backward<_Float16>{n, d, x, ldx, gain, y, ldy, dy, lddy,
-                                                              stats, dx, lddx, p, blocks, s});
+            e = with_shape<_Float16>(sh, d, Backward<_Float16>{n, d, x, ldx, gain, y, ldy, dy, lddy, stats,
+                                                   dx, lddx, p, blocks, s});
             break;
         }
         if (e != hipSuccess)
