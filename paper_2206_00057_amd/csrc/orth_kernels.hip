@@ -461,6 +461,15 @@ __device__ __forceinline__ bool stored(int rp, int cp, int mb, int nb)
     return mb < rp && nb < cp;
 }
 
+__device__ __forceinline__ floatx16 zero16()
+{
+    floatx16 z;
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+        z[e] = 0.f;
+    return z;
+}
+
 // The large products: a TILE x TILE tile of D per workgroup and CU, 128 (4
 // waves of 64 x 64) or 256 (8 waves of 128 x 64, which read each line of LDS
 // and of memory fewer times).  Lines (32 k) of both operands' rows come into a
@@ -502,14 +511,18 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
     const int lane = threadIdx.x % kWave, wave = wave_id();
     const int wm = wave / WN * TM, wn = wave % WN * TN;   // in blocks of 32
 
-    floatx16 acc[TM][TN];
+    // the small products have sums of their own where registers allow, added at
+    // the end: the large ones are then rounded a third as often
+    constexpr bool TWO = TILE == 128;
+    floatx16 acc[TM][TN], low[TWO ? TM : 1][TWO ? TN : 1];
 #pragma unroll
     for (int x = 0; x < TM; ++x)
 #pragma unroll
-        for (int y = 0; y < TN; ++y)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                acc[x][y][e] = 0.f;
+        for (int y = 0; y < TN; ++y) {
+            acc[x][y] = zero16();
+            if constexpr (TWO)
+                low[x][y] = zero16();
+        }
 
     // A wave's instruction takes 1 KB of a line's 4 KB for 32 rows; rows past
     // the operand repeat its last 32 (their products are not stored).
@@ -551,8 +564,9 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
             for (int x = 0; x < TM; ++x)
 #pragma unroll
                 for (int y = 0; y < TN; ++y) {
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                        f.p[k == 2][x], f.q[k == 1][y], acc[x][y], 0, 0, 0);
+                    floatx16 &d = TWO && k > 0 ? low[TWO ? x : 0][TWO ? y : 0] : acc[x][y];
+                    d = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.p[k == 2][x], f.q[k == 1][y], d, 0,
+                                                               0, 0);
                     beside((k * TM + x) * TN + y);
                     __builtin_amdgcn_sched_barrier(0);
                 }
@@ -626,6 +640,10 @@ __global__ __launch_bounds__(Waves<TILE>::W *kWave) void k_orth_gemm(OrthBatch b
             const int mb = tm * BM + (wm + x) * 32, nb = tn * BN + (wn + y) * 32;
             if (!stored<MODE>(it.rp, it.cp, mb, nb))
                 continue;
+            if constexpr (TWO)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    acc[x][y][e] += low[x][y][e];
             if (part < 0) {
 #pragma unroll
                 for (int s = 0; s < 2; ++s) {
@@ -733,14 +751,16 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
         if (stores)
             a.load(it, mb + 16 * s, nb);
 
-    floatx16 acc[TS][TS];
+    constexpr bool TWO = TS == 1;   // (sums of their own for the small products, as above)
+    floatx16 acc[TS][TS], low[TWO ? TS : 1][TWO ? TS : 1];
 #pragma unroll
     for (int x = 0; x < TS; ++x)
 #pragma unroll
-        for (int y = 0; y < TS; ++y)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                acc[x][y][e] = 0.f;
+        for (int y = 0; y < TS; ++y) {
+            acc[x][y] = zero16();
+            if constexpr (TWO)
+                low[x][y] = zero16();
+        }
     struct Line {
         half8 p[2][2][TS], q[2][2][TS];   // [16 k][part][block]
     };
@@ -768,9 +788,11 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
 #pragma unroll
                 for (int x = 0; x < TS; ++x)
 #pragma unroll
-                    for (int y = 0; y < TS; ++y)
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                            l.p[s][k == 2][x], l.q[s][k == 1][y], acc[x][y], 0, 0, 0);
+                    for (int y = 0; y < TS; ++y) {
+                        floatx16 &d = TWO && k > 0 ? low[TWO ? x : 0][TWO ? y : 0] : acc[x][y];
+                        d = __builtin_amdgcn_mfma_f32_32x32x16_f16(l.p[s][k == 2][x],
+                                                                   l.q[s][k == 1][y], d, 0, 0, 0);
+                    }
     };
     if (wave < nk) {
         Line l[DEPTH];
@@ -791,12 +813,17 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
 #pragma unroll
         for (int x = 0; x < TS; ++x)
 #pragma unroll
-            for (int y = 0; y < TS; ++y)
+            for (int y = 0; y < TS; ++y) {
+                if constexpr (TWO)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        acc[x][y][e] += low[x][y][e];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
                     sum[wave][(TS * x + y) * 4 + g][lane] =
                         make_float4(acc[x][y][4 * g], acc[x][y][4 * g + 1], acc[x][y][4 * g + 2],
                                     acc[x][y][4 * g + 3]);
+            }
     __syncthreads();
     if (!stores)
         return;
@@ -964,10 +991,10 @@ __device__ __forceinline__ void block_products(const LdsPlane &P, const int (&m)
                                                const LdsPlane &Q, const int (&n)[BLOCKS], int K,
                                                int lane, floatx4 (&acc)[BLOCKS])
 {
+    floatx4 low[BLOCKS];   // (the small products')
 #pragma unroll
     for (int i = 0; i < BLOCKS; ++i)
-        acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 2
+        acc[i] = low[i] = floatx4{0.f, 0.f, 0.f, 0.f};
     for (int k = 0; k < K; k += 32) {
         half8 p[BLOCKS][2], q[BLOCKS][2];
 #pragma unroll
@@ -980,10 +1007,14 @@ __device__ __forceinline__ void block_products(const LdsPlane &P, const int (&m)
 #pragma unroll
         for (int t = 0; t < 3; ++t)
 #pragma unroll
-            for (int i = 0; i < BLOCKS; ++i)
-                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i][t == 2], q[i][t == 1], acc[i],
-                                                                0, 0, 0);
+            for (int i = 0; i < BLOCKS; ++i) {
+                floatx4 &d = t ? low[i] : acc[i];
+                d = __builtin_amdgcn_mfma_f32_16x16x32_f16(p[i][t == 2], q[i][t == 1], d, 0, 0, 0);
+            }
     }
+#pragma unroll
+    for (int i = 0; i < BLOCKS; ++i)
+        acc[i] += low[i];
 }
 
 template <bool UPDATE, class T>
