@@ -459,8 +459,9 @@ digest_status digest_sgd_average(float *w, const float *const *grads, int32_t n_
  *   stats    device [n_rows][2], (mean, rstd) of each row, 8-byte aligned;
  *            written by the forward (NULL: not kept), read by the backward.
  * Every sum runs in a fixed order (equal calls give equal bits).  A row with
- * a NaN or an infinity is NaN (through the ReLU too) and touches no other;
- * rows whose squared deviations pass fp32's range come out as shift.
+ * a NaN or an infinity is NaN (through the ReLU too) and touches no other.
+ * Rows whose sums or squared deviations pass fp32's range are not normalised
+ * (they come out as shift or NaN).
  * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
  */
 digest_status digest_layer_norm_forward(int64_t n_rows, int32_t width, int32_t type,

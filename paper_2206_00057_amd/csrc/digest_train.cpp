@@ -379,6 +379,9 @@ digest_status digest_orthogonalize(int32_t count, const int32_t *rows, const int
     for (int32_t i = 1; i < count; ++i)
         if (order[i] == order[i - 1])
             return fail(DIGEST_EINVAL, "two matrices have the same output");
+    for (int32_t i = 0; i < count; ++i)
+        if (in[i] != out[i] && std::binary_search(order, order + count, in[i]))
+            return fail(DIGEST_EINVAL, "matrix %d is the output of another", i);
     if (digest_status st =
             check_workspace(workspace, bytes, orth_workspace(count, rows, cols)))
         return st;

@@ -196,6 +196,22 @@ def test_in_place_and_absent_arrays(D):
         assert none is None and torch.equal(y2, y)
 
 
+def test_offsets_past_32_bits(D):
+    """Row strides that take the last rows past 2^31 elements."""
+    ld, n, d = 1_200_000_000, 3, 133
+    whole = torch.zeros(2 * ld + 2000, dtype=torch.bfloat16, device="cuda")
+    part = lambda at: whole.as_strided((n, d), (ld, 1), at)
+    x, y, dy, dx = part(3), part(303), part(601), part(901)
+    x.copy_(rows(n, d, torch.bfloat16, 1))
+    dy.copy_(rows(n, d, torch.bfloat16, 2))
+    gain, shift = params(d, 3)
+    _, stats = call_forward(D, x, gain, shift, True, y=y)
+    check_forward(y, stats, x, gain, shift, True)
+    out = call_backward(D, x, gain, y, dy, stats, True, dx=dx)
+    check_backward(*out, x, gain, y, dy, stats, True)
+    assert int((whole != 0).sum()) <= 4 * n * d
+
+
 def test_no_rows(D):
     x = torch.empty(0, 70, device="cuda")
     y, stats = call_forward(D, x, None, None, True)

@@ -145,6 +145,57 @@ def test_groups(D):
     assert all(float((a - b).abs().max()) <= 1e-4 for a, b in zip(one, outs))
 
 
+@pytest.mark.parametrize("shapes", [
+    [(1024, 1024), (300, 4096), (2500, 49), (1030, 1100)],   # long and short k side by side
+    [(2048, 2048), (3, 5)], [(1500, 1500)], [(600, 4100), (4100, 600)],
+    [(4096, 4096)], [(2300, 5000)], [(129, 9000), (4000, 257), (513, 513)]])
+def test_large_groups(D, shapes):
+    mats = [matrix(r, c, 3 + i) for i, (r, c) in enumerate(shapes)]
+    outs = run(D, mats)
+    for u, out in zip(mats, outs):
+        check(out, u)
+    again = run(D, mats)
+    assert all(torch.equal(a, b) for a, b in zip(outs, again))
+
+
+def test_offsets_past_32_bits(D):
+    """Row strides that take the last rows past 2^31 elements."""
+    ld, r, c = 1_200_000_000, 3, 70
+    whole = torch.zeros(2 * ld + 1000, dtype=torch.bfloat16, device="cuda")
+    u = whole.as_strided((r, c), (ld, 1), 11)
+    out = whole.as_strided((r, c), (ld, 1), 311)
+    u.copy_(matrix(r, c, 1, "noise"))
+    run(D, [u], [out])
+    check(out, u)
+    assert int((whole != 0).sum()) <= 2 * r * c
+
+
+def test_calls_in_turn_share_a_workspace(D):
+    """Two captured updates over one workspace, replayed one after the other."""
+    sets = [muon_setup(s, 2, 4) for s in ([(90, 200)], [(33, 40), (300, 70)])]
+    mine = [[[v.clone() for v in w], [v.clone() for v in m]] for w, m, _ in sets]
+    ws = torch.empty(max(D.digest_orthogonalize_query([v.shape for v in w]) for w, _, _ in sets),
+                     dtype=torch.uint8, device="cuda")
+    graphs = []
+    for (w, m, g) in sets:
+        D.digest_muon_average(w, m, g, ws, 0.0, 1.0)   # (lr 0: weights stay; momenta grow)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            D.digest_muon_average(w, m, g, ws, 0.1)
+        graphs.append(graph)
+    for (w, m), (_, _, g) in zip(mine, sets):
+        D.digest_muon_average(w, m, g, ws, 0.0, 1.0)
+    for i in range(3):
+        for k, (w, m) in enumerate(mine):
+            D.digest_muon_average(w, m, sets[k][2], ws, 0.1)
+        torch.cuda.synchronize()
+        for graph in graphs:
+            graph.replay()
+        torch.cuda.synchronize()
+        for (w, m), (rw, rm, _) in zip(mine, sets):
+            assert all(torch.equal(a, b) for a, b in zip(w + m, rw + rm)), i
+
+
 def test_strides_and_in_place(D):
     for t in TYPES.values():
         # three column slices of one array, into slices of another

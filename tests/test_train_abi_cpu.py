@@ -82,6 +82,7 @@ def test_orthogonalize_refuses():
                dict(outs=None), dict(ins=_ptrs(P[0], None)), dict(ins=_ptrs(P[0] + 2, P[1])),
                dict(outs=_ptrs(P[2], P[3] + 1)), dict(ldi=_i64(7, 4)), dict(ldo=_i64(8, 3)),
                dict(ldi=_i64(8, 2 ** 31)), dict(outs=_ptrs(P[2], P[2])), dict(steps=0),
+               dict(outs=_ptrs(P[1], P[3])),                      # the other's input
                dict(steps=65), dict(steps=1, coeffs=_f32(float("nan"), 0, 0)),
                dict(steps=1, coeffs=_f32(1, float("inf"), 0)),
                dict(steps=1, coeffs=_f32(0, 0, 0)),               # nothing is left
@@ -90,6 +91,7 @@ def test_orthogonalize_refuses():
         assert call(**kw) == D.EINVAL, kw
     need = D.digest_orthogonalize_query([(4, 8), (8, 4)])
     assert call(nbytes=need - 1) == D.ENOMEM
+    assert call(outs=_ptrs(P[0], P[1]), nbytes=0) == D.ENOMEM     # in place is fine
 
 
 def test_muon_refuses():
@@ -128,6 +130,11 @@ def test_orthogonalize_query():
         up = lambda v: v + 256
         high = sum(4 * (3 * up(r) * up(c) + 2 * up(min(r, c)) ** 2) + 8192 for r, c in shapes)
         assert b % 256 == 0 and low <= b <= high, (shapes, b)
+        assert b < 2 ** 40
+    # large ones: at most one part of a tile for each CU and split beside the planes
+    for shapes in ([(65536, 65536)], [(1024, 4096)] * 16):
+        low = sum(4 * (3 * r * c + 2 * min(r, c) ** 2) for r, c in shapes)
+        assert low <= q(shapes) <= low + (16 * 8192 + (1 << 28)), shapes
     # groups of sixteen share their memory
     assert q([(100, 100)] * 40) == q([(100, 100)] * 16)
     with pytest.raises(D.DigestError):
