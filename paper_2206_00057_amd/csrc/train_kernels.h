@@ -35,7 +35,7 @@ hipError_t launch_norm_backward(int32_t type, int32_t n, int32_t d, const void *
 // of two fp16, in the order in which the matrix instructions take them.  Rows
 // and k are padded to kOrthPad, with zeros.
 constexpr int kOrthItems = 16;       // matrices of one launch
-constexpr int kOrthGrads = 192;      // gradient pointers of one launch (its arguments stay below 4 KB)
+constexpr int kOrthGrads = 192;      // gradients of one launch (arguments below 4 KB)
 constexpr int kOrthPad = 64;
 constexpr int kOrthSumBlocks = 1024;  // partial sums of |U|_F^2, at most
 constexpr int64_t kOrthSumRun = 4096;

@@ -43,7 +43,8 @@ def rows(n, d, t, seed, pad=0, start=0, scale=1.0, offset=0.3):
 
 def params(d, seed):
     g = torch.Generator().manual_seed(seed)
-    return (1.0 + 0.2 * torch.randn(d, generator=g)).cuda(), (0.3 * torch.randn(d, generator=g)).cuda()
+    return ((1.0 + 0.2 * torch.randn(d, generator=g)).cuda(),
+            (0.3 * torch.randn(d, generator=g)).cuda())
 
 
 def forward64(x, gain, shift, relu):

@@ -79,7 +79,8 @@ def network64(g, parts, X, y, Ws, norms):
     nll = -logp[torch.arange(g.n), torch.from_numpy(y.astype(np.int64))]
     loss = sum(nll[torch.from_numpy(p.owned)].mean() for p in parts) / len(parts)
     loss.backward()
-    return float(loss.detach()), h.detach(), [w.grad for w in Ws], [[v.grad for v in n] for n in norms]
+    return (float(loss.detach()), h.detach(), [w.grad for w in Ws],
+            [[v.grad for v in n] for n in norms])
 
 
 def orth64(u):
@@ -195,7 +196,8 @@ def test_gat_norm_gradients_by_differences():
             v[i] = keep - h
             down = loss()
             v[i] = keep
-            assert abs((up - down) / (2 * h) - float(gr[i])) <= 2e-4 + 0.05 * abs(float(gr[i])), (l, k, i)
+            diff = (up - down) / (2 * h)
+            assert abs(diff - float(gr[i])) <= 2e-4 + 0.05 * abs(float(gr[i])), (l, k, i)
 
 
 def test_io_overlap_gives_the_same_rows():

@@ -276,7 +276,8 @@ def test_muon_average(D, shapes, M, nesterov):
         # M roundings of the sum, the mean's, the momentum's two
         assert bool(((mom[i].double() - m).abs() <= (M + 4) * U * size).all())
         u = g + beta * m if nesterov else m
-        start = (M + 8) * U * float(torch.linalg.vector_norm(2 * size) / torch.linalg.vector_norm(u))
+        start = (M + 8) * U * float(torch.linalg.vector_norm(2 * size) /
+                                    torch.linalg.vector_norm(u))
         o, tol = exact(u, start=start)
         ref = (1 - lr * decay) * w0[i].double() - lr * scales[i] * o
         # the factor 1 - lr decay, its product, the step's and the difference
