@@ -283,6 +283,8 @@ digest_status digest_layer_norm_forward(int64_t n_rows, int32_t width, int32_t t
     if (stats)
         if (digest_status st = check_ptr(stats, 8, "stats"))
             return st;
+    if (x == y && ldx != ldy)
+        return fail(DIGEST_EINVAL, "y is x with another row stride");
     if (digest_status st = check_stream((hipStream_t)hip_stream))
         return st;
     return hip_check(digest::launch_norm_forward(type, (int32_t)n_rows, width, x, ldx, gain, shift,
@@ -331,6 +333,14 @@ digest_status digest_layer_norm_backward(int64_t n_rows, int32_t width, int32_t 
     if (dgain || dshift)
         if (digest_status st = check_workspace(workspace, bytes, norm_workspace(n_rows, width)))
             return st;
+    if (n_rows > 0 && dx) {
+        if (dx == dy && lddx != lddy)
+            return fail(DIGEST_EINVAL, "dx is dy with another row stride");
+        if (dx == x || (relu && dx == y))
+            return fail(DIGEST_EINVAL, "dx is x or y");
+    }
+    if (dgain && dgain == dshift)
+        return fail(DIGEST_EINVAL, "dgain is dshift");
     if (digest_status st = check_stream((hipStream_t)hip_stream))
         return st;
     return hip_check(digest::launch_norm_backward(type, (int32_t)n_rows, width, x, ldx, gain, y,

@@ -141,3 +141,22 @@ def test_orthogonalize_query():
         q([(0, 4)])
     with pytest.raises(ValueError):
         q([])
+
+
+def test_layer_norm_refuses_shared_outputs():
+    """y may be x and dx may be dy, with one stride; no other output lies where
+    another array starts."""
+    L = D._train_lib()
+
+    def fwd(x, ldx, y, ldy):
+        return L.digest_layer_norm_forward(4, 8, D.F32, x, ldx, None, None, 1e-5, 0, y, ldy, None,
+                                           None)
+
+    def bwd(x=P[0], y=P[1], dy=P[2], lddy=8, dx=P[3], lddx=8, dgain=P[4], dshift=P[5]):
+        return L.digest_layer_norm_backward(4, 8, D.F32, x, 8, None, D.ACT_RELU, y, 8, dy, lddy,
+                                            P[6], dx, lddx, dgain, dshift, P[7], 1 << 19, None)
+
+    assert fwd(P[0], 8, P[0], 9) == D.EINVAL
+    assert fwd(P[0], 9, P[0], 8) == D.EINVAL
+    for kw in (dict(dx=P[2], lddx=9), dict(dx=P[0]), dict(dx=P[1]), dict(dgain=P[5])):
+        assert bwd(**kw) == D.EINVAL, kw
