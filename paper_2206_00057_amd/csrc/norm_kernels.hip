@@ -2,12 +2,13 @@
 //
 // A row of up to 16,384 elements is held in the registers of GL lanes
 // (GL <= 64, rows of up to 1,024) or of the WAVES waves of one workgroup, E
-// elements a lane in 16-byte vectors, so that x is read once: the mean, then the centred
-// squares (two sums over registers, no cancellation), then the outputs.
-// Bound by memory: 306,250 x 256 float32 with ReLU forward 120 us (5.2 TB/s;
-// a large copy here runs at 5.1), backward 231 us (5.4 TB/s), 16,384 x 4,096
-// bfloat16 backward 85 us (4.7 TB/s).  Sums are fp32, in a fixed order.  Rows may start at any element: global
-// loads and stores take 16-byte vectors at element alignment.
+// elements a lane in 16-byte vectors, so that x is read once: the mean, then
+// the centred squares (two sums over registers, no cancellation), then the
+// outputs.  Bound by memory: 306,250 x 256 float32 with ReLU forward 122 us
+// (5.2 TB/s; a large copy here runs at 5.1), backward 229 us (5.5 TB/s),
+// 16,384 x 4,096 bfloat16 backward 85 us (4.8 TB/s).  Sums are fp32, in a fixed
+// order.  Rows may start at any element: global loads and stores take 16-byte
+// vectors at element alignment.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

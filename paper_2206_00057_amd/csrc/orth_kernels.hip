@@ -10,9 +10,10 @@
 // holds 22 to 23 bits of x, and of h h' + h l' + l h' + l l' the last, at
 // most 2^-22 of a product and 2^-25 on average, is left out.  Three fp16
 // matrix instructions then do the work of one fp32 product at 5 times the
-// fp32 instructions' rate.  The error of five steps against 64 bits is 0.7e-6
-// to 1.5e-6 of the result from 8 x 8 to 2,048 x 2,048 (3.3e-6 at 4,096 x
-// 4,096), that of fp32 products 0.5e-6 to 4.2e-6.  A and B are symmetric: only
+// fp32 instructions' peak rate (3 times, by large library products of either).
+// The error of five steps against 64 bits is 0.7e-6 to 1.5e-6 of the result
+// from 8 x 8 to 2,048 x 2,048 (3.3e-6 at 4,096 x 4,096), that of fp32 products
+// 0.5e-6 to 4.2e-6.  A and B are symmetric: only
 // the tiles on and above the diagonal are computed, each stored twice.
 //
 // Large products are bound by the matrix instructions at the clock that the
@@ -848,8 +849,9 @@ __global__ __launch_bounds__(kSmallWaves *kWave) void k_orth_small(OrthBatch b, 
 // rows and k in [32 j, 32 j + 32) itself, whose layout as a result is the
 // matrix instruction's layout as an operand, and multiplies it by its 32 k of
 // X.  The waves' sums meet in LDS.  B is formed again for every 32 columns of
-// X: 100 x 256 6.0 us a step where B and B X take 4.2 and 4.4, but 256 x 256
-// (eight waves) 9.5 where they take 4.6 each, so it stops at 128.
+// X: 100 x 256 in five steps takes 52 us for 61 (5.8 us a step here), but
+// 256 x 256 (eight waves) 9.5 us a step where B and B X take 4.6 each, so it
+// stops at 128.
 constexpr int kFuseWaves = 4;
 constexpr int kFuseRows = 32 * kFuseWaves;
 
@@ -1208,9 +1210,9 @@ constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each
 //   256   8 + (2.0 + 0.6 n / 256) a line of each round
 // A tile's k may be split where tiles are few or left over by whole rounds:
 // the join takes 3.5 + 0.015 (128) or 4 + 0.045 (256) a part.  (1,024 x 4,096:
-// X X^T 35 us with 64, 20 and 6 with 128 in seven parts each; B X 48 and 30;
-// 256 x 256: 4.6 us with 32, 6.3 with 64, 12 with 128; 4,096 x 4,096: B X 412
-// with 128, 344 with 256.)
+// X X^T 35 us with 64, 20 and 6 with 128 in seven parts each; B X 48 and 32;
+// 256 x 256: 4.8 us with 32, 6.3 with 64, 11 to 13 with 128; 4,096 x 4,096:
+// B X 418 with 128, 348 with 256.)
 template <int MODE>
 OrthPlan plan_products(const OrthBatch &b)
 {
