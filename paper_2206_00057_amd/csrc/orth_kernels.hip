@@ -60,10 +60,11 @@ __device__ __forceinline__ int64_t plane_at(int64_t row, int32_t pitch, int k)
 // The update's matrix U and its norm
 // ---------------------------------------------------------------------------
 
-// The workgroup's sum of v, to all its threads, in a fixed order.
+// The sum of v over a workgroup of THREADS, to all its threads, in a fixed order.
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v)
 {
-    __shared__ double sum[kThreads / kWave];
+    __shared__ double sum[THREADS / kWave];
 #pragma unroll
     for (int off = kWave / 2; off > 0; off >>= 1)
         v += __shfl_xor(v, off);
@@ -72,28 +73,31 @@ __device__ __forceinline__ double block_sum(double v)
     __syncthreads();
     v = 0;
 #pragma unroll
-    for (int w = 0; w < kThreads / kWave; ++w)
+    for (int w = 0; w < THREADS / kWave; ++w)
         v += sum[w];
     return v;
 }
 
-// Runs of kOrthSumRun elements of a matrix, a vector of V a thread: f(element
-// index, count) for each thread's vectors; the matrix's rows one after another
-// where they are contiguous, else each row's runs.
-template <int V, class F>
+// Runs of kOrthSumRun elements of a matrix, one vector of four a thread:
+// f(element index, count) for each thread's vectors; the matrix's rows one
+// after another where they are contiguous, else each row's runs.  (With
+// four a thread they came one after another: the momenta of a 100-256-256-47
+// network from eight gradients 8.4 us, now 4.8; of six matrices of 1,024 x
+// 1,024 to 4,096 34 to 35 either way.)
+constexpr int kRunVec = 4;
+static_assert(kOrthSumRun == kThreads * kRunVec, "a run is one vector a thread");
+template <class F>
 __device__ __forceinline__ void for_vectors(const OrthItem &it, int64_t ld, F f)
 {
+    constexpr int V = kRunVec;
     const bool flat = ld == it.cols;
     const int64_t len = flat ? (int64_t)it.rows * it.cols : it.cols;
     const int64_t runs = (len + kOrthSumRun - 1) / kOrthSumRun;
     for (int64_t q = blockIdx.x; q < runs * (flat ? 1 : it.rows); q += it.sums) {
         const int64_t row = flat ? 0 : q / runs, from = (q - row * runs) * kOrthSumRun;
-#pragma unroll
-        for (int j = 0; j < (int)kOrthSumRun / (kThreads * V); ++j) {
-            const int64_t at = from + (j * kThreads + (int)threadIdx.x) * V;
-            if (at < len)
-                f(row * ld + at, (int)min((int64_t)V, len - at));
-        }
+        const int64_t at = from + (int)threadIdx.x * V;
+        if (at < len)
+            f(row * ld + at, (int)min((int64_t)V, len - at));
     }
 }
 
@@ -132,18 +136,18 @@ __device__ __forceinline__ void store_some(T *p, int n, typename Vec<T, V>::type
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_orth_sum(OrthBatch b)
 {
-    constexpr int V = 16 / sizeof(T);
+    constexpr int V = kRunVec;
     const OrthItem &it = b.item[blockIdx.y];
     if ((int)blockIdx.x >= it.sums)
         return;
     double v = 0;
-    for_vectors<V>(it, it.ldu, [&](int64_t at, int n) {
+    for_vectors(it, it.ldu, [&](int64_t at, int n) {
         const auto x = load_some<T, V>((const T *)it.u + at, n);
 #pragma unroll
         for (int j = 0; j < V; ++j)
             v += (double)(float)x[j] * (double)(float)x[j];
     });
-    v = block_sum(v);
+    v = block_sum<kThreads>(v);
     if (threadIdx.x == 0)
         it.part[blockIdx.x] = v;
 }
@@ -159,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_momentum(OrthBatch b, OrthGra
     float *u = (float *)it.u;
     const float inv = 1.f / (float)per_item;
     double v = 0;
-    for_vectors<4>(it, it.cols, [&](int64_t at, int n) {
+    for_vectors(it, it.cols, [&](int64_t at, int n) {
         auto mo = load_some<float, 4>(it.mom + at, n);
         auto s = load_some<float, 4>(g[0] + at, n);
         int m = 1;
@@ -186,7 +190,7 @@ __global__ __launch_bounds__(kThreads) void k_muon_momentum(OrthBatch b, OrthGra
         store_some<float, 4>(it.mom + at, n, mo);
         store_some<float, 4>(u + at, n, x);
     });
-    v = block_sum(v);
+    v = block_sum<kThreads>(v);
     if (threadIdx.x == 0)
         it.part[blockIdx.x] = v;
 }
@@ -207,8 +211,8 @@ __device__ __forceinline__ void split8(const float (&x)[8], _Float16 *dst)
     *reinterpret_cast<half8 *>(dst + kPart) = l;
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double scale)
+template <class T, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_orth_split(OrthBatch b, double scale)
 {
     __shared__ float tile[kSplitTile][kSplitTile + 1];
     const OrthItem &it = b.item[blockIdx.z];
@@ -218,12 +222,12 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
     if (i0 >= (tall ? it.cp : it.rp) || j0 >= (tall ? it.rp : it.cp))
         return;
     const T *u = (const T *)it.u;
-    constexpr int N = kSplitTile * kSplitTile / kThreads;
+    constexpr int N = kSplitTile * kSplitTile / THREADS;
     const int tj = threadIdx.x % kSplitTile, t0 = threadIdx.x / kSplitTile;
     float x[N];   // (on their way while the norm is formed)
 #pragma unroll
     for (int q = 0; q < N; ++q) {
-        const int i = i0 + t0 + q * (kThreads / kSplitTile), j = j0 + tj;
+        const int i = i0 + t0 + q * (THREADS / kSplitTile), j = j0 + tj;
         x[q] = i < it.rows && j < it.cols ? (float)u[(int64_t)i * it.ldu + j] : 0.f;
     }
     double sum = 0;
@@ -234,20 +238,20 @@ __global__ __launch_bounds__(kThreads) void k_orth_split(OrthBatch b, double sca
         for (int off = kWave / 2; off > 0; off >>= 1)
             sum += __shfl_xor(sum, off);
     } else {
-        for (int i = threadIdx.x; i < it.sums; i += kThreads)
+        for (int i = threadIdx.x; i < it.sums; i += THREADS)
             sum += it.part[i];
-        sum = block_sum(sum);
+        sum = block_sum<THREADS>(sum);
     }
     const double norm = sqrt(sum);
     const double f = norm == 0 ? 0.0 : scale / norm;
 #pragma unroll
     for (int q = 0; q < N; ++q)
-        tile[t0 + q * (kThreads / kSplitTile)][tj] = (float)((double)x[q] * f);
+        tile[t0 + q * (THREADS / kSplitTile)][tj] = (float)((double)x[q] * f);
     __syncthreads();
     _Float16 *p = (_Float16 *)(tall ? it.Xt[0] : it.X);
     _Float16 *pt = (_Float16 *)(tall ? it.X : it.Xt[0]);
     const int kp = tall ? it.rk : it.ck, kt = tall ? it.ck : it.rk;
-    for (int q = threadIdx.x; q < kSplitTile * kSplitTile / 8; q += kThreads) {
+    for (int q = threadIdx.x; q < kSplitTile * kSplitTile / 8; q += THREADS) {
         const int row = q % kSplitTile, k = q / kSplitTile * 8;   // (rows side by side)
         float x[8];
         if (j0 < kp) {
@@ -1364,6 +1368,20 @@ hipError_t launch_muon_momentum(const OrthBatch &b, const OrthGrads &g, int32_t 
     return hipGetLastError();
 }
 
+constexpr int64_t kSplitFew = 1024;   // tiles
+
+template <int THREADS>
+hipError_t launch_split(const OrthBatch &b, int32_t type, dim3 grid, double scale, hipStream_t s)
+{
+    switch (type) {
+    case kF32: k_orth_split<float, THREADS><<<grid, THREADS, 0, s>>>(b, scale); break;
+    case kBF16: k_orth_split<__bf16, THREADS><<<grid, THREADS, 0, s>>>(b, scale); break;
+    case kF16: k_orth_split<_Float16, THREADS><<<grid, THREADS, 0, s>>>(b, scale); break;
+    default: return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+
 hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStream_t s)
 {
     int32_t gi = 1, gj = 1;
@@ -1373,15 +1391,13 @@ hipError_t launch_orth_split(const OrthBatch &b, int32_t type, int32_t e, hipStr
         gi = std::max(gi, (tall ? it.cp : it.rp) / kSplitTile);
         gj = std::max(gj, (tall ? it.rp : it.cp) / kSplitTile);
     }
-    const dim3 grid(gj, gi, b.n);
-    const double scale = std::ldexp(1.0, e);
-    switch (type) {
-    case kF32: k_orth_split<float><<<grid, kThreads, 0, s>>>(b, scale); break;
-    case kBF16: k_orth_split<__bf16><<<grid, kThreads, 0, s>>>(b, scale); break;
-    case kF16: k_orth_split<_Float16><<<grid, kThreads, 0, s>>>(b, scale); break;
-    default: return hipErrorInvalidValue;
-    }
-    return hipGetLastError();
+    // Few tiles are bound by latency, where twice the threads do half each:
+    // the planes of a 100-256-256-47 network's matrices 5.9 us against 8.7, of
+    // 1,024 x 4,096 (1,024 tiles) 12.2 against 14.7; of 4,096 x 4,096 39.6
+    // against 38.0, of six matrices of 1,024 x 1,024 to 4,096 49 against 41.
+    const bool few = (int64_t)gi * gj * b.n <= kSplitFew;
+    return few ? launch_split<2 * kThreads>(b, type, dim3(gj, gi, b.n), std::ldexp(1.0, e), s)
+               : launch_split<kThreads>(b, type, dim3(gj, gi, b.n), std::ldexp(1.0, e), s);
 }
 
 hipError_t launch_orth_whole(const OrthBatch &b, const OrthStep *st, int32_t steps, bool muon,

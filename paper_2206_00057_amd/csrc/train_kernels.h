@@ -38,7 +38,7 @@ constexpr int kOrthItems = 16;       // matrices of one launch
 constexpr int kOrthGrads = 192;      // gradients of one launch (arguments below 4 KB)
 constexpr int kOrthPad = 64;
 constexpr int kOrthSumBlocks = 1024;  // partial sums of |U|_F^2, at most
-constexpr int64_t kOrthSumRun = 4096;
+constexpr int64_t kOrthSumRun = 1024;
 
 struct OrthItem {
     int32_t rows, cols;              // of U and of the result
