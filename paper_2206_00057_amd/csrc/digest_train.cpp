@@ -189,14 +189,16 @@ digest_status plan_steps(int32_t steps, const float *coeffs, OrthStep *out)
         double q = std::max(poly(0), poly(l)), p = s * poly(l);
         if (c != 0 && -b / (2 * c) > 0 && -b / (2 * c) < l)
             q = std::max(q, poly(-b / (2 * c)));
-        // extrema of the odd polynomial: a + 3 b y + 5 c y^2 = 0
+        // extrema of the odd polynomial: a + 3 b y + 5 c y^2 = 0.  t is formed
+        // without a difference, so that neither root is lost as c vanishes
         const double disc = 9 * b * b - 20 * a * c;
         double y[2] = {-1, -1};
-        if (c != 0 && disc >= 0) {
-            y[0] = (-3 * b + std::sqrt(disc)) / (10 * c);
-            y[1] = (-3 * b - std::sqrt(disc)) / (10 * c);
-        } else if (c == 0 && b != 0) {
-            y[0] = -a / (3 * b);
+        if (disc >= 0) {
+            const double t = -0.5 * (3 * b + std::copysign(std::sqrt(disc), b));
+            if (c != 0)
+                y[0] = t / (5 * c);
+            if (t != 0)
+                y[1] = a / t;
         }
         for (double v : y)
             if (v > 0 && v < l)
