@@ -538,6 +538,7 @@ digest_status digest_orthogonalize(int32_t count, const int32_t *rows, const int
  *   n_grads  M, 1 .. 64, the same for every matrix.
  *   scales   HOST [count] (NULL: ones), e.g. sqrt(max(1, cols / rows)) for
  *            weights that map rows to cols.
+ *   lr, beta, decay, scales[i], 1 - lr decay and lr scales[i] finite.
  * A matrix with a gradient or momentum that is not finite becomes NaN.
  * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
  */

@@ -430,6 +430,16 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
         return fail(DIGEST_EINVAL, "need 1 <= n_grads <= 64, got %d", n_grads);
     if (!w || !momentum || !grads)
         return fail(DIGEST_EINVAL, "NULL w, momentum or grads");
+    // the weights and momenta are replaced: no factor may make them NaN
+    const float keep = 1.f - lr * decay;
+    if (!std::isfinite(lr) || !std::isfinite(beta) || !std::isfinite(decay) ||
+        !std::isfinite(keep))
+        return fail(DIGEST_EINVAL, "lr %g, beta %g, decay %g or 1 - lr decay is not finite",
+                    (double)lr, (double)beta, (double)decay);
+    for (int32_t i = 0; scales && i < count; ++i)
+        if (!std::isfinite(scales[i]) || !std::isfinite(lr * scales[i]))
+            return fail(DIGEST_EINVAL, "scale %g of matrix %d, or lr times it, is not finite",
+                        (double)scales[i], i);
     OrthStep plan[kMaxSteps];
     if (digest_status st = plan_steps(steps, coeffs, plan))
         return st;
@@ -499,7 +509,7 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
                 return st;
         }
         if (digest_status st =
-                run_steps(batch, plan, steps, true, DIGEST_F32, 1.f - lr * decay, base, s))
+                run_steps(batch, plan, steps, true, DIGEST_F32, keep, base, s))
             return st;
     }
     return DIGEST_OK;
