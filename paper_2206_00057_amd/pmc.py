@@ -38,11 +38,17 @@ import re
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
+# The sources of the profiled kernels and of their launches, with the headers
+# that they include.
+CSRC = os.path.join(ROOT, "paper_2206_00057_amd", "csrc")
+KERNEL_SOURCES = ("digest_kernels.hip", "device.h", "kernels.h", "digest_host.cpp", "status.h")
+
+
 def kernel_source_hash() -> str:
     """Hash of the sources that define the kernels and their launches."""
     h = hashlib.sha256()
-    for f in ("digest_kernels.hip", "kernels.h", "digest_host.cpp"):
-        with open(os.path.join(ROOT, "paper_2206_00057_amd", "csrc", f), "rb") as fh:
+    for f in KERNEL_SOURCES:
+        with open(os.path.join(CSRC, f), "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:16]
 
