@@ -1,7 +1,8 @@
 """The host code of the training operators (argument checks, coefficient bounds,
-workspace layout) under AddressSanitizer and UBSan, on the CPU: their ABI tests and a seeded fuzz of matrix lists and norm sizes run in a
-child process against the g++ sanitizer build.  Any report aborts the child.
-No kernel is launched."""
+workspace layout) under AddressSanitizer and UBSan, on the CPU: their ABI
+tests and a seeded fuzz of matrix lists and norm sizes run in a child process
+against the g++ sanitizer build.  Any report aborts the child.  No kernel is
+launched."""
 import os
 import subprocess
 import sys
