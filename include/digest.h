@@ -448,7 +448,8 @@ digest_status digest_sgd_average(float *w, const float *const *grads, int32_t n_
  * DIGEST_ACT_IDENTITY followed by this one with the layer's activation.
  *   n_rows   0 .. 2^31 - 2;  width 1 .. 65536.
  *   type     element type of x, y, dy and dx (DIGEST_F32, _BF16, _F16); the
- *            other arrays are fp32, and so is every sum.
+ *            other arrays are fp32, and so is every sum but the last of
+ *            dgain and dshift, over the workgroups, which has 64 bits.
  *   x, y, dy, dx  device arrays of rows, each with its row stride in
  *            elements (ldx, ldy, lddy, lddx: width .. 2^31 - 1); rows may
  *            start at any element, what lies between them is left alone.

@@ -6,9 +6,9 @@
 // the centred squares (two sums over registers, no cancellation), then the
 // outputs.  Bound by memory: 306,250 x 256 float32 with ReLU forward 122 us
 // (5.2 TB/s; a large copy here runs at 5.1), backward 229 us (5.5 TB/s),
-// 16,384 x 4,096 bfloat16 backward 85 us (4.8 TB/s).  Sums are fp32, in a fixed
-// order.  Rows may start at any element: global loads and stores take 16-byte
-// vectors at element alignment.
+// 16,384 x 4,096 bfloat16 backward 85 us (4.8 TB/s).  Sums are fp32 (over the
+// workgroups 64 bits), in a fixed order.  Rows may start at any element: global
+// loads and stores take 16-byte vectors at element alignment.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -284,10 +284,14 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
                 if constexpr (R > 1) {
                     sum[threadIdx.x] = v;
                     lds_barrier();
-                    v = 0.f;
+                    static_assert(R % 4 == 0, "four sums side by side");
+                    float a[4] = {0.f, 0.f, 0.f, 0.f};
                     if (threadIdx.x < L)
-                        for (int i = 0; i < R; ++i)
-                            v += sum[i * L + l];
+                        for (int i = 0; i < R; i += 4)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                a[j] += sum[(i + j) * L + l];
+                    v = (a[0] + a[1]) + (a[2] + a[3]);
                     lds_barrier();
                 }
                 if (threadIdx.x < L && at.in(e))
@@ -432,16 +436,18 @@ __global__ __launch_bounds__(kThreads) void k_norm_param_wide(
 
 // out[k][c] = sum over the blocks of part[block][k][c], in a fixed order: 64
 // columns a workgroup, its 16 waves each take every 16th block, then add up.
+// In 64 bits, at no cost; what is left of fp32's roundings are a lane's own rows
+// (n over those of a round: 75 of 306,250 x 256) and a workgroup's.
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
     const float *__restrict__ part, int32_t blocks, int32_t d, float *__restrict__ dgain,
     float *__restrict__ dshift)
 {
-    __shared__ float sum[kSumWaves][kWave];
+    __shared__ double sum[kSumWaves][kWave];
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
     const int64_t c = (int64_t)blockIdx.x * kWave + lane;
     const int64_t width = 2 * (int64_t)d;
-    float v = 0.f;
+    double v = 0;
     if (c < width) {
         constexpr int U = 16;   // in flight, added in order
         int b = w;
@@ -460,13 +466,13 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
     sum[w][lane] = v;
     lds_barrier();
     if (w == 0 && c < width) {
-        v = 0.f;
+        v = 0;
 #pragma unroll
         for (int i = 0; i < kSumWaves; ++i)
             v += sum[i][lane];
         float *out = c < d ? dgain : dshift;
         if (out)
-            out[c < d ? c : c - d] = v;
+            out[c < d ? c : c - d] = (float)v;
     }
 }
 

@@ -26,16 +26,15 @@ SIZES = [(9001, 256, "f32"), (70001, 64, "f32"), (140003, 47, "bf16"), (300001, 
          (530, 17001, "bf16")]
 
 
-def rounds(n, d, t):
-    """Rows of x that one lane adds up, and roundings behind them: the sums over
-    the workgroup's rows and over the workgroups."""
+def layout(n, d, t):
+    """Rows of x that one lane adds up, rows of a workgroup at a time, workgroups."""
     vec = 4 if t == "f32" else 8
     lanes = 2
     while lanes < 64 and lanes * vec < d:
         lanes *= 2
-    rows_at_once = 256 // lanes if d <= 1024 else 1
-    groups = min(-(-n // rows_at_once), 1024 if d <= 1024 else 512 if d <= 4096 else 256)
-    return -(-n // (groups * rows_at_once)), rows_at_once + -(-groups // 16) + 16
+    at_once = 256 // lanes if d <= 1024 else 1
+    groups = min(-(-n // at_once), 1024 if d <= 1024 else 512 if d <= 4096 else 256)
+    return -(-n // (groups * at_once)), at_once, groups
 
 
 @pytest.mark.parametrize("n,d,t", SIZES)
@@ -44,7 +43,7 @@ def test_every_row_counts_once(D, n, d, t):  # noqa: F811
     ints = lambda k: torch.randint(-k, k + 1, (n, d), generator=g, device="cuda").to(TYPES[t])
     x, dy, y = ints(3), ints(2), ints(1)
     stats = torch.tensor([0.0, 1.0], device="cuda").repeat(n, 1)
-    assert rounds(n, d, t)[0] > 1
+    assert layout(n, d, t)[0] > 1
     for relu in (False, True):
         up = dy.float() * (y > 0) if relu else dy.float()
         want = (up * x.float()).sum(0, dtype=torch.float64), up.sum(0, dtype=torch.float64)
@@ -64,11 +63,31 @@ def test_rounds_of_rows(D, n, d, t):  # noqa: F811
         dx, dgain, dshift = call_backward(D, x, gain, y, dy, stats, relu)
         check_backward(dx, None, None, x, gain, y, dy, stats, relu)
         _, rdg, rdb, up, _, xh, _ = backward64(x, gain, y, dy, stats, relu)
-        # x_hat is rounded twice, each row's product with the sum it joins
-        depth = sum(rounds(n, d, t))
+        # x_hat is rounded twice, each row's product with the sum it joins; then four
+        # sums side by side over the workgroup's rows, and the result once
+        own, at_once, _ = layout(n, d, t)
+        depth = own + (at_once // 4 + 1 if at_once > 1 else 0) + 1
         tol = (depth + 3) * U * (up * xh).abs().sum(0)
         assert bool(((dgain.double() - rdg).abs() <= tol).all())
         assert bool(((dshift.double() - rdb).abs() <= (depth + 1) * U * up.abs().sum(0)).all())
         again = call_backward(D, x, gain, y, dy, stats, relu)
         for a, b in zip(again, (dx, dgain, dshift)):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n,d,t", [(9001, 256, "f32"), (70001, 64, "f32"), (4099, 13, "f32"),
+                                   (1601, 2051, "f32"), (700, 5000, "f32"), (601, 9000, "f32")])
+def test_sums_over_the_workgroups_are_rounded_once(D, n, d, t):  # noqa: F811
+    """Integers again, a lane's sum and a workgroup's below 2^24, so exact in fp32,
+    but not their total: it comes out as the nearest fp32 number."""
+    own, at_once, _ = layout(n, d, t)
+    most = 2 ** 23 // (own * at_once)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    dy = torch.randint(most // 2, most, (n, d), generator=g, device="cuda").float()
+    x = torch.randint(0, 2, (n, d), generator=g, device="cuda").float()
+    stats = torch.tensor([0.0, 1.0], device="cuda").repeat(n, 1)
+    _, dgain, dshift = call_backward(D, x, None, None, dy, stats, False)
+    total = dy.double().sum(0)
+    assert float(total.max()) > 2 ** 25
+    assert torch.equal(dshift, total.float())
+    assert torch.equal(dgain, (dy.double() * x.double()).sum(0).float())
