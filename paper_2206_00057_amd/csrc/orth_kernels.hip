@@ -1216,7 +1216,12 @@ constexpr int kMinChunk = 4;   // lines of a part, at least (an even number each
 // the join takes 3.5 + 0.015 (128) or 4 + 0.045 (256) a part.  (1,024 x 4,096:
 // X X^T 35 us with 64, 20 and 6 with 128 in seven parts each; B X 48 and 32;
 // 256 x 256: 4.8 us with 32, 6.3 with 64, 11 to 13 with 128; 4,096 x 4,096:
-// B X 418 with 128, 348 with 256.)
+// B X 418 with 128, 348 with 256.)  Past those sizes the times are the same
+// lines carried on, and still choose: with the other tile of 128 and 256 for
+// either symmetric product, or for B X, five steps take 2.5 and 10% longer for
+// two 4,096 x 4,096 in one call (6,720 us), 2.7 and 7% for 5,120 x 5,120, 4.6
+// and 12% for 8,192 x 8,192 (25,340).  Where the two are close they can err: 128
+// for B X takes 1,285 us at 2,816 x 2,816, the 256 chosen 1,322.
 template <int MODE>
 OrthPlan plan_products(const OrthBatch &b)
 {

@@ -216,8 +216,9 @@ class DigestTrainer:
 
     def capture(self):
         """Record one HIP graph per pull/push pattern of the schedule.  The
-        warm-up and the captures run rounds, so they also train: the caller
-        restores W (and the store) afterwards if it needs a fixed start."""
+        warm-up runs rounds, so it also trains: the caller restores the
+        parameters (W, norms, attention), momenta and stores afterwards if it
+        needs a fixed start."""
         patterns = sorted({D.digest_sync_period(self.K, r) for r in range(1, 2 * self.K + 1)})
         side = torch.cuda.Stream()
         side.wait_stream(torch.cuda.current_stream())
