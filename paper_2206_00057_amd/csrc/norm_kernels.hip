@@ -215,7 +215,13 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_f
 
 // dx of each row, and the workgroup's partial sums of dgain and dshift: a
 // lane adds its columns over its rows in registers, the rows side by side in
-// the workgroup are added through LDS at the end.
+// the workgroup are added through LDS at the end.  Runs of kSumRows rows have
+// sums of their own, so that roundings grow as the root of a lane's runs, not
+// of its rows: over 306,250 x 256 float32 dgain is 0.9e-7 to 1.2e-7 off, one sum
+// 1.3e-7 to 1.9e-7, in the same time (232 us).  Not where one wave holds 16
+// elements a lane, whose registers they would pass: 29,125 x 602 bfloat16 takes 32
+// us, with them 42.
+constexpr int kSumRows = 16;
 template <class T, int GL, int WAVES, int E, Rest REST, bool PARAMS>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_backward(
     int32_t n, int32_t d, const T *__restrict__ x, int64_t ldx, const float *__restrict__ gain,
@@ -230,12 +236,19 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
     const int64_t step = (int64_t)gridDim.x * R;
     const Columns<T, E, REST> at{d, l, L};
     constexpr int N = at.N;
+    constexpr bool RUNS = PARAMS && !(WAVES == 1 && E == 16);
     float g[N], dg[PARAMS ? N : 1], db[PARAMS ? N : 1];
+    float dgs[RUNS ? N : 1], dbs[RUNS ? N : 1];   // of the whole runs
+    int run = 0;
     at.read(gain, 1.f, g);
     if constexpr (PARAMS)
 #pragma unroll
         for (int e = 0; e < N; ++e)
             dg[e] = db[e] = 0.f;
+    if constexpr (RUNS)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            dgs[e] = dbs[e] = 0.f;
     const float inv = 1.f / (float)d;
     for (int64_t r = (int64_t)blockIdx.x * R + threadIdx.x / L; r < n; r += step) {
         Row<T, E, REST> in, up, out;
@@ -270,7 +283,23 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
             }
             out.store(dx + r * lddx, at);
         }
+        if constexpr (RUNS)
+            if (++run == kSumRows) {   // uniform
+                run = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    dgs[e] += dg[e];
+                    dbs[e] += db[e];
+                    dg[e] = db[e] = 0.f;
+                }
+            }
     }
+    if constexpr (RUNS)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            dg[e] += dgs[e];
+            db[e] += dbs[e];
+        }
     if constexpr (PARAMS) {
         float *p = part + (int64_t)blockIdx.x * 2 * d;
         // the R rows of the workgroup, one column set a time
@@ -284,14 +313,10 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES *kWave) void k_norm_b
                 if constexpr (R > 1) {
                     sum[threadIdx.x] = v;
                     lds_barrier();
-                    static_assert(R % 4 == 0, "four sums side by side");
-                    float a[4] = {0.f, 0.f, 0.f, 0.f};
+                    v = 0.f;
                     if (threadIdx.x < L)
-                        for (int i = 0; i < R; i += 4)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                a[j] += sum[(i + j) * L + l];
-                    v = (a[0] + a[1]) + (a[2] + a[3]);
+                        for (int i = 0; i < R; ++i)
+                            v += sum[i * L + l];
                     lds_barrier();
                 }
                 if (threadIdx.x < L && at.in(e))
@@ -409,7 +434,8 @@ __global__ __launch_bounds__(kWideThreads) void k_norm_backward_wide(
 }
 
 // Partial sums of dgain and dshift of rows too wide for the registers of one
-// workgroup beside the sums: a thread per column, the workgroup's rows in order.
+// workgroup beside the sums: a thread per column, the workgroup's rows in order
+// (in runs, as above).
 template <class T>
 __global__ __launch_bounds__(kThreads) void k_norm_param_wide(
     int32_t n, int32_t d, int32_t rows, const T *__restrict__ x, int64_t ldx,
@@ -420,8 +446,13 @@ __global__ __launch_bounds__(kThreads) void k_norm_param_wide(
     if (c >= d)
         return;
     const int64_t r0 = (int64_t)blockIdx.y * rows, r1 = min((int64_t)n, r0 + rows);
-    float dg = 0.f, db = 0.f;
+    float dg = 0.f, db = 0.f, dgs = 0.f, dbs = 0.f;
     for (int64_t r = r0; r < r1; ++r) {
+        if ((r - r0) % kSumRows == 0) {
+            dgs += dg;
+            dbs += db;
+            dg = db = 0.f;
+        }
         const float2 st = *reinterpret_cast<const float2 *>(stats + 2 * r);
         float D = (float)dy[r * lddy + c];
         if (y && !((float)y[r * ldy + c] > 0.f))
@@ -430,14 +461,14 @@ __global__ __launch_bounds__(kThreads) void k_norm_param_wide(
         db += D;
     }
     float *p = part + (int64_t)blockIdx.y * 2 * d;
-    p[c] = dg;
-    p[d + c] = db;
+    p[c] = dgs + dg;
+    p[d + c] = dbs + db;
 }
 
 // out[k][c] = sum over the blocks of part[block][k][c], in a fixed order: 64
 // columns a workgroup, its 16 waves each take every 16th block, then add up.
-// In 64 bits, at no cost; what is left of fp32's roundings are a lane's own rows
-// (n over those of a round: 75 of 306,250 x 256) and a workgroup's.
+// In 64 bits (0.1 us of 2.0 to 5.6); what is left of fp32's roundings are a lane's
+// own rows and a workgroup's.
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
     const float *__restrict__ part, int32_t blocks, int32_t d, float *__restrict__ dgain,
@@ -447,9 +478,9 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
     const int lane = threadIdx.x % kWave, w = threadIdx.x / kWave;
     const int64_t c = (int64_t)blockIdx.x * kWave + lane;
     const int64_t width = 2 * (int64_t)d;
-    double v = 0;
+    double a[4] = {0, 0, 0, 0};   // (one sum would wait for each addition)
     if (c < width) {
-        constexpr int U = 16;   // in flight, added in order
+        constexpr int U = 16;   // in flight
         int b = w;
         for (; b + (U - 1) * kSumWaves < blocks; b += U * kSumWaves) {
             float x[U];
@@ -458,15 +489,15 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_norm_param_sum(
                 x[u] = part[(b + u * kSumWaves) * width + c];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                v += x[u];
+                a[u % 4] += x[u];
         }
         for (; b < blocks; b += kSumWaves)
-            v += part[b * width + c];
+            a[0] += part[b * width + c];
     }
-    sum[w][lane] = v;
+    sum[w][lane] = (a[0] + a[1]) + (a[2] + a[3]);
     lds_barrier();
     if (w == 0 && c < width) {
-        v = 0;
+        double v = 0;
 #pragma unroll
         for (int i = 0; i < kSumWaves; ++i)
             v += sum[i][lane];

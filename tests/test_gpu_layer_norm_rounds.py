@@ -24,6 +24,9 @@ SIZES = [(9001, 256, "f32"), (70001, 64, "f32"), (140003, 47, "bf16"), (300001, 
          (9001, 602, "bf16"), (5003, 1000, "f16"), (1601, 2051, "f32"), (1301, 4096, "bf16"),
          (700, 5000, "f32"), (700, 5003, "bf16"), (601, 9000, "f16"), (530, 16384, "f32"),
          (530, 17001, "bf16")]
+# past the 16 rounds after which a lane's sums are set aside, whole runs and not
+LONG = [(65536, 256, "f32"), (70001, 250, "f32"), (2300001, 5, "f32"), (1200001, 13, "bf16"),
+        (18001, 1030, "f16"), (4500, 4100, "f32"), (70001, 600, "bf16"), (8500, 9000, "f16")]
 
 
 def layout(n, d, t):
@@ -37,7 +40,7 @@ def layout(n, d, t):
     return -(-n // (groups * at_once)), at_once, groups
 
 
-@pytest.mark.parametrize("n,d,t", SIZES)
+@pytest.mark.parametrize("n,d,t", SIZES + LONG)
 def test_every_row_counts_once(D, n, d, t):  # noqa: F811
     g = torch.Generator(device="cuda").manual_seed(n + d)
     ints = lambda k: torch.randint(-k, k + 1, (n, d), generator=g, device="cuda").to(TYPES[t])
@@ -63,10 +66,10 @@ def test_rounds_of_rows(D, n, d, t):  # noqa: F811
         dx, dgain, dshift = call_backward(D, x, gain, y, dy, stats, relu)
         check_backward(dx, None, None, x, gain, y, dy, stats, relu)
         _, rdg, rdb, up, _, xh, _ = backward64(x, gain, y, dy, stats, relu)
-        # x_hat is rounded twice, each row's product with the sum it joins; then four
-        # sums side by side over the workgroup's rows, and the result once
+        # x_hat is rounded twice, each row's product with the sum it joins; then the
+        # sum over the workgroup's rows, and the result once
         own, at_once, _ = layout(n, d, t)
-        depth = own + (at_once // 4 + 1 if at_once > 1 else 0) + 1
+        depth = own + at_once + 1
         tol = (depth + 3) * U * (up * xh).abs().sum(0)
         assert bool(((dgain.double() - rdg).abs() <= tol).all())
         assert bool(((dshift.double() - rdb).abs() <= (depth + 1) * U * up.abs().sum(0)).all())
@@ -91,3 +94,20 @@ def test_sums_over_the_workgroups_are_rounded_once(D, n, d, t):  # noqa: F811
     assert float(total.max()) > 2 ** 25
     assert torch.equal(dshift, total.float())
     assert torch.equal(dgain, (dy.double() * x.double()).sum(0).float())
+
+
+@pytest.mark.parametrize("n,d,t", LONG)
+def test_long_sums(D, n, d, t):  # noqa: F811
+    """Equal rows, whose roundings do not cancel.  Of a lane's rows at most 16 are
+    added one after another, then its runs, then as in test_rounds_of_rows; one wave
+    with 16 elements a lane (513 to 1,024 wide) adds them in one sum."""
+    own, at_once, _ = layout(n, d, t)
+    g = torch.Generator().manual_seed(d)
+    row = lambda: (1.0 + torch.rand(d, generator=g)).to(TYPES[t]).cuda().expand(n, d).contiguous()
+    x, dy = row(), row()
+    stats = torch.tensor([0.0, 1.0], device="cuda").repeat(n, 1)
+    _, dgain, dshift = call_backward(D, x, None, None, dy, stats, False)
+    depth = own if 512 < d <= 1024 else min(own, 16) + own // 16
+    depth += at_once + 1
+    for got, want in ((dgain, dy[0].double() * x[0].double() * n), (dshift, dy[0].double() * n)):
+        assert bool(((got.double() - want).abs() <= (depth + 1) * U * want).all())
