@@ -551,6 +551,87 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
                                   size_t bytes, void *hip_stream);
 
 /*
+ * Rows held in 8 bits, a quarter of fp32's memory and traffic: the stale
+ * representations of a store, the inputs that a layer keeps for its backward,
+ * the operands of a product.  A row x of `width` elements is held as a scale
+ * and a whole number q_c of -127 .. 127 (its code) for each element:
+ *   scale = fp32(max_c |x_c| / 127),  q_c = the whole number nearest to the
+ *   exact x_c / scale (ties to even),  value of element c: q_c scale.
+ * A scale below the smallest normal number becomes 0 and its row zeros (rows
+ * of zeros among them).  A row with a NaN or an infinity gets the scale NaN
+ * and codes 0: it reads as NaN and touches no other row.
+ *   codes    device [n][ldq], 16-byte aligned, ldq a multiple of 16 of at
+ *            least DIGEST_Q8_STRIDE(width); the columns from width up to that
+ *            are written as zeros and must be zeros where codes are read by
+ *            the product, what lies behind them is left alone.
+ *   scales   device [n].
+ *   n_rows   0 .. 2^31 - 2;  widths 1 .. 65536.
+ *   type     element type of x, w, y and dy (DIGEST_F32, _BF16, _F16), which
+ *            are device arrays of rows with row strides in elements (ldx, ldw,
+ *            ldy, lddy: the width .. 2^31 - 1) and may start at any element.
+ *   rows     device [n_rows], the rows that are taken, in this order, out of
+ *            an array of n_x (n_codes) rows, each any number of times; NULL:
+ *            all in their order.  A number outside the array gives a row of
+ *            NaN.
+ * Outputs overlap nothing.  Equal calls give equal bits.  None of the calls
+ * belongs to a partition handle.
+ * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
+ */
+#define DIGEST_Q8_STRIDE(width) (((width) + 15) / 16 * 16)
+
+/* Row i of codes and scales from row rows[i] of x. */
+digest_status digest_quantize_rows(int64_t n_rows, int32_t width, int32_t type, const void *x,
+                                   int64_t ldx, const int64_t *rows, int64_t n_x, int8_t *codes,
+                                   int64_t ldq, float *scales, void *hip_stream);
+
+/* Row j of codes (n_cols rows of width n_rows) and scales from column j of the
+ * n_rows x n_cols matrix w: a weight matrix for digest_q8_product, with a
+ * scale for each output channel. */
+digest_status digest_quantize_columns(int32_t n_rows, int32_t n_cols, int32_t type, const void *w,
+                                      int64_t ldw, int8_t *codes, int64_t ldq, float *scales,
+                                      void *hip_stream);
+
+/* Row i of y = the values of row rows[i] of codes and scales, each rounded to
+ * fp32 and from there to the type. */
+digest_status digest_dequantize_rows(int64_t n_rows, int32_t width, const int8_t *codes,
+                                     int64_t ldq, const float *scales, const int64_t *rows,
+                                     int64_t n_codes, int32_t type, void *y, int64_t ldy,
+                                     void *hip_stream);
+
+/*
+ * The product of rows by a weight matrix, both in 8 bits:
+ *   y[r][j] = act(scales[r] w_scales[j] sum_c codes[r][c] w_codes[j][c])
+ *   codes    n_rows rows of width d_in;  w_codes  d_out rows of width d_in.
+ *   y        [n_rows, d_out] of `type`.  The sum is a whole number and exact;
+ *            it is rounded to fp32, multiplied by the smaller and by the
+ *            larger scale, and rounded to the type.
+ */
+digest_status digest_q8_product(int64_t n_rows, int32_t d_in, int32_t d_out, const int8_t *codes,
+                                int64_t ldq, const float *scales, const int8_t *w_codes,
+                                int64_t ldw, const float *w_scales, int32_t act, int32_t type,
+                                void *y, int64_t ldy, void *hip_stream);
+
+/*
+ * Weight gradient of a layer whose input rows were kept in 8 bits:
+ *   D = dy (identity) or dy 1[y > 0] (ReLU),
+ *   dw[c][j] = sum_r codes[r][c] (scales[r] D[r][j])      [d_in, d_out], fp32
+ * with scales[r] D rounded to fp32, exact products and fp32 sums in a fixed
+ * order.  y, the layer's output, is read with DIGEST_ACT_RELU only.  Without
+ * rows dw is zero.  An infinity or NaN in row r of D makes its column of dw
+ * NaN, a scale that is NaN all of dw.
+ *   workspace  256-byte aligned device memory of at least the queried bytes;
+ *            its contents need not be kept between calls, and calls that may
+ *            overlap need one each.
+ */
+digest_status digest_q8_weight_grad_query(int64_t n_rows, int32_t d_in, int32_t d_out,
+                                          size_t *workspace_bytes);
+digest_status digest_q8_weight_grad(int64_t n_rows, int32_t d_in, int32_t d_out,
+                                    const int8_t *codes, int64_t ldq, const float *scales,
+                                    int32_t type, const void *dy, int64_t lddy, int32_t act,
+                                    const void *y, int64_t ldy, float *dw, void *workspace,
+                                    size_t bytes, void *hip_stream);
+
+/*
  * Synchronisation schedule of Algorithm 1 (pure, host only): in round
  * iter (1-based) with interval K >= 1, *do_pull = (iter mod K == 0) and
  * *do_push = ((iter-1) mod K == 0); both apply to levels 1..L-1.

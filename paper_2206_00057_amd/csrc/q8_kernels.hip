@@ -1,0 +1,575 @@
+// gfx950 kernels of rows held in 8 bits: a scale and whole numbers of -127 to
+// 127 for each row.  Writing and reading such rows, the product of two sets of
+// them, and the weight gradient from kept ones.
+//
+// The scale is s = fl(a / 127) for the row's largest magnitude a, and the code
+// of x the whole number nearest to the exact quotient x / s (ties to even), so
+// that a row has one set of codes whatever computes them.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cfloat>
+
+#include "device.h"
+#include "q8_kernels.h"
+#include "train_kernels.h"
+
+namespace digest {
+namespace {
+
+constexpr int kThreads = 256;
+
+template <class T>
+constexpr int kVecOf = 16 / (int)sizeof(T);
+
+// A vector of N values of T, aligned to its elements only.
+template <class T, int N>
+struct Vec {
+    typedef T type __attribute__((ext_vector_type(N), aligned(sizeof(T))));
+};
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ int64_t row_number(const RowList &l, int64_t i)
+{
+    if (!l.p)
+        return i;
+    return l.wide ? ((const int64_t *)l.p)[i] : ((const int32_t *)l.p)[i];
+}
+
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// A row's scale and what its codes are formed with, from the bits of its
+// largest magnitude (a NaN's are above infinity's, that is above any number's).
+struct Scale {
+    float s, inv;
+    __device__ __forceinline__ explicit Scale(uint32_t top)
+    {
+        s = __uint_as_float(top) / 127.f;
+        // below the normal numbers the quotients have no reciprocal to start from
+        if (s < FLT_MIN)
+            s = 0.f;
+        inv = s > 0.f ? 1.f / s : 0.f;
+        if (top >= 0x7f800000u)
+            s = __uint_as_float(0x7fc00000u), inv = 0.f;
+    }
+};
+
+// The codes of the four values x as bytes.  x inv plus 1.5 * 2^23 has the
+// rounded quotient in its low byte; it is off by one at most, where the
+// quotient lies next to a half.  r = x - q s is exact there (a multiple of s's
+// last place below s), so that 2 |r| > s, or a tie at an odd q, tells.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[4], const Scale &sc)
+{
+    constexpr float kMagic = 12582912.f;
+    float u[4], r[4];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        u[i] = __builtin_fmaf(x[i], sc.inv, kMagic);
+        r[i] = __builtin_fmaf(-(u[i] - kMagic), sc.s, x[i]);
+        near |= __builtin_fabsf(r[i]) + __builtin_fabsf(r[i]) >= sc.s;
+    }
+    uint32_t b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        b[i] = __float_as_uint(u[i]);
+    if (near && sc.inv > 0.f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float twice = __builtin_fabsf(r[i]) + __builtin_fabsf(r[i]);
+            if (twice > sc.s || (twice == sc.s && (b[i] & 1)))
+                b[i] += r[i] > 0.f ? 1 : -1;
+        }
+    }
+    if (!(sc.inv > 0.f))
+        return 0;
+    return (b[0] & 255) | (b[1] & 255) << 8 | (b[2] & 255) << 16 | b[3] << 24;
+}
+
+// A row in the registers of GL lanes (WAVES == 1, 64 / GL rows a wave) or of
+// WAVES waves of one workgroup, Q vectors of 16 bytes a lane: one reading of x.
+template <class T, int GL, int Q, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quantize_rows(
+    int32_t n, int32_t d, const T *__restrict__ x, int64_t ldx, RowList src, int64_t n_x,
+    int8_t *__restrict__ codes, int64_t ldq, float *__restrict__ scales, RowList dst)
+{
+    constexpr int V = kVecOf<T>;
+    constexpr int L = WAVES == 1 ? GL : WAVES * kWave;   // lanes of a row
+    typedef typename Vec<T, V>::type vec;
+    const int lane = threadIdx.x % L;
+    const int64_t row = WAVES == 1 ? (int64_t)blockIdx.x * (kThreads / GL) + threadIdx.x / GL
+                                   : (int64_t)blockIdx.x;
+    const bool live = row < n;
+    const int64_t from = live ? row_number(src, row) : 0;
+    const bool there = live && from >= 0 && from < n_x;
+    const T *xr = x + (there ? from * ldx : 0);
+
+    vec v[Q];
+    uint32_t top = there ? 0 : 0x7fc00000u;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int c = (q * L + lane) * V;
+        if (there && c + V <= d) {
+            v[q] = *reinterpret_cast<const vec *>(xr + c);
+        } else {
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                v[q][j] = there && c + j < d ? xr[c + j] : (T)0.f;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+#pragma unroll
+        for (int j = 0; j < V; ++j)
+            top = max(top, magnitude((float)v[q][j]));
+#pragma unroll
+    for (int m = (WAVES == 1 ? GL : kWave) / 2; m > 0; m /= 2)
+        top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    if constexpr (WAVES > 1) {
+        __shared__ uint32_t red[WAVES];
+        if (lane % kWave == 0)
+            red[lane / kWave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w)
+            top = max(top, red[w]);
+    }
+    if (!live)
+        return;
+    const Scale sc(top);
+    const int64_t to = row_number(dst, row);
+    int8_t *out = codes + to * ldq;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        const int c = (q * L + lane) * V;
+        if (c >= q8_padded(d))
+            continue;
+        uint32_t w[V / 4];
+#pragma unroll
+        for (int j = 0; j < V / 4; ++j) {
+            const float f[4] = {(float)v[q][4 * j], (float)v[q][4 * j + 1],
+                                (float)v[q][4 * j + 2], (float)v[q][4 * j + 3]};
+            w[j] = codes4(f, sc);
+        }
+        if constexpr (V == 4)
+            *reinterpret_cast<uint32_t *>(out + c) = w[0];
+        else
+            *reinterpret_cast<uint2 *>(out + c) = make_uint2(w[0], w[1]);
+    }
+    if (lane == 0)
+        scales[to] = sc.s;
+}
+
+// Columns of w as rows of codes: a workgroup takes 16 columns, its 16 groups of
+// 16 lanes their rows in turn; one pass for the largest magnitudes, one for
+// the codes, which leave through LDS 16 rows (one 16-byte piece a column) at a
+// time.
+template <class T>
+__global__ __launch_bounds__(256) void k_quantize_columns(int32_t rows, int32_t cols,
+                                                          const T *__restrict__ w, int64_t ldw,
+                                                          int8_t *__restrict__ codes, int64_t ldq,
+                                                          float *__restrict__ scales)
+{
+    __shared__ uint32_t red[16][17];
+    const int c = threadIdx.x % 16, g = threadIdx.x / 16;
+    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    uint32_t top = 0;
+    if (col < cols)
+        for (int32_t r = g; r < rows; r += 16)
+            top = max(top, magnitude((float)w[(int64_t)r * ldw + col]));
+    red[g][c] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        top = max(top, red[i][c]);
+    if (col >= cols)
+        return;
+    const Scale sc(top);
+    if (g == 0)
+        scales[col] = sc.s;
+    for (int32_t r0 = g * 16; r0 < rows; r0 += 256) {
+        uint32_t p[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float f[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int32_t r = r0 + 4 * j + i;
+                f[i] = r < rows ? (float)w[(int64_t)r * ldw + col] : 0.f;
+            }
+            p[j] = codes4(f, sc);
+        }
+        *reinterpret_cast<uint4 *>(codes + col * ldq + r0) = make_uint4(p[0], p[1], p[2], p[3]);
+    }
+}
+
+// Lanes and vectors as in k_quantize_rows, rows wider than their L Q V columns
+// in several turns.
+template <class T, int GL, int Q>
+__global__ __launch_bounds__(kThreads) void k_dequantize_rows(
+    int32_t n, int32_t d, const int8_t *__restrict__ codes, int64_t ldq,
+    const float *__restrict__ scales, RowList src, int64_t n_x, T *__restrict__ y, int64_t ldy)
+{
+    constexpr int V = kVecOf<T>;
+    typedef typename Vec<T, V>::type vec;
+    const int lane = threadIdx.x % GL;
+    const int64_t row = (int64_t)blockIdx.x * (kThreads / GL) + threadIdx.x / GL;
+    if (row >= n)
+        return;
+    const int64_t from = row_number(src, row);
+    const bool there = from >= 0 && from < n_x;
+    const float s = there ? scales[from] : __uint_as_float(0x7fc00000u);
+    const int8_t *q8 = codes + (there ? from * ldq : 0);
+    T *yr = y + row * ldy;
+    for (int32_t c0 = 0; c0 < d; c0 += GL * Q * V) {
+        uint32_t w[Q][V / 4];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int c = c0 + (q * GL + lane) * V;
+            const bool in = there && c < d;
+            if constexpr (V == 4) {
+                w[q][0] = in ? *reinterpret_cast<const uint32_t *>(q8 + c) : 0;
+            } else {
+                const uint2 t = in ? *reinterpret_cast<const uint2 *>(q8 + c) : make_uint2(0, 0);
+                w[q][0] = t.x, w[q][1] = t.y;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            const int c = c0 + (q * GL + lane) * V;
+            vec out;
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                out[j] = (T)((float)(int8_t)(w[q][j / 4] >> (8 * (j % 4))) * s);
+            if (c + V <= d) {
+                *reinterpret_cast<vec *>(yr + c) = out;
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (c + j < d)
+                        yr[c + j] = out[j];
+            }
+        }
+    }
+}
+
+// An element of the product from its exact sum.  The smaller scale first: a
+// whole number times it is at least the smallest normal number, so that
+// nothing is lost on the way to a result that can be held.
+__device__ __forceinline__ float scaled(int sum, float s, float t)
+{
+    const bool less = s < t;
+    return (float)sum * (less ? s : t) * (less ? t : s);
+}
+
+// ReLU that keeps a NaN.
+__device__ __forceinline__ float relu_of(float v, bool relu) { return relu && v <= 0.f ? 0.f : v; }
+
+// 64 rows x 64 channels a workgroup, 32 x 32 a wave, straight from memory.  The
+// channels are the instruction's rows, so that a lane holds four channels in
+// a row of one output row.  The sums are whole numbers below 2^31 (k <= 65536),
+// exact in any order.
+template <class T>
+__global__ __launch_bounds__(256) void k_q8_product(int32_t n, int32_t m, int32_t k,
+                                                    const int8_t *__restrict__ q, int64_t ldq,
+                                                    const float *__restrict__ s,
+                                                    const int8_t *__restrict__ p, int64_t ldp,
+                                                    const float *__restrict__ t, bool relu,
+                                                    T *__restrict__ y, int64_t ldy)
+{
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t r0 = (int64_t)blockIdx.x * 64 + wave / 2 * 32;
+    const int64_t j0 = (int64_t)blockIdx.y * 64 + wave % 2 * 32;
+    const int l = lane % 16, g = lane / 16;
+    i32x4 acc[2][2] = {};
+    for (int32_t c0 = 0; c0 < k; c0 += 64) {
+        const int32_t c = c0 + g * 16;
+        i32x4 a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int64_t j = j0 + 16 * i + l, r = r0 + 16 * i + l;
+            const i32x4 zero = {0, 0, 0, 0};
+            a[i] = j < m && c < k ? *reinterpret_cast<const i32x4 *>(p + j * ldp + c) : zero;
+            b[i] = r < n && c < k ? *reinterpret_cast<const i32x4 *>(q + r * ldq + c) : zero;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                acc[i][h] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[h], acc[i][h], 0, 0, 0);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t r = r0 + 16 * h + l;
+        if (r >= n)
+            continue;
+        const float sr = s[r];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t j = j0 + 16 * i + g * 4 + e;
+                if (j < m)
+                    y[r * ldy + j] = (T)relu_of(scaled(acc[i][h][e], sr, t[j]), relu);
+            }
+    }
+}
+
+// dw over rows [z chunk, (z + 1) chunk) into slice z: 64 columns of codes x 64
+// of D a workgroup, 32 x 32 a wave, 32 rows a step through LDS.  The codes are
+// exact in bfloat16; s D is split into three bfloat16 by cutting off its low
+// bits, which together are exactly its 24 bits, so that the products are
+// exact and the sums fp32.
+constexpr int kGradRows = 32;
+template <class T>
+__global__ __launch_bounds__(256) void k_q8_grad(int32_t n, int32_t k, int32_t m, int64_t chunk,
+                                                 const int8_t *__restrict__ q, int64_t ldq,
+                                                 const float *__restrict__ s,
+                                                 const T *__restrict__ dy, int64_t lddy,
+                                                 const T *__restrict__ y, int64_t ldy,
+                                                 float *__restrict__ part)
+{
+    __shared__ bf16x8 lq[4][64], ld[3][4][64];   // [rows / 8][column]
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t c0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
+    const int64_t rb = blockIdx.z * chunk, re = min((int64_t)n, rb + chunk);
+    const int64_t c = c0 + lane, j = j0 + lane;
+    f32x4 acc[2][2] = {};
+    for (int64_t r0 = rb; r0 < re; r0 += kGradRows) {
+        bf16x8 vq, vd[3];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t r = r0 + wave * 8 + i;
+            float code = 0.f, D = 0.f;
+            if (r < re && c < k)
+                code = (float)q[r * ldq + c];
+            if (r < re && j < m) {
+                D = (float)dy[r * lddy + j];
+                if (y && !((float)y[r * ldy + j] > 0.f))
+                    D = 0.f;
+                D *= s[r];
+            }
+            vq[i] = (__bf16)code;
+#pragma unroll
+            for (int h = 0; h < 3; ++h) {
+                const float top = __uint_as_float(__float_as_uint(D) & 0xffff0000u);
+                vd[h][i] = (__bf16)top;
+                D -= top;
+            }
+        }
+        __syncthreads();
+        lq[wave][lane] = vq;
+#pragma unroll
+        for (int h = 0; h < 3; ++h)
+            ld[h][wave][lane] = vd[h];
+        __syncthreads();
+        const int l = lane % 16, g = lane / 16;
+        bf16x8 b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            b[i] = lq[g][wave / 2 * 32 + 16 * i + l];
+#pragma unroll
+        for (int h = 2; h >= 0; --h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bf16x8 a = ld[h][g][wave % 2 * 32 + 16 * i + l];
+#pragma unroll
+                for (int o = 0; o < 2; ++o)
+                    acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[o], acc[i][o], 0, 0,
+                                                                        0);
+            }
+    }
+    float *out = part + (int64_t)blockIdx.z * k * m;
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int64_t cc = c0 + wave / 2 * 32 + 16 * o + lane % 16;
+                const int64_t jj = j0 + wave % 2 * 32 + 16 * i + lane / 16 * 4 + e;
+                if (cc < k && jj < m)
+                    out[cc * m + jj] = acc[i][o][e];
+            }
+}
+
+// dw = the sum of the slices, in their order.
+__global__ __launch_bounds__(256) void k_q8_grad_sum(const float *__restrict__ part,
+                                                     int32_t splits, int64_t count,
+                                                     float *__restrict__ dw)
+{
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= count)
+        return;
+    float v = 0.f;
+    for (int32_t z = 0; z < splits; ++z)
+        v += part[z * count + e];
+    dw[e] = v;
+}
+
+template <class T>
+struct Tag {
+    typedef T type;
+};
+
+template <class F>
+hipError_t with_type(int32_t type, F f)
+{
+    if (type == kF32)
+        return f(Tag<float>{});
+    if (type == kBF16)
+        return f(Tag<__bf16>{});
+    return f(Tag<_Float16>{});
+}
+
+// Launches over rows [r0, r0 + n), at most kTurn at a time: a grid's threads are
+// counted in 32 bits.
+constexpr int32_t kTurn = 1 << 21;
+template <class F>
+hipError_t in_turns(int32_t n, F f)
+{
+    for (int64_t r0 = 0; r0 < n; r0 += kTurn)
+        if (hipError_t e = f((int64_t)r0, (int32_t)std::min<int64_t>(kTurn, n - r0)))
+            return e;
+    return hipSuccess;
+}
+
+RowList from(RowList l, int64_t r0)
+{
+    if (l.p)
+        l.p = (const char *)l.p + r0 * (l.wide ? 8 : 4);
+    return l;
+}
+
+template <class T, int GL, int Q, int WAVES>
+hipError_t quantize(int32_t n, int32_t d, const T *x, int64_t ldx, RowList src, int64_t n_x,
+                    int8_t *codes, int64_t ldq, float *scales, RowList dst, hipStream_t s)
+{
+    const int rows = WAVES == 1 ? kThreads / GL : 1;
+    const uint32_t blocks = (uint32_t)(((int64_t)n + rows - 1) / rows);
+    k_quantize_rows<T, GL, Q, WAVES>
+        <<<blocks, WAVES == 1 ? kThreads : WAVES * kWave, 0, s>>>(n, d, x, ldx, src, n_x, codes,
+                                                                  ldq, scales, dst);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize_rows(int32_t type, int32_t n, int32_t d, const void *x, int64_t ldx,
+                                RowList src, int64_t n_x, int8_t *codes, int64_t ldq,
+                                float *scales, RowList dst, hipStream_t s)
+{
+    return in_turns(n, [&](int64_t r0, int32_t n) { return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        const int vectors = (q8_padded(d) + kVecOf<T> - 1) / kVecOf<T>;
+        auto run = [&](auto f) {
+            return f(n, d, (const T *)x + (src.p ? 0 : r0 * ldx), ldx, from(src, r0),
+                     src.p ? n_x : n, codes + (dst.p ? 0 : r0 * ldq), ldq,
+                     scales + (dst.p ? 0 : r0), from(dst, r0), s);
+        };
+        if (vectors <= 8)
+            return run(quantize<T, 4, 2, 1>);
+        if (vectors <= 16)
+            return run(quantize<T, 4, 4, 1>);
+        if (vectors <= 32)
+            return run(quantize<T, 8, 4, 1>);
+        if (vectors <= 64)
+            return run(quantize<T, 16, 4, 1>);
+        if (vectors <= 128)
+            return run(quantize<T, 32, 4, 1>);
+        if (vectors <= 256)
+            return run(quantize<T, 64, 4, 1>);
+        if (vectors <= 1024)
+            return run(quantize<T, 64, 4, 4>);
+        if (vectors <= 4096)
+            return run(quantize<T, 64, 4, 16>);
+        return run(quantize<T, 64, 16, 16>);
+    }); });
+}
+
+hipError_t launch_quantize_columns(int32_t type, int32_t rows, int32_t cols, const void *w,
+                                   int64_t ldw, int8_t *codes, int64_t ldq, float *scales,
+                                   hipStream_t s)
+{
+    return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        k_quantize_columns<T><<<(cols + 15) / 16, 256, 0, s>>>(rows, cols, (const T *)w, ldw,
+                                                               codes, ldq, scales);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_dequantize_rows(int32_t type, int32_t n, int32_t d, const int8_t *codes,
+                                  int64_t ldq, const float *scales, RowList src, int64_t n_x,
+                                  void *y, int64_t ldy, hipStream_t s)
+{
+    return in_turns(n, [&](int64_t r0, int32_t n) { return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        const int vectors = (d + kVecOf<T> - 1) / kVecOf<T>;
+        auto run = [&](auto gl) {
+            constexpr int GL = decltype(gl)::value;
+            const int rows = kThreads / GL;
+            k_dequantize_rows<T, GL, 4>
+                <<<(uint32_t)(((int64_t)n + rows - 1) / rows), kThreads, 0, s>>>(
+                    n, d, codes + (src.p ? 0 : r0 * ldq), ldq, scales + (src.p ? 0 : r0),
+                    from(src, r0), src.p ? n_x : n, (T *)y + r0 * ldy, ldy);
+            return hipGetLastError();
+        };
+        if (vectors <= 16)
+            return run(std::integral_constant<int, 4>{});
+        if (vectors <= 32)
+            return run(std::integral_constant<int, 8>{});
+        if (vectors <= 64)
+            return run(std::integral_constant<int, 16>{});
+        if (vectors <= 128)
+            return run(std::integral_constant<int, 32>{});
+        return run(std::integral_constant<int, 64>{});
+    }); });
+}
+
+hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, const int8_t *q,
+                             int64_t ldq, const float *s, const int8_t *p, int64_t ldp,
+                             const float *t, bool relu, void *y, int64_t ldy, hipStream_t st)
+{
+    return in_turns(n, [&](int64_t r0, int32_t n) { return with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        const dim3 grid((uint32_t)(((int64_t)n + 63) / 64), (uint32_t)((m + 63) / 64));
+        k_q8_product<T><<<grid, 256, 0, st>>>(n, m, k, q + r0 * ldq, ldq, s + r0, p, ldp, t, relu,
+                                              (T *)y + r0 * ldy, ldy);
+        return hipGetLastError();
+    }); });
+}
+
+int32_t q8_grad_splits(int32_t n, int32_t k, int32_t m)
+{
+    const int64_t tiles = (int64_t)((k + 63) / 64) * ((m + 63) / 64);
+    const int64_t want = (1024 + tiles - 1) / tiles;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (int64_t)n / 128, 256}));
+}
+
+hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
+                                 int64_t ldq, const float *s, const void *dy, int64_t lddy,
+                                 const void *y, int64_t ldy, float *part, float *dw,
+                                 hipStream_t st)
+{
+    const int32_t splits = q8_grad_splits(n, k, m);
+    int64_t chunk = ((int64_t)n + splits - 1) / splits;
+    chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
+    const hipError_t e = with_type(type, [&](auto tag) {
+        typedef typename decltype(tag)::type T;
+        const dim3 grid((k + 63) / 64, (m + 63) / 64, splits);
+        k_q8_grad<T><<<grid, 256, 0, st>>>(n, k, m, chunk, q, ldq, s, (const T *)dy, lddy,
+                                           (const T *)y, ldy, splits > 1 ? part : dw);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess || splits <= 1)
+        return e;
+    const int64_t count = (int64_t)k * m;
+    k_q8_grad_sum<<<(uint32_t)((count + 255) / 256), 256, 0, st>>>(part, splits, count, dw);
+    return hipGetLastError();
+}
+
+}  // namespace digest

@@ -720,3 +720,148 @@ def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0,
         float(beta), float(decay),
         (ctypes.c_float * n)(*[float(v) for v in scales]) if scales is not None else None,
         int(bool(nesterov)), int(steps), _coeffs(coeffs, steps), work, nbytes, _stream(stream)))
+
+
+# Rows held in 8 bits.
+
+_q8 = None
+
+
+def _q8_lib():
+    """The library with the calls on rows held in 8 bits; raises if this build
+    of the ABI lacks them."""
+    global _q8
+    if _q8 is None or _q8 is not lib():
+        L = lib()
+        P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
+        sig = {
+            "digest_quantize_rows": [i64, i32, i32, P, i64, P, i64, P, i64, P, P],
+            "digest_quantize_columns": [i32, i32, i32, P, i64, P, i64, P, P],
+            "digest_dequantize_rows": [i64, i32, P, i64, P, P, i64, i32, P, i64, P],
+            "digest_q8_product": [i64, i32, i32, P, i64, P, P, i64, P, i32, i32, P, i64, P],
+            "digest_q8_weight_grad_query": [i64, i32, i32, P],
+            "digest_q8_weight_grad": [i64, i32, i32, P, i64, P, i32, P, i64, i32, P, i64, P, P, sz,
+                                      P],
+        }
+        for name, args in sig.items():
+            f = getattr(L, name)
+            f.argtypes = args
+            f.restype = ctypes.c_int
+        _q8 = L
+    return _q8
+
+
+def digest_q8_stride(width):
+    """Row stride of the codes of rows of `width` elements (DIGEST_Q8_STRIDE)."""
+    return (int(width) + 15) // 16 * 16
+
+
+def _codes(t, scales, n, width, dev, name, scales_name):
+    """(pointer, row stride, pointer of the scales) of the codes [n,
+    digest_q8_stride(width)] and scales [n] of n rows."""
+    import torch
+    return (*_rows(t, (n, digest_q8_stride(width)), torch.int8, dev, name),
+            _need(_floats(scales, n, dev, scales_name), scales_name))
+
+
+def _need(p, name):
+    if p is None:
+        raise ValueError(f"{name} is required")
+    return p
+
+
+def _list(rows, n, dev):
+    """Pointer of n row numbers (int64), None for None."""
+    import torch
+    if rows is None:
+        return None
+    _here(rows, dev, "rows")
+    if rows.dtype != torch.int64:
+        raise TypeError(f"rows must be torch.int64, got {rows.dtype}")
+    if rows.dim() != 1 or not rows.is_contiguous() or rows.numel() != n:
+        raise ValueError(f"rows must be {n} contiguous numbers")
+    return rows.data_ptr()
+
+
+def digest_quantize_rows(x, codes, scales, rows=None, stream=None):
+    """codes, scales = the rows of x [m, d] (those that rows, int64, lists, in
+    its order) held in 8 bits: codes int8 [n, digest_q8_stride(d)], scales
+    float32 [n]."""
+    dev = _device()
+    shape, dtype = _matrix(x, dev, "x")
+    m, d = shape
+    n = m if rows is None else rows.numel()
+    px, ldx = _rows(x, shape, dtype, dev, "x")
+    pq, ldq, ps = _codes(codes, scales, n, d, dev, "codes", "scales")
+    _check(_q8_lib().digest_quantize_rows(n, d, _TYPES[dtype], px, ldx, _list(rows, n, dev), m, pq,
+                                          ldq, ps, _stream(stream)))
+
+
+def digest_quantize_columns(w, codes, scales, stream=None):
+    """codes, scales = the columns of w [k, m] held in 8 bits: codes int8 [m,
+    digest_q8_stride(k)], scales float32 [m]."""
+    dev = _device()
+    shape, dtype = _matrix(w, dev, "w")
+    k, m = shape
+    pw, ldw = _rows(w, shape, dtype, dev, "w")
+    pq, ldq, ps = _codes(codes, scales, m, k, dev, "codes", "scales")
+    _check(_q8_lib().digest_quantize_columns(k, m, _TYPES[dtype], pw, ldw, pq, ldq, ps,
+                                             _stream(stream)))
+
+
+def digest_dequantize_rows(codes, scales, y, rows=None, stream=None):
+    """y [n, d] = the values of the rows (those that rows, int64, lists, in its
+    order) that codes [m, digest_q8_stride(d)] and scales [m] hold."""
+    dev = _device()
+    shape, dtype = _matrix(y, dev, "y")
+    n, d = shape
+    m = n if rows is None else codes.shape[0]
+    pq, ldq, ps = _codes(codes, scales, m, d, dev, "codes", "scales")
+    py, ldy = _rows(y, shape, dtype, dev, "y")
+    _check(_q8_lib().digest_dequantize_rows(n, d, pq, ldq, ps, _list(rows, n, dev), m,
+                                            _TYPES[dtype], py, ldy, _stream(stream)))
+
+
+def digest_q8_product(codes, scales, w_codes, w_scales, y, act=ACT_IDENTITY, stream=None):
+    """y [n, d_out] = act(the product of the rows in 8 bits (codes [n, k], scales
+    [n]) by the weight matrix whose columns w_codes [d_out, k], w_scales [d_out]
+    hold)."""
+    dev = _device()
+    shape, dtype = _matrix(y, dev, "y")
+    n, m = shape
+    k = codes.shape[-1]
+    pq, ldq, ps = _codes(codes, scales, n, k, dev, "codes", "scales")
+    pw, ldw, pt = _codes(w_codes, w_scales, m, k, dev, "w_codes", "w_scales")
+    py, ldy = _rows(y, shape, dtype, dev, "y")
+    _check(_q8_lib().digest_q8_product(n, k, m, pq, ldq, ps, pw, ldw, pt, act, _TYPES[dtype], py,
+                                       ldy, _stream(stream)))
+
+
+def digest_q8_weight_grad_query(n_rows, d_in, d_out):
+    """Bytes of the workspace of digest_q8_weight_grad."""
+    out = ctypes.c_size_t(0)
+    _check(_q8_lib().digest_q8_weight_grad_query(int(n_rows), int(d_in), int(d_out),
+                                                 ctypes.byref(out)))
+    return int(out.value)
+
+
+def digest_q8_weight_grad(codes, scales, dy, dw, workspace, act=ACT_IDENTITY, y=None, stream=None):
+    """dw [d_in, d_out], float32 = the transpose of the rows that codes [n,
+    digest_q8_stride(d_in)] and scales [n] hold, times dy [n, d_out], with
+    ACT_RELU masked by y > 0; workspace: a CUDA tensor of at least
+    digest_q8_weight_grad_query(n, d_in, d_out) bytes."""
+    dev = _device()
+    shape, dtype = _matrix(dy, dev, "dy")
+    n, m = shape
+    if getattr(dw, "ndim", 0) != 2 or dw.shape[1] != m:
+        raise ValueError(f"dw must be [d_in, {m}]")
+    k = dw.shape[0]
+    pq, ldq, ps = _codes(codes, scales, n, k, dev, "codes", "scales")
+    pdy, lddy = _rows(dy, shape, dtype, dev, "dy")
+    if act == ACT_RELU and y is None:
+        raise ValueError("y is required with ACT_RELU")
+    py, ldy = _rows(y, shape, dtype, dev, "y") if act == ACT_RELU else (None, 0)
+    ws, nbytes = _workspace(workspace, dev)
+    _check(_q8_lib().digest_q8_weight_grad(n, k, m, pq, ldq, ps, _TYPES[dtype], pdy, lddy, act,
+                                           py, ldy, _floats(dw, k * m, dev, "dw"), ws, nbytes,
+                                           _stream(stream)))

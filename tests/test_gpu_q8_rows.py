@@ -1,0 +1,430 @@
+"""Rows held in 8 bits on the GPU: written, read back, multiplied and summed
+into a weight gradient, against plain forms in 64 bits.
+
+Codes and scales are equal to the definition's bit for bit.  Bounds of the
+others, with u = 2^-24 and h half a step of the type:
+  read back     one product in fp32, one rounding to the type: u + h
+  product       the sum is exact; its rounding to fp32, two products, one
+                rounding to the type: 3 u + h of the value
+  weight grad   s D rounded once (u of each term), then n terms of exact
+                products summed in fp32 over three parts each: an element is
+                off by at most 2 (n + 2) u times the sum of its terms' magnitudes
+                (a sum that cuts off instead of rounding takes twice u a term)
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2206_00057_amd import digest as D
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.bfloat16, torch.float16]
+U = 2.0 ** -24
+ACTS = [D.ACT_IDENTITY, D.ACT_RELU]
+
+
+def half(t):
+    return 0.0 if t == torch.float32 else torch.finfo(t).eps / 2
+
+
+def held(x):
+    """(codes as int64, scales as float32) of the rows of x, numpy in 64 bits."""
+    v = x.detach().cpu().double().numpy()
+    with np.errstate(all="ignore"):
+        s = (np.abs(v).max(1) / 127).astype(np.float32)
+        s[s < np.finfo(np.float32).tiny] = 0
+        q = np.rint(v / s[:, None].astype(np.float64))
+        bad = ~np.isfinite(v).all(1)
+    s[bad] = np.nan
+    q[(s == 0) | bad] = 0
+    return q.astype(np.int64), s
+
+
+def quantize(x, rows=None, pad=0):
+    n = x.shape[0] if rows is None else rows.numel()
+    ld = D.digest_q8_stride(x.shape[1])
+    whole = torch.full((n, ld + pad), 77, dtype=torch.int8, device="cuda")
+    codes, scales = whole[:, :ld], torch.full((n,), 5.0, device="cuda")
+    D.digest_quantize_rows(x, codes, scales, rows=rows)
+    if pad:
+        assert bool((whole[:, ld:] == 77).all())
+    return codes, scales
+
+
+def check_codes(codes, scales, q, s, d):
+    c = codes.cpu().numpy().astype(np.int64)
+    np.testing.assert_array_equal(scales.cpu().numpy(), s)
+    np.testing.assert_array_equal(c[:, :d], q)
+    assert not c[:, d:].any()
+
+
+def strided(n, d, t, gap, shift, make):
+    """An [n, d] view with a row stride of d + gap, starting `shift` elements in."""
+    base = torch.zeros(n * (d + gap) + shift + 8, dtype=t, device="cuda")
+    v = base[shift:shift + n * (d + gap)].view(n, d + gap)[:, :d]
+    v.copy_(make)
+    return v
+
+
+WIDTHS = [1, 3, 15, 16, 17, 31, 33, 47, 64, 65, 100, 129, 256, 257, 511, 513, 602, 1024, 1025, 2049,
+          4097, 8193, 16385, 40000, 65535, 65536]
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("d", WIDTHS)
+def test_rows(d, t):
+    g = torch.Generator(device="cuda").manual_seed(d)
+    n = 37 if d < 4000 else 5
+    x = torch.randn(n, d, generator=g, device="cuda") * torch.exp(
+        torch.randn(n, 1, generator=g, device="cuda"))
+    x = strided(n, d, t, 3, 1, x)
+    x[1] = 0
+    q, s = held(x)
+    codes, scales = quantize(x, pad=16)
+    check_codes(codes, scales, q, s, d)
+    # back, in an order with repeats and rows outside
+    idx = torch.tensor([n - 1, 0, 0, 2, -1, n, 1, 2 ** 40], device="cuda")
+    y = strided(8, d, t, 5, 3, torch.full((8, d), 9.0, device="cuda"))
+    D.digest_dequantize_rows(codes, scales, y, rows=idx)
+    got = y.cpu().double().numpy()
+    for i, r in enumerate(idx.tolist()):
+        if not 0 <= r < n:
+            assert np.isnan(got[i]).all()
+            continue
+        want = q[r] * s[r].astype(np.float64)
+        tiny = 2.0 ** -25 if t == torch.float16 else 0.0
+        assert (np.abs(got[i] - want) <= (U + half(t)) * 1.001 * np.abs(want) + tiny).all(), (i, r)
+
+
+def test_rows_behind_are_left():
+    x = torch.randn(6, 40, device="cuda")
+    codes = torch.full((9, 48), 3, dtype=torch.int8, device="cuda")
+    scales = torch.full((9,), 2.0, device="cuda")
+    D.digest_quantize_rows(x, codes[:6], scales[:6])
+    assert bool((codes[6:] == 3).all()) and bool((scales[6:] == 2).all())
+    y = torch.full((4, 50), 8.0, device="cuda")
+    D.digest_dequantize_rows(codes[:3], scales[:3], y[:3, :40])
+    assert bool((y[3] == 8).all()) and bool((y[:, 40:] == 8).all())
+
+
+def test_borders():
+    """Values on and next to the halves between two codes, for scales that are no
+    powers of two, and ties at scale 1."""
+    rng = np.random.default_rng(0)
+    rows = []
+    for i in range(200):
+        a = np.float32(np.exp(rng.uniform(-60, 60)))
+        s = np.float32(a / np.float32(127))
+        k = rng.integers(-127, 127, 100)
+        mid = ((k + 0.5) * s.astype(np.float64)).astype(np.float32)
+        x = np.concatenate([[a], mid, np.nextafter(mid, np.float32(np.inf)),
+                            np.nextafter(mid, np.float32(-np.inf))])
+        rows.append(np.clip(x, -a, a))
+    rows.append(np.concatenate([[127.0], np.tile(np.arange(-127, 127) + 0.5, 2)[:300]]))
+    x = torch.tensor(np.stack(rows).astype(np.float32), device="cuda")
+    check_codes(*quantize(x), *held(x), x.shape[1])
+
+
+def test_extremes():
+    big, tiny = 3.4028234663852886e38, 2.0 ** -149
+    x = torch.zeros(12, 20, device="cuda")
+    x[0, 3], x[0, 4] = float("nan"), 1.0
+    x[1, 19] = float("inf")
+    x[2, 0] = float("-inf")
+    x[3] = big
+    x[4, 7] = tiny                       # no scale: zeros
+    x[5, 7] = 127 * 2.0 ** -126          # the smallest scale
+    x[5, 8] = 64 * 2.0 ** -126
+    x[6, 7] = np.nextafter(np.float32(127 * 2.0 ** -126), np.float32(0)).item()
+    x[7] = -0.0
+    x[8] = torch.linspace(-1, 1, 20)
+    x[9, 0], x[9, 1] = 1.0, tiny
+    x[10] = -big
+    q, s = held(x)
+    codes, scales = quantize(x)
+    check_codes(codes, scales, q, s, 20)
+    y = torch.empty_like(x)
+    D.digest_dequantize_rows(codes, scales, y)
+    bad = torch.tensor([0, 1, 2], device="cuda")
+    assert bool(torch.isnan(y[bad]).all()) and bool(torch.isfinite(y[4:10]).all())
+    # fp16's largest and smallest numbers
+    h = torch.zeros(3, 9, dtype=torch.float16, device="cuda")
+    h[0], h[1, 2], h[2, 2] = 65504.0, 2.0 ** -24, float("inf")
+    check_codes(*quantize(h), *held(h), 9)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("k,m", [(1, 1), (15, 3), (16, 16), (17, 33), (64, 47), (100, 256),
+                                 (255, 17), (257, 70), (602, 256), (1025, 41), (4099, 19)])
+def test_columns(k, m, t):
+    g = torch.Generator(device="cuda").manual_seed(k)
+    w = strided(k, m, t, 2, 1, torch.randn(k, m, generator=g, device="cuda"))
+    w[:, m // 2] *= 50
+    if m > 2:
+        w[k // 2, 0] = float("nan")
+        w[:, 1] = 0
+    codes = torch.full((m, D.digest_q8_stride(k)), 77, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(m, device="cuda")
+    D.digest_quantize_columns(w, codes, scales)
+    check_codes(codes, scales, *held(w.t()), k)
+
+
+def random_codes(n, d, g, gap=0):
+    """Codes [n, padded d] with a row stride of 16 gap more, and scales."""
+    ld = D.digest_q8_stride(d)
+    whole = torch.full((n, ld + 16 * gap), 99, dtype=torch.int8, device="cuda")
+    codes = whole[:, :ld]
+    codes.zero_()
+    codes[:, :d] = torch.randint(-127, 128, (n, d), generator=g, device="cuda").to(torch.int8)
+    return codes, torch.exp(torch.randn(n, generator=g, device="cuda")) * 1e-2
+
+
+def check_product(n, k, m, t, act, gap=0):
+    g = torch.Generator(device="cuda").manual_seed(n * 7 + k * 3 + m)
+    q, s = random_codes(n, k, g, gap)
+    p, w = random_codes(m, k, g, gap)
+    y = strided(n, m, t, gap, gap, torch.full((n, m), 3.0, device="cuda"))
+    D.digest_q8_product(q, s, p, w, y, act)
+    sums = torch.mm(q.cpu().double(), p.cpu().double().t())
+    want = sums * s.cpu().double()[:, None] * w.cpu().double()
+    if act == D.ACT_RELU:
+        want = want.clamp_min(0)
+    err = (y.cpu().double() - want).abs()
+    tiny = 2.0 ** -25 if t == torch.float16 else 0.0
+    assert bool((err <= 1.001 * (3 * U + half(t)) * want.abs() + tiny).all()), float(err.max())
+
+
+ROWS = [1, 2, 3, 7, 16, 17, 33, 64, 65, 130, 300]
+
+
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("k,m", [(1, 1), (16, 7), (17, 16), (47, 47), (64, 64), (100, 256),
+                                 (256, 256), (602, 41), (1000, 130), (2050, 65)])
+def test_product(n, k, m):
+    check_product(n, k, m, TYPES[(n + k) % 3], ACTS[(n + m) % 2])
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n,k,m,gap", [(1, 4096, 4096, 0), (5, 640, 1030, 3), (33, 100, 47, 1),
+                                       (513, 256, 256, 0), (1030, 1024, 520, 0), (400, 602, 256, 5),
+                                       (2, 65536, 9, 0), (300, 65520, 20, 0), (20, 48, 5000, 2)])
+def test_product_types(n, k, m, gap, t, act):
+    check_product(n, k, m, t, act, gap)
+
+
+def test_product_largest_sums():
+    """Every code 127 at the largest width: sums of 2^30, scales far apart."""
+    q = torch.full((3, 65536), 127, dtype=torch.int8, device="cuda")
+    p = torch.full((2, 65536), -127, dtype=torch.int8, device="cuda")
+    s = torch.tensor([2.0 ** -126, 1.5, 2.0 ** 100], device="cuda")
+    w = torch.tensor([2.0 ** -20, 2.0 ** 97], device="cuda")
+    y = torch.empty(3, 2, device="cuda")
+    D.digest_q8_product(q, s, p, w, y)
+    want = -(65536 * 127.0 ** 2) * s.double()[:, None] * w.double()
+    got = y.double()
+    over = want.abs() > torch.finfo(torch.float32).max
+    assert bool(torch.isinf(got[over]).all())
+    assert bool(((got - want).abs()[~over] <= 3.01 * U * want.abs()[~over]).all())
+
+
+def test_product_nan_scales():
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, s = random_codes(70, 100, g)
+    p, w = random_codes(50, 100, g)
+    q[3], s[3] = 0, float("nan")
+    p[7], w[7] = 0, float("nan")
+    for act in ACTS:
+        y = torch.zeros(70, 50, device="cuda")
+        D.digest_q8_product(q, s, p, w, y, act)
+        nan = torch.isnan(y)
+        want = torch.zeros_like(nan)
+        want[3], want[:, 7] = True, True
+        assert torch.equal(nan, want)
+
+
+def grad_reference(q, s, dy, y):
+    D64 = dy.cpu().double()
+    if y is not None:
+        D64 = D64 * (y.cpu() > 0)
+    a = q.cpu().double() * s.cpu().double()[:, None]
+    return torch.mm(a.t(), D64), torch.mm(a.abs().t(), D64.abs())
+
+
+def workspace(n, k, m):
+    return torch.empty(D.digest_q8_weight_grad_query(n, k, m), dtype=torch.uint8, device="cuda")
+
+
+def check_grad(n, k, m, t, relu, gap=0):
+    g = torch.Generator(device="cuda").manual_seed(n * 5 + k + m)
+    q, s = random_codes(n, k, g, gap)
+    dy = strided(n, m, t, gap, gap, torch.randn(n, m, generator=g, device="cuda"))
+    y = None
+    if relu:
+        y = strided(n, m, t, gap + 1, gap, torch.randn(n, m, generator=g, device="cuda"))
+        y[y < 0.2] = 0
+    dw = torch.full((k, m), 7.0, device="cuda")
+    ws = workspace(n, k, m)
+    ws.fill_(255)                                  # NaN wherever a partial sum is not written
+    D.digest_q8_weight_grad(q, s, dy, dw, ws, ACTS[relu], y)
+    want, size = grad_reference(q[:, :k], s, dy, y)
+    err = (dw.cpu().double() - want).abs()
+    assert bool((err <= 2 * (n + 2) * U * size).all()), float((err / size.clamp_min(1e-30)).max())
+    again = torch.empty_like(dw)
+    D.digest_q8_weight_grad(q, s, dy, again, ws, ACTS[relu], y)
+    assert torch.equal(dw, again)
+
+
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 100, 257, 1000])
+@pytest.mark.parametrize("k,m", [(1, 1), (16, 7), (17, 47), (64, 16), (65, 65), (100, 256),
+                                 (256, 256), (602, 41), (130, 300)])
+def test_weight_grad(n, k, m):
+    check_grad(n, k, m, TYPES[(n + k) % 3], (n + m) % 2)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("relu", [0, 1])
+@pytest.mark.parametrize("n,k,m,gap", [(500, 64, 16, 0), (700, 602, 256, 3), (5000, 256, 256, 0),
+                                       (333, 1025, 130, 2), (3000, 47, 33, 1), (64, 40, 1030, 5),
+                                       (20000, 20, 300, 0)])
+def test_weight_grad_types(n, k, m, gap, t, relu):
+    check_grad(n, k, m, t, relu, gap)
+
+
+def test_weight_grad_without_rows():
+    dw = torch.full((20, 6), 7.0, device="cuda")
+    D.digest_q8_weight_grad(torch.empty(0, 32, dtype=torch.int8, device="cuda"),
+                            torch.empty(0, device="cuda"), torch.empty(0, 6, device="cuda"), dw,
+                            workspace(0, 20, 6))
+    assert bool((dw == 0).all())
+
+
+def test_weight_grad_not_finite():
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, s = random_codes(300, 40, g)
+    dy = torch.randn(300, 70, generator=g, device="cuda")
+    dy[5, 3], dy[299, 69], dy[100, 40] = float("inf"), float("nan"), float("-inf")
+    dw = torch.zeros(40, 70, device="cuda")
+    ws = workspace(300, 40, 70)
+    D.digest_q8_weight_grad(q, s, dy, dw, ws)
+    cols = torch.isnan(dw).all(0)
+    assert cols.nonzero()[:, 0].tolist() == [3, 40, 69]
+    assert bool(torch.isfinite(dw[:, ~cols]).all())
+    # masked rows are left out; a masked infinity is zero
+    y = torch.ones_like(dy)
+    y[5, 3] = y[299, 69] = y[100, 40] = 0
+    D.digest_q8_weight_grad(q, s, dy, dw, ws, D.ACT_RELU, y)
+    assert bool(torch.isfinite(dw).all())
+    y[:] = 0                                       # a mask that leaves nothing
+    D.digest_q8_weight_grad(q, s, dy, dw, ws, D.ACT_RELU, y)
+    assert bool((dw == 0).all())
+    s[7] = float("nan")
+    D.digest_q8_weight_grad(q, s, torch.ones_like(dy), dw, ws)
+    assert bool(torch.isnan(dw).all())
+
+
+def test_gradient_by_differences():
+    """dw of the product from kept rows is the derivative of sum(y dy) by W."""
+    g = torch.Generator(device="cuda").manual_seed(9)
+    n, k, m = 50, 24, 10
+    x = torch.randn(n, k, generator=g, device="cuda")
+    q, s = quantize(x)
+    xq = torch.empty_like(x)
+    D.digest_dequantize_rows(q, s, xq)
+    w = torch.randn(k, m, generator=g, device="cuda").double()
+    dy = torch.randn(n, m, generator=g, device="cuda")
+    y = torch.mm(xq.double(), w).clamp_min(0)
+    dw = torch.empty(k, m, device="cuda")
+    D.digest_q8_weight_grad(q, s, dy, dw, workspace(n, k, m), D.ACT_RELU, y.float())
+    h = 1e-6
+    loss = lambda w: (torch.mm(xq.double(), w).clamp_min(0) * dy.double()).sum()
+    for c, j in ((0, 0), (5, 3), (23, 9), (11, 7)):
+        e = torch.zeros_like(w)
+        e[c, j] = h
+        diff = (loss(w + e) - loss(w - e)) / (2 * h)
+        # a difference of sums of 500 terms of size 1 in 64 bits over 2 h
+        assert abs(float(diff) - float(dw[c, j])) < 1e-4
+
+
+def test_run_of_them():
+    """A store's rows written, read, multiplied and their gradient, as a layer uses
+    them, on a stream of its own and replayed from a graph."""
+    g = torch.Generator(device="cuda").manual_seed(11)
+    n, k, m = 400, 100, 60
+    x = torch.randn(n, k, generator=g, device="cuda")
+    w = torch.randn(k, m, generator=g, device="cuda")
+    dy = torch.randn(n, m, generator=g, device="cuda")
+    rows = torch.randperm(n, generator=g, device="cuda")[:300]
+    codes = torch.empty(300, D.digest_q8_stride(k), dtype=torch.int8, device="cuda")
+    wc = torch.empty(m, D.digest_q8_stride(k), dtype=torch.int8, device="cuda")
+    scales, ws = torch.empty(300, device="cuda"), torch.empty(m, device="cuda")
+    back, y = torch.empty(300, k, device="cuda"), torch.empty(300, m, device="cuda")
+    dw, part = torch.empty(k, m, device="cuda"), workspace(300, k, m)
+
+    def run(stream=None):
+        D.digest_quantize_rows(x, codes, scales, rows=rows, stream=stream)
+        D.digest_quantize_columns(w, wc, ws, stream=stream)
+        D.digest_dequantize_rows(codes, scales, back, stream=stream)
+        D.digest_q8_product(codes, scales, wc, ws, y, D.ACT_RELU, stream=stream)
+        D.digest_q8_weight_grad(codes, scales, dy[:300], dw, part, D.ACT_RELU, y, stream=stream)
+
+    outs = lambda: [t.clone() for t in (codes, scales, back, y, dw)]
+    run()
+    first = outs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for t in (codes, scales, back, y, dw):
+        t.zero_()
+    torch.cuda.synchronize()
+    run(stream=side)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(first, outs()))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    for turn in range(3):
+        x.copy_(torch.randn(n, k, generator=g, device="cuda"))
+        run()
+        want = outs()
+        for t in (codes, scales, back, y, dw):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, outs())), turn
+    want, size = grad_reference(codes[:, :k], scales, dy[:300], y)
+    assert bool(((dw.cpu().double() - want).abs() <= 2 * 302 * U * size).all())
+
+
+def test_binding_refuses():
+    x = torch.randn(8, 20, device="cuda")
+    codes = torch.zeros(8, 32, dtype=torch.int8, device="cuda")
+    scales = torch.zeros(8, device="cuda")
+    y = torch.zeros(8, 20, device="cuda")
+    with pytest.raises(TypeError):
+        D.digest_quantize_rows(x.double(), codes, scales)
+    with pytest.raises(TypeError):
+        D.digest_quantize_rows(x, codes.to(torch.uint8), scales)
+    with pytest.raises(ValueError):
+        D.digest_quantize_rows(x, codes[:, :16], scales)
+    with pytest.raises(ValueError):
+        D.digest_quantize_rows(x, codes, scales[:7])
+    with pytest.raises(ValueError):
+        D.digest_quantize_rows(x, codes, None)
+    with pytest.raises(TypeError):
+        D.digest_quantize_rows(x, codes, scales, rows=torch.arange(8, device="cuda").int())
+    with pytest.raises(TypeError):
+        D.digest_quantize_rows(x.cpu(), codes, scales)
+    with pytest.raises(ValueError):
+        D.digest_dequantize_rows(codes[:4], scales, y)
+    with pytest.raises(ValueError):
+        D.digest_q8_product(codes, scales, codes[:, :16], scales, y[:, :8])
+    with pytest.raises(ValueError):
+        D.digest_q8_weight_grad(codes, scales, y, torch.zeros(40, 20, device="cuda"),
+                                workspace(8, 20, 20))
+    with pytest.raises(ValueError):
+        D.digest_q8_weight_grad(codes, scales, y, torch.zeros(20, 20, device="cuda"),
+                                workspace(8, 20, 20), D.ACT_RELU)
+    narrow = torch.zeros(8, 16, dtype=torch.int8, device="cuda")
+    with pytest.raises(D.DigestError):               # onto the codes themselves
+        D.digest_dequantize_rows(narrow, scales, narrow.view(torch.float32))
