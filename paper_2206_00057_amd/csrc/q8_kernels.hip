@@ -31,6 +31,7 @@ struct Vec {
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ int64_t row_number(const RowList &l, int64_t i)
 {
@@ -318,82 +319,162 @@ __global__ __launch_bounds__(256) void k_q8_product(int32_t n, int32_t m, int32_
     }
 }
 
-// dw over rows [z chunk, (z + 1) chunk) into slice z: 64 columns of codes x 64
-// of D a workgroup, 32 x 32 a wave, 32 rows a step through LDS.  The codes are
-// exact in bfloat16; s D is split into three bfloat16 by cutting off its low
-// bits, which together are exactly its 24 bits, so that the products are
-// exact and the sums fp32.
-constexpr int kGradRows = 32;
+// Four neighbouring elements of a row, as numbers: those below `left`.
 template <class T>
-__global__ __launch_bounds__(256) void k_q8_grad(int32_t n, int32_t k, int32_t m, int64_t chunk,
-                                                 const int8_t *__restrict__ q, int64_t ldq,
-                                                 const float *__restrict__ s,
-                                                 const T *__restrict__ dy, int64_t lddy,
-                                                 const T *__restrict__ y, int64_t ldy,
-                                                 float *__restrict__ part)
+__device__ __forceinline__ f32x4 load4(const T *p, int left)
 {
-    __shared__ bf16x8 lq[4][64], ld[3][4][64];   // [rows / 8][column]
-    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t c0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
-    const int64_t rb = blockIdx.z * chunk, re = min((int64_t)n, rb + chunk);
-    const int64_t c = c0 + lane, j = j0 + lane;
-    f32x4 acc[2][2] = {};
-    for (int64_t r0 = rb; r0 < re; r0 += kGradRows) {
-        bf16x8 vq, vd[3];
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (left >= 4) {
+        const auto t = *reinterpret_cast<const typename Vec<T, 4>::type *>(p);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t r = r0 + wave * 8 + i;
-            float code = 0.f, D = 0.f;
-            if (r < re && c < k)
-                code = (float)q[r * ldq + c];
-            if (r < re && j < m) {
-                D = (float)dy[r * lddy + j];
-                if (y && !((float)y[r * ldy + j] > 0.f))
-                    D = 0.f;
-                D *= s[r];
-            }
-            vq[i] = (__bf16)code;
+        for (int i = 0; i < 4; ++i)
+            v[i] = (float)t[i];
+    } else {
 #pragma unroll
-            for (int h = 0; h < 3; ++h) {
-                const float top = __uint_as_float(__float_as_uint(D) & 0xffff0000u);
-                vd[h][i] = (__bf16)top;
-                D -= top;
-            }
+        for (int i = 0; i < 3; ++i)
+            if (i < left)
+                v[i] = (float)p[i];
+    }
+    return v;
+}
+
+// dw over rows [z chunk, (z + 1) chunk) into slice z: TC columns of codes x TJ
+// of D a workgroup of 8 waves, 32 rows a step.  The codes are exact in
+// bfloat16; s D is split into three bfloat16 by cutting off its low bits,
+// which together are exactly its 24 bits, so that the products are exact and
+// the sums fp32.
+//
+// A thread fetches four columns of four rows, a step ahead in registers, and
+// leaves them in LDS as the matrix instructions take them: [rows / 8][slot]
+// pieces of 16 bytes, slot i T / 4 + q holding column 4 q + i, so that
+// neighbouring lanes write neighbouring bytes (two lanes a piece) and a wave's
+// four tiles of D give each lane 16 columns in a row of dw to store.
+constexpr int kGradRows = 32, kGradThreads = 512;
+template <class T, int TC, int TJ>
+__global__ __launch_bounds__(kGradThreads) void k_q8_grad(
+    int32_t n, int32_t k, int32_t m, int64_t chunk, int32_t tiles_c, int32_t tiles_j,
+    const int8_t *__restrict__ q, int64_t ldq, const float *__restrict__ s,
+    const T *__restrict__ dy, int64_t lddy, const T *__restrict__ y, int64_t ldy,
+    float *__restrict__ part)
+{
+    constexpr int WJ = TJ / 64, WC = 8 / WJ, CW = TC / WC, NI = CW / 16;
+    constexpr int UD = TJ * 2, UC = TC * 2;   // threads that fetch D and codes
+    static_assert(UD <= kGradThreads && UC <= kGradThreads && NI >= 1, "one unit a thread");
+    __shared__ bf16x4 lc[2][4][TC][2], ld[2][3][4][TJ][2];   // [buffer](part)[octet][slot][half]
+
+    const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+    const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int32_t tile = id % (tiles_c * tiles_j), z = id / (tiles_c * tiles_j);
+    const int64_t c0 = (int64_t)(tile / tiles_j) * TC, j0 = (int64_t)(tile % tiles_j) * TJ;
+    const int64_t rb = z * chunk, re = min((int64_t)n, rb + chunk);
+
+    const int half = tid % 2;
+    const int qd = tid / 2 % (TJ / 4), od = tid / 2 / (TJ / 4);
+    const int qc = tid / 2 % (TC / 4), oc = tid / 2 / (TC / 4);
+    const bool does_d = UD == kGradThreads || tid < UD, does_c = UC == kGradThreads || tid < UC;
+    const int64_t jd = j0 + 4 * qd, cc = c0 + 4 * qc;
+    const int left = does_d ? (int)min((int64_t)4, m - jd) : 0;
+    const bool codes_in = does_c && cc < k;
+
+    f32x4 vd[4], vy[4];
+    float vs[4];
+    uint32_t vc[4];
+    auto fetch = [&](int64_t r0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t rd = r0 + od * 8 + half * 4 + i, rc = r0 + oc * 8 + half * 4 + i;
+            const int here = rd < re ? left : 0;
+            vd[i] = load4(dy + rd * lddy + jd, here);
+            if (y)
+                vy[i] = load4(y + rd * ldy + jd, here);
+            vs[i] = here > 0 ? s[rd] : 0.f;
+            vc[i] = codes_in && rc < re ? *reinterpret_cast<const uint32_t *>(q + rc * ldq + cc)
+                                        : 0;
         }
-        __syncthreads();
-        lq[wave][lane] = vq;
+    };
+    auto stash = [&](int b) {
+        if (does_c)
 #pragma unroll
-        for (int h = 0; h < 3; ++h)
-            ld[h][wave][lane] = vd[h];
-        __syncthreads();
-        const int l = lane % 16, g = lane / 16;
-        bf16x8 b[2];
+            for (int i = 0; i < 4; ++i) {
+                bf16x4 v;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-            b[i] = lq[g][wave / 2 * 32 + 16 * i + l];
+                for (int e = 0; e < 4; ++e)
+                    v[e] = (__bf16)(float)(int8_t)(vc[e] >> (8 * i));
+                lc[b][oc][i * (TC / 4) + qc][half] = v;
+            }
+        if (does_d)
 #pragma unroll
-        for (int h = 2; h >= 0; --h)
+            for (int i = 0; i < 4; ++i) {
+                bf16x4 v[3];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const bf16x8 a = ld[h][g][wave % 2 * 32 + 16 * i + l];
+                for (int e = 0; e < 4; ++e) {
+                    float D = vd[e][i];
+                    if (y && !(vy[e][i] > 0.f))
+                        D = 0.f;
+                    D *= vs[e];
 #pragma unroll
-                for (int o = 0; o < 2; ++o)
-                    acc[i][o] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[o], acc[i][o], 0, 0,
+                    for (int h = 0; h < 3; ++h) {
+                        const uint32_t top = __float_as_uint(D) & 0xffff0000u;
+                        v[h][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+                        D -= __uint_as_float(top);
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 3; ++h)
+                    ld[b][h][od][i * (TJ / 4) + qd][half] = v[h];
+            }
+    };
+
+    f32x4 acc[NI][4] = {};
+    const int l = lane % 16, g = lane / 16;
+    const int wj = wave % WJ, wc = wave / WJ;
+    fetch(rb);
+    int b = 0;
+    for (int64_t r0 = rb; r0 < re; r0 += kGradRows, b ^= 1) {
+        stash(b);
+        fetch(r0 + kGradRows);
+        lds_barrier();
+        bf16x8 c[NI];
+#pragma unroll
+        for (int o = 0; o < NI; ++o)
+            c[o] = *reinterpret_cast<const bf16x8 *>(&lc[b][g][wc * CW + o * 16 + l][0]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 2; h >= 0; --h) {
+                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(
+                    &ld[b][h][g][i * (TJ / 4) + wj * 16 + l][0]);
+#pragma unroll
+                for (int o = 0; o < NI; ++o)
+                    acc[o][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, c[o], acc[o][i], 0, 0,
                                                                         0);
             }
     }
-    float *out = part + (int64_t)blockIdx.z * k * m;
+    float *out = part + (int64_t)z * k * m;
 #pragma unroll
-    for (int o = 0; o < 2; ++o)
+    for (int o = 0; o < NI; ++o) {
+        const int slot = wc * CW + o * 16 + l;
+        const int64_t c = c0 + slot % (TC / 4) * 4 + slot / (TC / 4);
+        if (c >= k)
+            continue;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int e = 0; e < 4; ++e) {
+            const int64_t j = j0 + 4 * (wj * 16 + g * 4 + e);
+            float *p = out + c * m + j;
+            if (j + 4 <= m) {
+                typename Vec<float, 4>::type v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t cc = c0 + wave / 2 * 32 + 16 * o + lane % 16;
-                const int64_t jj = j0 + wave % 2 * 32 + 16 * i + lane / 16 * 4 + e;
-                if (cc < k && jj < m)
-                    out[cc * m + jj] = acc[i][o][e];
+                for (int i = 0; i < 4; ++i)
+                    v[i] = acc[o][i][e];
+                *reinterpret_cast<typename Vec<float, 4>::type *>(p) = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (j + i < m)
+                        p[i] = acc[o][i][e];
             }
+        }
+    }
 }
 
 // dw = the sum of the slices, in their order.
@@ -543,11 +624,17 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
     }); });
 }
 
+// Tile sides of the weight gradient: the smallest that hold the matrix, up to
+// 256.
+static int grad_tile_c(int32_t k) { return k > 128 ? 256 : 128; }
+static int grad_tile_j(int32_t m) { return m > 128 ? 256 : m > 64 ? 128 : 64; }
+
+// One workgroup a compute unit.
 int32_t q8_grad_splits(int32_t n, int32_t k, int32_t m)
 {
-    const int64_t tiles = (int64_t)((k + 63) / 64) * ((m + 63) / 64);
-    const int64_t want = (1024 + tiles - 1) / tiles;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>({want, (int64_t)n / 128, 256}));
+    const int tc = grad_tile_c(k), tj = grad_tile_j(m);
+    const int64_t tiles = (int64_t)((k + tc - 1) / tc) * ((m + tj - 1) / tj);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
 }
 
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
@@ -560,10 +647,23 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
     chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
     const hipError_t e = with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        const dim3 grid((k + 63) / 64, (m + 63) / 64, splits);
-        k_q8_grad<T><<<grid, 256, 0, st>>>(n, k, m, chunk, q, ldq, s, (const T *)dy, lddy,
-                                           (const T *)y, ldy, splits > 1 ? part : dw);
-        return hipGetLastError();
+        auto run = [&](auto tc, auto tj) {
+            constexpr int TC = decltype(tc)::value, TJ = decltype(tj)::value;
+            const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
+            k_q8_grad<T, TC, TJ><<<(uint32_t)(nc * nj * splits), kGradThreads, 0, st>>>(
+                n, k, m, chunk, nc, nj, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy,
+                splits > 1 ? part : dw);
+            return hipGetLastError();
+        };
+        typedef std::integral_constant<int, 64> i64;
+        typedef std::integral_constant<int, 128> i128;
+        typedef std::integral_constant<int, 256> i256;
+        const int tj = grad_tile_j(m);
+        if (grad_tile_c(k) == 256)
+            return tj == 256 ? run(i256{}, i256{}) : tj == 128 ? run(i256{}, i128{})
+                                                               : run(i256{}, i64{});
+        return tj == 256 ? run(i128{}, i256{}) : tj == 128 ? run(i128{}, i128{})
+                                                           : run(i128{}, i64{});
     });
     if (e != hipSuccess || splits <= 1)
         return e;
