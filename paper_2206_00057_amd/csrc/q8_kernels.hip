@@ -164,46 +164,81 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quant
         scales[to] = sc.s;
 }
 
-// Columns of w as rows of codes: a workgroup takes 16 columns, its 16 groups of
-// 16 lanes their rows in turn; one pass for the largest magnitudes, one for
-// the codes, which leave through LDS 16 rows (one 16-byte piece a column) at a
-// time.
-template <class T>
-__global__ __launch_bounds__(256) void k_quantize_columns(int32_t rows, int32_t cols,
-                                                          const T *__restrict__ w, int64_t ldw,
-                                                          int8_t *__restrict__ codes, int64_t ldq,
-                                                          float *__restrict__ scales)
+// Columns of w as rows of codes: a workgroup takes C columns, a thread P pieces
+// of 16 rows of one of them, in registers (P > 0: one reading of w), or in two
+// passes (P == 0, rows past 16 P kColThreads / C).  A piece is 16 bytes of codes.
+constexpr int kColThreads = 1024;
+template <class T, int C, int P>
+__global__ __launch_bounds__(kColThreads) void k_quantize_columns(
+    int32_t rows, int32_t cols, const T *__restrict__ w, int64_t ldw, int8_t *__restrict__ codes,
+    int64_t ldq, float *__restrict__ scales)
 {
-    __shared__ uint32_t red[16][17];
-    const int c = threadIdx.x % 16, g = threadIdx.x / 16;
-    const int64_t col = (int64_t)blockIdx.x * 16 + c;
+    constexpr int G = kColThreads / C, H = P ? P : 1;
+    __shared__ uint32_t red[kColThreads / kWave][C];
+    const int c = threadIdx.x % C, g = threadIdx.x / C;
+    const int64_t col = (int64_t)blockIdx.x * C + c;
+    const int32_t left = col < cols ? rows : 0;
+    auto load = [&](int32_t r0, T (&f)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            f[i] = r0 + i < left ? w[(int64_t)(r0 + i) * ldw + col] : (T)0.f;
+    };
+    auto largest = [](uint32_t top, const T (&f)[16]) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            top = max(top, magnitude((float)f[i]));
+        return top;
+    };
+    T f[H][16];
     uint32_t top = 0;
-    if (col < cols)
-        for (int32_t r = g; r < rows; r += 16)
-            top = max(top, magnitude((float)w[(int64_t)r * ldw + col]));
-    red[g][c] = top;
+    if constexpr (P > 0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            load((p * G + g) * 16, f[p]);
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            top = largest(top, f[p]);
+    } else {
+        for (int32_t r0 = g * 16; r0 < left; r0 += G * 16) {
+            load(r0, f[0]);
+            top = largest(top, f[0]);
+        }
+    }
+#pragma unroll
+    for (int m = kWave / 2; m >= C; m /= 2)
+        top = max(top, (uint32_t)__shfl_xor((int)top, m));
+    if (threadIdx.x % kWave < C)
+        red[threadIdx.x / kWave][c] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+    for (int i = 0; i < kColThreads / kWave; ++i)
         top = max(top, red[i][c]);
-    if (col >= cols)
+    if (left == 0)
         return;
     const Scale sc(top);
     if (g == 0)
         scales[col] = sc.s;
-    for (int32_t r0 = g * 16; r0 < rows; r0 += 256) {
+    auto store = [&](int32_t r0, const T (&f)[16]) {
+        if (r0 >= rows)
+            return;
         uint32_t p[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            float f[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int32_t r = r0 + 4 * j + i;
-                f[i] = r < rows ? (float)w[(int64_t)r * ldw + col] : 0.f;
-            }
-            p[j] = codes4(f, sc);
+            const float x[4] = {(float)f[4 * j], (float)f[4 * j + 1], (float)f[4 * j + 2],
+                                (float)f[4 * j + 3]};
+            p[j] = codes4(x, sc);
         }
         *reinterpret_cast<uint4 *>(codes + col * ldq + r0) = make_uint4(p[0], p[1], p[2], p[3]);
+    };
+    if constexpr (P > 0) {
+#pragma unroll
+        for (int p = 0; p < P; ++p)
+            store((p * G + g) * 16, f[p]);
+    } else {
+        for (int32_t r0 = g * 16; r0 < rows; r0 += G * 16) {
+            load(r0, f[0]);
+            store(r0, f[0]);
+        }
     }
 }
 
@@ -269,53 +304,207 @@ __device__ __forceinline__ float scaled(int sum, float s, float t)
 // ReLU that keeps a NaN.
 __device__ __forceinline__ float relu_of(float v, bool relu) { return relu && v <= 0.f ? 0.f : v; }
 
-// 64 rows x 64 channels a workgroup, 32 x 32 a wave, straight from memory.  The
-// channels are the instruction's rows, so that a lane holds four channels in
-// a row of one output row.  The sums are whole numbers below 2^31 (k <= 65536),
-// exact in any order.
-template <class T>
-__global__ __launch_bounds__(256) void k_q8_product(int32_t n, int32_t m, int32_t k,
-                                                    const int8_t *__restrict__ q, int64_t ldq,
-                                                    const float *__restrict__ s,
-                                                    const int8_t *__restrict__ p, int64_t ldp,
-                                                    const float *__restrict__ t, bool relu,
-                                                    T *__restrict__ y, int64_t ldy)
+// Outputs of N channels in a row of row r: scaled, activated, rounded, stored
+// below channel m.
+template <class T, int N>
+__device__ __forceinline__ void store_row(const int (&sum)[N], float sr,
+                                          const float *__restrict__ t, bool relu, int64_t j,
+                                          int32_t m, T *__restrict__ yr)
 {
+    if (j + N <= m) {
+        typename Vec<T, N>::type v;
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            v[e] = (T)relu_of(scaled(sum[e], sr, t[j + e]), relu);
+        *reinterpret_cast<typename Vec<T, N>::type *>(yr + j) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (j + e < m)
+                yr[j + e] = (T)relu_of(scaled(sum[e], sr, t[j + e]), relu);
+    }
+}
+
+// Few rows (up to 16 NT): bound by reading the weight's codes, 16 channels a
+// workgroup, its W waves a share of k each, straight from memory; the waves'
+// sums, whole numbers, are added through LDS.
+template <class T, int NT, int W>
+__global__ __launch_bounds__(W *kWave) void k_q8_few(int32_t n, int32_t m, int32_t k,
+                                                     const int8_t *__restrict__ q, int64_t ldq,
+                                                     const float *__restrict__ s,
+                                                     const int8_t *__restrict__ p, int64_t ldp,
+                                                     const float *__restrict__ t, bool relu,
+                                                     T *__restrict__ y, int64_t ldy)
+{
+    __shared__ i32x4 red[W][NT][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t r0 = (int64_t)blockIdx.x * 64 + wave / 2 * 32;
-    const int64_t j0 = (int64_t)blockIdx.y * 64 + wave % 2 * 32;
     const int l = lane % 16, g = lane / 16;
-    i32x4 acc[2][2] = {};
-    for (int32_t c0 = 0; c0 < k; c0 += 64) {
-        const int32_t c = c0 + g * 16;
-        i32x4 a[2], b[2];
+    const int64_t j0 = (int64_t)blockIdx.x * 16;
+    const i32x4 zero = {0, 0, 0, 0};
+    const int8_t *pj = p + min(j0 + l, (int64_t)m - 1) * ldp;
+    const int8_t *qr[NT];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int64_t j = j0 + 16 * i + l, r = r0 + 16 * i + l;
-            const i32x4 zero = {0, 0, 0, 0};
-            a[i] = j < m && c < k ? *reinterpret_cast<const i32x4 *>(p + j * ldp + c) : zero;
-            b[i] = r < n && c < k ? *reinterpret_cast<const i32x4 *>(q + r * ldq + c) : zero;
-        }
+    for (int i = 0; i < NT; ++i)
+        qr[i] = q + min(16 * i + l, n - 1) * ldq;
+    i32x4 acc[NT] = {};
+    // (a lane's k past the end: a zero code on the weight's side is enough)
+    const int32_t steps = (k + 63) / 64, each = (steps + W - 1) / W;
+    const int32_t u1 = min(steps, (wave + 1) * each);
+#pragma unroll 4
+    for (int32_t u = wave * each; u < u1; ++u) {
+        const int32_t c = u * 64 + g * 16, at = min(c, k - 16);
+        const i32x4 a = c < k ? *reinterpret_cast<const i32x4 *>(pj + at) : zero;
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                acc[i][h] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[h], acc[i][h], 0, 0, 0);
+        for (int i = 0; i < NT; ++i)
+            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+                a, *reinterpret_cast<const i32x4 *>(qr[i] + at), acc[i], 0, 0, 0);
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t r = r0 + 16 * h + l;
+    for (int i = 0; i < NT; ++i)
+        red[wave][i][lane] = acc[i];
+    __syncthreads();
+    for (int i = wave; i < NT; i += W) {
+        i32x4 v = red[0][i][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+            v += red[w][i][lane];
+        const int64_t r = 16 * i + l;
+        const int sum[4] = {v[0], v[1], v[2], v[3]};
+        if (r < n)
+            store_row(sum, s[r], t, relu, j0 + 4 * g, m, y + r * ldy);
+    }
+}
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+__device__ const uint4 kZeros = {0, 0, 0, 0};
+
+// A tile of BN rows x BM channels a workgroup, (64 TM) channels x 64 rows a wave
+// (WM x WN waves).  The channels are the instruction's rows, so that a lane
+// holds channels in a row of one output row.  Lines of 64 k of both operands
+// come straight into a ring of places in LDS: 16 rows of 64 bytes are a block
+// of 1 KB, the 16-byte piece c of row r at place c ^ (r / 2 % 4), so that the
+// lanes of a read (16 rows, one piece each) fall on different banks.  The sums are
+// whole numbers below 2^31 (k <= 65536), exact in any order.
+//
+// With 16-bit outputs the channels of a pair of blocks are dealt to the block's
+// rows so that a lane holds eight in a row.
+template <class T, int WM, int WN, int TM>
+__global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
+    int32_t n, int32_t m, int32_t k, int32_t tiles_m, const int8_t *__restrict__ q, int64_t ldq,
+    const float *__restrict__ s, const int8_t *__restrict__ p, int64_t ldp,
+    const float *__restrict__ t, bool relu, T *__restrict__ y, int64_t ldy)
+{
+    constexpr int W = WM * WN, TN = 4, BM = WM * TM * 16, BN = WN * TN * 16;
+    constexpr int BLOCKS = (BM + BN) / 16, L = BLOCKS / W, RING = 4;
+    static_assert(BLOCKS % W == 0 && TM % 2 == 0, "every wave loads as much");
+    __shared__ i32x4 lds0[BLOCKS * kWave], lds1[BLOCKS * kWave], lds2[BLOCKS * kWave],
+        lds3[BLOCKS * kWave];
+
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t j0 = (int64_t)(id % tiles_m) * BM, r0 = (int64_t)(id / tiles_m) * BN;
+
+    // what this lane loads of each of its blocks: row lane / 4, place lane % 4
+    const int8_t *src[L];
+    const int lr = lane / 4, lc = (lane % 4 ^ lr / 2 % 4) * 16;
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+        const int blk = i * W + wave;
+        if (blk < BM / 16) {
+            const int ch = sizeof(T) == 2 ? blk / 2 * 32 + lr / 4 * 8 + blk % 2 * 4 + lr % 4
+                                          : blk * 16 + lr;
+            src[i] = p + min(j0 + ch, (int64_t)m - 1) * ldp + lc;
+        } else {
+            src[i] = q + min(r0 + (blk - BM / 16) * 16 + lr, (int64_t)n - 1) * ldq + lc;
+        }
+    }
+    auto load_one = [&](int32_t line, i32x4 *dst, int i) {
+        const void *from = line * 64 + lc < k ? (const void *)(src[i] + line * 64)
+                                              : (const void *)&kZeros;
+        __builtin_amdgcn_global_load_lds((global_void *)from,
+                                         (lds_void *)(&dst[(i * W + wave) * kWave]), 16, 0, 0);
+    };
+    auto load = [&](int32_t line, i32x4 *dst) {
+#pragma unroll
+        for (int i = 0; i < L; ++i)
+            load_one(line, dst, i);
+    };
+    // Waits until all but the wave's newest `lines` lines are in LDS and its reads
+    // are done, then for the other waves.
+    static_assert((RING - 1) * L < 64, "vmcnt holds six bits");
+    auto sync = [&](auto lines) {
+        constexpr int c = decltype(lines)::value * L;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt((c & 15) | 7 << 4 | (c >> 4) << 14);
+        asm volatile("s_barrier" ::: "memory");
+    };
+    const int l = lane % 16, g = lane / 16;
+    const int read = l * 4 + (g ^ l / 2 % 4);
+    const int wm = wave / WN * TM, wn = BM / 16 + wave % WN * TN;
+
+    i32x4 acc[TM][TN] = {};
+    const int32_t lines = (k + 63) / 64;
+    // One line; its place is loaded with the line RING - 1 ahead of it... the one
+    // read before, which every wave has left at the barrier.  (Past the last line
+    // zeros are loaded, so that the waits count alike.)
+    auto step = [&](int32_t line, const i32x4 *now, i32x4 *free) {
+        sync(std::integral_constant<int, RING - 2>());
+        i32x4 a[TM], b[TN];
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+            b[i] = now[(wn + i) * kWave + read];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+            a[i] = now[(wm + i) * kWave + read];
+        load(line + RING - 1, free);
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int h = 0; h < TN; ++h)
+                acc[i][h] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[i], b[h], acc[i][h], 0, 0, 0);
+    };
+    load(0, lds0);
+    load(1, lds1);
+    load(2, lds2);
+    int32_t line = 0;
+    for (; line + 4 <= lines; line += 4) {
+        step(line, lds0, lds3);
+        step(line + 1, lds1, lds0);
+        step(line + 2, lds2, lds1);
+        step(line + 3, lds3, lds2);
+    }
+    if (line < lines)
+        step(line, lds0, lds3);
+    if (line + 1 < lines)
+        step(line + 1, lds1, lds0);
+    if (line + 2 < lines)
+        step(line + 2, lds2, lds1);
+    // (no load may still be under way to LDS when the workgroup's ends)
+    __builtin_amdgcn_s_waitcnt(0);
+
+#pragma unroll
+    for (int h = 0; h < TN; ++h) {
+        const int64_t r = r0 + (wn - BM / 16 + h) * 16 + l;
         if (r >= n)
             continue;
         const float sr = s[r];
+        if constexpr (sizeof(T) == 2) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t j = j0 + 16 * i + g * 4 + e;
-                if (j < m)
-                    y[r * ldy + j] = (T)relu_of(scaled(acc[i][h][e], sr, t[j]), relu);
+            for (int i = 0; i < TM; i += 2) {
+                const int sum[8] = {acc[i][h][0], acc[i][h][1], acc[i][h][2], acc[i][h][3],
+                                    acc[i + 1][h][0], acc[i + 1][h][1], acc[i + 1][h][2],
+                                    acc[i + 1][h][3]};
+                store_row(sum, sr, t, relu, j0 + (wm + i) * 16 + g * 8, m, y + r * ldy);
             }
+        } else {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int sum[4] = {acc[i][h][0], acc[i][h][1], acc[i][h][2], acc[i][h][3]};
+                store_row(sum, sr, t, relu, j0 + (wm + i) * 16 + g * 4, m, y + r * ldy);
+            }
+        }
     }
 }
 
@@ -477,18 +666,45 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     }
 }
 
-// dw = the sum of the slices, in their order.
-__global__ __launch_bounds__(256) void k_q8_grad_sum(const float *__restrict__ part,
-                                                     int32_t splits, int64_t count,
-                                                     float *__restrict__ dw)
+// dw = the sum of the slices: 64 vectors of four elements a workgroup, whose 16
+// waves sum a run of slices each, in their order, and then the waves' sums in
+// theirs.
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kSumWaves *kWave) void k_q8_grad_sum(const float *__restrict__ part,
+                                                                  int32_t splits, int64_t count,
+                                                                  float *__restrict__ dw)
 {
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= count)
+    __shared__ f32x4 red[kSumWaves][kWave];
+    typedef typename Vec<float, 4>::type vec;
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+    const int64_t e = ((int64_t)blockIdx.x * kWave + lane) * 4;
+    const int32_t each = (splits + kSumWaves - 1) / kSumWaves;
+    const int32_t z0 = wave * each, z1 = min(splits, z0 + each);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (e + 4 <= count) {
+#pragma unroll 8
+        for (int32_t z = z0; z < z1; ++z)
+            v += *reinterpret_cast<const vec *>(part + z * count + e);
+    } else {
+        for (int i = 0; i < 3; ++i)
+            if (e + i < count)
+                for (int32_t z = z0; z < z1; ++z)
+                    v[i] += part[z * count + e + i];
+    }
+    red[wave][lane] = v;
+    __syncthreads();
+    if (wave > 0)
         return;
-    float v = 0.f;
-    for (int32_t z = 0; z < splits; ++z)
-        v += part[z * count + e];
-    dw[e] = v;
+#pragma unroll
+    for (int w = 1; w < kSumWaves; ++w)
+        v += red[w][lane];
+    if (e + 4 <= count) {
+        *reinterpret_cast<vec *>(dw + e) = v;
+    } else {
+        for (int i = 0; i < 3; ++i)
+            if (e + i < count)
+                dw[e + i] = v[i];
+    }
 }
 
 template <class T>
@@ -577,9 +793,20 @@ hipError_t launch_quantize_columns(int32_t type, int32_t rows, int32_t cols, con
 {
     return with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        k_quantize_columns<T><<<(cols + 15) / 16, 256, 0, s>>>(rows, cols, (const T *)w, ldw,
-                                                               codes, ldq, scales);
-        return hipGetLastError();
+        auto run = [&](auto c, auto p) {
+            constexpr int C = decltype(c)::value, P = decltype(p)::value;
+            k_quantize_columns<T, C, P><<<(cols + C - 1) / C, kColThreads, 0, s>>>(
+                rows, cols, (const T *)w, ldw, codes, ldq, scales);
+            return hipGetLastError();
+        };
+        // few columns: four a workgroup, so that more of them share the rows
+        if (cols <= 1024 && rows <= 4096)
+            return run(std::integral_constant<int, 4>{}, std::integral_constant<int, 1>{});
+        if (rows <= 1024)
+            return run(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
+        if (rows <= 4096)
+            return run(std::integral_constant<int, 16>{}, std::integral_constant<int, 4>{});
+        return run(std::integral_constant<int, 16>{}, std::integral_constant<int, 0>{});
     });
 }
 
@@ -617,10 +844,36 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
 {
     return in_turns(n, [&](int64_t r0, int32_t n) { return with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        const dim3 grid((uint32_t)(((int64_t)n + 63) / 64), (uint32_t)((m + 63) / 64));
-        k_q8_product<T><<<grid, 256, 0, st>>>(n, m, k, q + r0 * ldq, ldq, s + r0, p, ldp, t, relu,
-                                              (T *)y + r0 * ldy, ldy);
-        return hipGetLastError();
+        q += r0 * ldq, s += r0;
+        T *out = (T *)y + r0 * ldy;
+        auto few = [&](auto nt) {
+            k_q8_few<T, decltype(nt)::value, 8><<<(m + 15) / 16, 8 * kWave, 0, st>>>(
+                n, m, k, q, ldq, s, p, ldp, t, relu, out, ldy);
+            return hipGetLastError();
+        };
+        if (n <= 16)
+            return few(std::integral_constant<int, 1>{});
+        if (n <= 32)
+            return few(std::integral_constant<int, 2>{});
+        if (n <= 64)
+            return few(std::integral_constant<int, 4>{});
+        auto gemm = [&](auto wm, auto wn, auto tm) {
+            constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value;
+            constexpr int TM = decltype(tm)::value, BM = WM * TM * 16, BN = WN * 64;
+            const int32_t nm = (m + BM - 1) / BM, nn = (n + BN - 1) / BN;
+            k_q8_gemm<T, WM, WN, TM><<<(uint32_t)nm * nn, WM * WN * kWave, 0, st>>>(
+                n, m, k, nm, q, ldq, s, p, ldp, t, relu, out, ldy);
+            return hipGetLastError();
+        };
+        typedef std::integral_constant<int, 2> i2;
+        typedef std::integral_constant<int, 4> i4;
+        typedef std::integral_constant<int, 8> i8;
+        const int64_t tiles = (int64_t)((m + 255) / 256) * ((n + 255) / 256);
+        if (tiles >= 256 && k >= 1024)
+            return gemm(i2{}, i4{}, i8{});   // 256 x 256
+        if (m > 64)
+            return gemm(i2{}, i2{}, i4{});   // 128 x 128
+        return gemm(i2{}, i2{}, i2{});       // 64 channels x 128 rows
     }); });
 }
 
@@ -668,7 +921,8 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
     if (e != hipSuccess || splits <= 1)
         return e;
     const int64_t count = (int64_t)k * m;
-    k_q8_grad_sum<<<(uint32_t)((count + 255) / 256), 256, 0, st>>>(part, splits, count, dw);
+    k_q8_grad_sum<<<(uint32_t)((count + 4 * kWave - 1) / (4 * kWave)), kSumWaves * kWave, 0, st>>>(
+        part, splits, count, dw);
     return hipGetLastError();
 }
 

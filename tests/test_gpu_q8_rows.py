@@ -214,6 +214,20 @@ def test_product_types(n, k, m, gap, t, act):
     check_product(n, k, m, t, act, gap)
 
 
+@pytest.mark.parametrize("n,k,m", [(4100, 1040, 4099), (3900, 1216, 4352), (70000, 130, 250)])
+def test_product_large(n, k, m):
+    """Against float64 products on the GPU: sums below 2^31, exact there."""
+    g = torch.Generator(device="cuda").manual_seed(n)
+    q, s = random_codes(n, k, g)
+    p, w = random_codes(m, k, g)
+    want = torch.mm(q.double(), p.double().t().contiguous()) * s.double()[:, None] * w.double()
+    for t in TYPES:
+        y = torch.full((n, m), 3.0, dtype=t, device="cuda")
+        D.digest_q8_product(q, s, p, w, y)
+        tiny = 2.0 ** -25 if t == torch.float16 else 0.0
+        assert bool(((y.double() - want).abs() <= 1.001 * (3 * U + half(t)) * want.abs() + tiny).all())
+
+
 def test_product_largest_sums():
     """Every code 127 at the largest width: sums of 2^30, scales far apart."""
     q = torch.full((3, 65536), 127, dtype=torch.int8, device="cuda")
