@@ -51,6 +51,7 @@ typedef enum {
 enum { DIGEST_ACT_RELU = 0, DIGEST_ACT_IDENTITY = 1 };
 enum { DIGEST_PUSH_BOUNDARY = 0, DIGEST_PUSH_ALL_OWNED = 1 };
 enum { DIGEST_PULL_ROWS = 0, DIGEST_PULL_AGGREGATE = 1 };
+enum { DIGEST_KEEP_F32 = 0, DIGEST_KEEP_Q8 = 1 };
 /* Element types of the calls that take them (all others are fp32). */
 enum { DIGEST_F32 = 0, DIGEST_BF16 = 1, DIGEST_F16 = 2 };
 
@@ -573,8 +574,8 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
  *            an array of n_x (n_codes) rows, each any number of times; NULL:
  *            all in their order.  A number outside the array gives a row of
  *            NaN.
- * Outputs overlap nothing.  Equal calls give equal bits.  None of the calls
- * belongs to a partition handle.
+ * Outputs overlap nothing.  Equal calls give equal bits.  The first five
+ * calls belong to no partition handle.
  * Errors: DIGEST_EINVAL, DIGEST_ENOMEM (workspace too small), DIGEST_EHIP.
  */
 #define DIGEST_Q8_STRIDE(width) (((width) + 15) / 16 * 16)
@@ -630,6 +631,53 @@ digest_status digest_q8_weight_grad(int64_t n_rows, int32_t d_in, int32_t d_out,
                                     int32_t type, const void *dy, int64_t lddy, int32_t act,
                                     const void *y, int64_t ldy, float *dw, void *workspace,
                                     size_t bytes, void *hip_stream);
+
+/*
+ * A partition's store in 8 bits: digest_push and digest_pull of a store whose
+ * level is held as codes [n_global, DIGEST_Q8_STRIDE(d_level)] (contiguous,
+ * 16-byte aligned) and scales [n_global], instead of floats.  A push writes
+ * the codes and scales of its rows, a pull reads the halo rows' values into
+ * the halo buffer and forms the halo aggregate from them, in both pull modes
+ * (in DIGEST_PULL_AGGREGATE the halo buffer may be written, but not read).  A
+ * level may be pulled from either kind of store.
+ * Errors: those of digest_push and digest_pull.
+ */
+digest_status digest_push_q8(digest_partition *p, int32_t level, const float *h_own,
+                             int8_t *codes, float *scales, int32_t mode, void *hip_stream);
+digest_status digest_pull_q8(digest_partition *p, int32_t level, const int8_t *codes,
+                             const float *scales, void *hip_stream);
+
+/*
+ * How the aggregated inputs AH that the layer forward keeps for the backward
+ * are held (host-side state, no device work):
+ *   DIGEST_KEEP_F32 (the default): as the floats that were multiplied by W.
+ *   DIGEST_KEEP_Q8: in 8 bits, a quarter of the memory; the layers share the
+ *     room of one AH in floats, and the weight gradient is formed from the
+ *     codes (digest_q8_weight_grad).  The forward's outputs are unchanged, dw
+ *     is that of the rounded AH.  Layers computed transform-first keep no AH
+ *     (they read h_in again) and are unchanged, and so is the GAT layer.
+ * A change of mode changes the workspace that the handle needs and unbinds
+ * it: query and bind it again.  Callers that capture graphs set the mode
+ * before the capture.
+ * Errors: DIGEST_EINVAL (NULL, unknown mode), DIGEST_ENOMEM (host memory).
+ */
+digest_status digest_partition_set_keep_mode(digest_partition *p, int32_t mode);
+
+/*
+ * Layer forward with the product in 8 bits:  h_out = act(Q(AH) W), AH = P_in
+ * h_in + P_out halo_buf[layer-1] aggregated in fp32 and held in 8 bits (Q),
+ * W given by its columns in 8 bits (digest_quantize_columns of W [d_{layer-1},
+ * d_layer]).  Always aggregates first.  Needs DIGEST_KEEP_Q8: Q(AH) is what is
+ * kept, so that the layer's backward (digest_layer_backward[_halo], with the
+ * fp32 W) takes dw from the same rows; roundings count as constants (the
+ * gradient of the values goes through to AH and W).
+ *   w_codes  device [d_layer, DIGEST_Q8_STRIDE(d_{layer-1})], contiguous;
+ *   w_scales device [d_layer];  other arguments as for digest_layer_forward.
+ * Errors: those of digest_layer_forward; DIGEST_ESTATE without DIGEST_KEEP_Q8.
+ */
+digest_status digest_layer_forward_q8(digest_partition *p, int32_t layer, const float *h_in,
+                                      const int8_t *w_codes, const float *w_scales, float *h_out,
+                                      int32_t act, void *hip_stream);
 
 /*
  * Synchronisation schedule of Algorithm 1 (pure, host only): in round

@@ -3,6 +3,7 @@
 // workspace layout, and the launch sequence of each C-ABI call.
 #include "digest.h"
 #include "kernels.h"
+#include "q8_kernels.h"
 #include "status.h"
 
 #include <hip/hip_runtime_api.h>
@@ -83,6 +84,7 @@ enum Kind : int32_t {
     K_TRANSPOSE_W,
     K_HALO_AGG,
     K_BND_ROWS,
+    K_QUANTIZE,
     K_COUNT
 };
 const char *const kKindNames[K_COUNT] = {
@@ -91,7 +93,7 @@ const char *const kKindNames[K_COUNT] = {
     "halo_gradient", "grad_push_add", "grad_pull_add", "gat_transform", "gat_scores",
     "gat_softmax", "gat_aggregate", "gat_row_terms", "gat_entry_grad", "gat_datt", "gat_dw",
     "gat_dgrad", "pad_rows", "spmm_gemm_fwd", "spmm_gemm_bwd", "relu_mask", "transpose_w",
-    "halo_aggregate", "boundary_rows"};
+    "halo_aggregate", "boundary_rows", "quantize_rows"};
 
 constexpr size_t kAlign = 256;
 constexpr int32_t kMaxWidth = 65536;
@@ -501,6 +503,9 @@ struct digest_partition {
     // DIGEST_PULL_AGGREGATE: a pull forms S straight from the store and
     // leaves the halo buffer alone (the calls that read it refuse).
     int32_t pull_mode = DIGEST_PULL_ROWS;
+    // DIGEST_KEEP_Q8: AH is kept in 8 bits (the launches come with the mode)
+    int32_t keep = DIGEST_KEEP_F32;
+    const digest::Q8Ops *q8 = nullptr;
     // P_s split at kFuseLong entries per row: the long rows (their count and
     // entries) and the distinct source rows the short and the long rows read
     int64_t long_rows_f = 0, long_nnz_f = 0, src_short_f = 0, src_long_f = 0;
@@ -529,6 +534,7 @@ struct digest_partition {
         std::vector<size_t> halo_buf;   // per level 0..L-1, rows padded_width(d_level) apart
         std::vector<size_t> hagg;       // per level 0..L-1: S, n_bnd rows padded like halo_buf
         std::vector<size_t> ah;         // per layer 1..L (index 0 unused), padded rows
+        std::vector<size_t> ahq, ahs;   // DIGEST_KEEP_Q8: AH's codes and scales (ah: one for all)
         size_t tmp, tmp_halo, tbuf, gemm_part, loss_part;
         size_t hpad;                    // a padded copy of h_in for widths not a multiple of 4
         size_t total;
@@ -808,8 +814,24 @@ void plan_layout(digest_partition &p)
     // padded copies of h_in (odd d_in) or dh_out (odd d_out), and a
     // transform-first ReLU layer's masked D
     int64_t hpad = 0;
+    int64_t q8_part = 0;   // partial sums of a dW from 8-bit rows
+    if (p.keep == DIGEST_KEEP_Q8) {
+        l.ahq.assign(p.L + 1, 0);
+        l.ahs.assign(p.L + 1, 0);
+        int32_t widest = 0;
+        for (int32_t k = 1; k <= p.L; ++k) {
+            const int32_t di = p.widths[k - 1], dout = p.widths[k];
+            l.ahq[k] = take((size_t)p.n_own * digest::q8_padded(di));
+            l.ahs[k] = take(sizeof(float) * (size_t)p.n_own);
+            widest = std::max(widest, padded_width(di));
+            q8_part = std::max<int64_t>(
+                q8_part, (int64_t)p.q8->grad_splits(p.n_own, di, dout) * di * dout);
+        }
+        std::fill(l.ah.begin(), l.ah.end(), take(sizeof(float) * (size_t)p.n_own * widest));
+    }
     for (int32_t k = 1; k <= p.L; ++k) {
-        l.ah[k] = take(sizeof(float) * (size_t)p.n_own * padded_width(p.widths[k - 1]));
+        if (p.keep == DIGEST_KEEP_F32)
+            l.ah[k] = take(sizeof(float) * (size_t)p.n_own * padded_width(p.widths[k - 1]));
         for (int32_t d : {p.widths[k - 1], p.widths[k]})
             if (d % 4)
                 hpad = std::max<int64_t>(hpad, (int64_t)p.n_own * padded_width(d));
@@ -817,7 +839,7 @@ void plan_layout(digest_partition &p)
             hpad = std::max<int64_t>(hpad, (int64_t)p.n_own * padded_width(p.widths[k]));
     }
     l.hpad = take(sizeof(float) * (size_t)hpad);
-    int64_t wmax = 0, gemm_part = 0, tbuf = 0;
+    int64_t wmax = 0, gemm_part = q8_part, tbuf = 0;
     for (int32_t k = 1; k <= p.L; ++k) {
         const int64_t di = p.widths[k - 1], dout = p.widths[k];
         wmax = std::max({wmax, di, dout});
@@ -1253,6 +1275,21 @@ digest_status halo_aggregate(digest_partition *p, int32_t level, hipStream_t s,
                                          p->at<float>(p->lay.halo_buf[level]), nullptr,
                                          p->n_halo, lw, out, s),
                      "halo aggregate");
+}
+
+// DIGEST_KEEP_Q8: the codes and scales of the aggregated input AH of `layer`,
+// which the layers share room for.
+digest_status keep_input(digest_partition *p, int32_t layer, hipStream_t s)
+{
+    if (p->keep != DIGEST_KEEP_Q8)
+        return DIGEST_OK;
+    const int32_t d = p->widths[layer - 1];
+    Timed t(p, K_QUANTIZE, layer, s);
+    return hip_check(p->q8->quantize(DIGEST_F32, p->n_own, d, p->at<float>(p->lay.ah[layer]),
+                                     padded_width(d), {}, p->n_own,
+                                     p->at<int8_t>(p->lay.ahq[layer]), digest::q8_padded(d),
+                                     p->at<float>(p->lay.ahs[layer]), {}, s),
+                     "quantize AH");
 }
 
 // T = [h_own; h2] W over the n_own owned rows and the n2 rows of a second
@@ -1738,8 +1775,13 @@ digest_status digest_push(digest_partition *p, int32_t level, const float *h_own
                      "push");
 }
 
-digest_status digest_layer_forward(digest_partition *p, int32_t layer, const float *h_in,
-                                   const float *w, float *h_out, int32_t act, void *hip_stream)
+}  // extern "C"
+
+namespace {
+
+// Argument and state checks shared by the layer forwards.
+digest_status check_forward(const digest_partition *p, int32_t layer, const void *h_in,
+                            const void *w, const void *h_out, int32_t act)
 {
     if (digest_status st = need_bound(p))
         return st;
@@ -1751,6 +1793,164 @@ digest_status digest_layer_forward(digest_partition *p, int32_t layer, const flo
         return fail(DIGEST_EINVAL, "NULL h_in, w or h_out");
     if (p->n_halo > 0 && !p->pulled[layer - 1])
         return fail(DIGEST_ESTATE, "level %d was never pulled", layer - 1);
+    return DIGEST_OK;
+}
+
+// Rows whose width is not a multiple of 4 are gathered from padded copies: h_in
+// or, copied into the workspace, its rows padded_width(d_in) apart.
+digest_status whole_vectors(digest_partition *p, int32_t layer, const float *h_in,
+                            const float **src, hipStream_t s)
+{
+    const int32_t d_in = p->widths[layer - 1], lh = padded_width(d_in);
+    *src = h_in;
+    if (lh == d_in)
+        return DIGEST_OK;
+    float *hp = p->at<float>(p->lay.hpad);
+    Timed t(p, K_PAD_ROWS, layer, s);
+    *src = hp;
+    return hip_check(
+        digest::launch_copy_rows(nullptr, nullptr, p->n_own, d_in, h_in, hp, s, d_in, lh),
+        "pad rows");
+}
+
+}  // namespace
+
+namespace digest {
+
+digest_status partition_set_keep(digest_partition *p, int32_t mode, const Q8Ops *ops)
+{
+    if (!p)
+        return fail(DIGEST_EINVAL, "NULL partition handle");
+    if (mode != DIGEST_KEEP_F32 && mode != DIGEST_KEEP_Q8)
+        return fail(DIGEST_EINVAL, "unknown keep mode %d", mode);
+    if (mode == p->keep)
+        return DIGEST_OK;
+    const int32_t before = p->keep;
+    p->keep = mode;
+    p->q8 = ops;
+    try {
+        plan_layout(*p);
+    } catch (const std::bad_alloc &) {
+        p->keep = before;
+        p->ws = nullptr;   // the layout may be half planned: nothing can be bound or run
+        p->lay.total = SIZE_MAX;
+        return fail(DIGEST_ENOMEM, "host allocation failed");
+    }
+    p->ws = nullptr;
+    return DIGEST_OK;
+}
+
+digest_status partition_push_q8(digest_partition *p, int32_t level, const float *h_own,
+                                int8_t *codes, float *scales, int32_t mode, const Q8Ops &ops,
+                                hipStream_t s)
+{
+    if (digest_status st = need_bound(p))
+        return st;
+    if (level < 1 || level >= p->L)
+        return fail(DIGEST_EINVAL, "push level %d outside [1, %d)", level, p->L);
+    if (!h_own || !codes || !scales || (uintptr_t)codes % kQ8Align)
+        return fail(DIGEST_EINVAL, "h_own, codes or scales is NULL or codes not %d-byte aligned",
+                    kQ8Align);
+    if (mode != DIGEST_PUSH_BOUNDARY && mode != DIGEST_PUSH_ALL_OWNED)
+        return fail(DIGEST_EINVAL, "unknown push mode %d", mode);
+    const bool all = mode == DIGEST_PUSH_ALL_OWNED;
+    const int32_t rows = all ? p->n_own : p->n_bnd, d = p->widths[level];
+    if (rows == 0)
+        return DIGEST_OK;
+    Timed t(p, K_PUSH, level, s);
+    return hip_check(ops.quantize(DIGEST_F32, rows, d, h_own, d,
+                                  {all ? nullptr : p->at<int32_t>(p->lay.bnd_local), false},
+                                  p->n_own, codes, q8_padded(d), scales,
+                                  {p->at<int32_t>(all ? p->lay.owned_gid : p->lay.bnd_gid), false},
+                                  s),
+                     "push in 8 bits");
+}
+
+digest_status partition_pull_q8(digest_partition *p, int32_t level, const int8_t *codes,
+                                const float *scales, const Q8Ops &ops, hipStream_t s)
+{
+    if (digest_status st = need_bound(p))
+        return st;
+    if (level < 0 || level >= p->L)
+        return fail(DIGEST_EINVAL, "pull level %d outside [0, %d)", level, p->L);
+    if (!codes || !scales || (uintptr_t)codes % kQ8Align)
+        return fail(DIGEST_EINVAL, "codes or scales is NULL or codes not %d-byte aligned",
+                    kQ8Align);
+    if (p->n_halo > 0) {
+        const int32_t d = p->widths[level];
+        {
+            Timed t(p, K_PULL, level, s);
+            if (digest_status st = hip_check(
+                    ops.dequantize(DIGEST_F32, p->n_halo, d, codes, q8_padded(d), scales,
+                                   {p->at<int32_t>(p->lay.halo_gid), false}, p->n_global,
+                                   p->at<float>(p->lay.halo_buf[level]), padded_width(d), s),
+                    "pull from 8 bits"))
+                return st;
+        }
+        if (!p->gws || p->pull_mode == DIGEST_PULL_AGGREGATE)
+            if (digest_status st = halo_aggregate(p, level, s))
+                return st;
+    }
+    p->pulled[level] = 1;
+    p->pull_gen[level] += 1;
+    return DIGEST_OK;
+}
+
+digest_status partition_forward_q8(digest_partition *p, int32_t layer, const float *h_in,
+                                   const int8_t *w_codes, const float *w_scales, float *h_out,
+                                   int32_t act, hipStream_t s)
+{
+    if (digest_status st = check_forward(p, layer, h_in, w_codes, h_out, act))
+        return st;
+    if (p->n_own > 0 && (!w_scales || (uintptr_t)w_codes % kQ8Align))
+        return fail(DIGEST_EINVAL, "w_scales is NULL or w_codes not %d-byte aligned", kQ8Align);
+    if (p->keep != DIGEST_KEEP_Q8)
+        return fail(DIGEST_ESTATE, "the partition does not keep its inputs in 8 bits");
+    const int32_t d_in = p->widths[layer - 1], d_out = p->widths[layer], lh = padded_width(d_in);
+    if (p->n_own > 0) {
+        if (p->gws && p->pull_mode == DIGEST_PULL_ROWS)
+            if (digest_status st = halo_aggregate(p, layer - 1, s))
+                return st;
+        const float *hs = p->n_bnd > 0 ? p->at<float>(p->lay.hagg[layer - 1]) : nullptr;
+        float *ah = p->at<float>(p->lay.ah[layer]);
+        if (use_sliced(*p, Csr::InH, d_in)) {
+            if (digest_status st = run_sliced(p, Csr::InH, h_in, d_in, nullptr, 0, hs, lh, d_in,
+                                              ah, lh, false, layer, s))
+                return st;
+        } else {
+            const float *src = nullptr;
+            if (digest_status st = whole_vectors(p, layer, h_in, &src, s))
+                return st;
+            if (digest_status st = run_spmm(p, Csr::InH, src, hs, p->n_own, lh, ah, layer, s))
+                return st;
+        }
+        if (digest_status st = keep_input(p, layer, s))
+            return st;
+        Timed t(p, K_GEMM_FWD, layer, s);
+        if (digest_status st = hip_check(
+                p->q8->product(DIGEST_F32, p->n_own, d_out, q8_padded(d_in),
+                               p->at<int8_t>(p->lay.ahq[layer]), q8_padded(d_in),
+                               p->at<float>(p->lay.ahs[layer]), w_codes, q8_padded(d_in), w_scales,
+                               act == DIGEST_ACT_RELU, h_out, d_out, s),
+                "forward product of 8-bit rows"))
+            return st;
+    }
+    p->fwd_done[layer] = 1;
+    p->act[layer] = act;
+    p->tf[layer] = false;
+    p->fwd_gen[layer] = p->pull_gen[layer - 1];
+    return DIGEST_OK;
+}
+
+}  // namespace digest
+
+extern "C" {
+
+digest_status digest_layer_forward(digest_partition *p, int32_t layer, const float *h_in,
+                                   const float *w, float *h_out, int32_t act, void *hip_stream)
+{
+    if (digest_status st = check_forward(p, layer, h_in, w, h_out, act))
+        return st;
     hipStream_t s = (hipStream_t)hip_stream;
     const int32_t d_in = p->widths[layer - 1], d_out = p->widths[layer];
     // The halo rows enter through their aggregate S = P_out halo (n_bnd rows),
@@ -1792,15 +1992,9 @@ digest_status digest_layer_forward(digest_partition *p, int32_t layer, const flo
         const int32_t lh = padded_width(d_in);
         const float *src0 = h_in;
         const bool sliced = use_sliced(*p, Csr::InH, d_in) && !fuse_forward(*p, layer, false);
-        if (lh != d_in && !sliced) {
-            float *hp = p->at<float>(p->lay.hpad);
-            Timed t(p, K_PAD_ROWS, layer, s);
-            if (digest_status st = hip_check(digest::launch_copy_rows(nullptr, nullptr, p->n_own,
-                                                                      d_in, h_in, hp, s, d_in, lh),
-                                             "pad rows"))
+        if (!sliced)
+            if (digest_status st = whole_vectors(p, layer, h_in, &src0, s))
                 return st;
-            src0 = hp;
-        }
         if (fuse_forward(*p, layer, tf) &&
             digest::spmm_gemm_ok(d_in, lh, lh, src0, hs, ah, ah)) {
             // the long rows through the ordinary kernel's long-row blocks,
@@ -1825,6 +2019,8 @@ digest_status digest_layer_forward(digest_partition *p, int32_t layer, const flo
                                              d_out, act == DIGEST_ACT_RELU, s),
                     "fused forward"))
                 return st;
+            if (digest_status st = keep_input(p, layer, s))
+                return st;
             p->fwd_done[layer] = 1;
             p->act[layer] = act;
             p->tf[layer] = tf;
@@ -1839,6 +2035,8 @@ digest_status digest_layer_forward(digest_partition *p, int32_t layer, const flo
                        run_spmm(p, Csr::InH, src0, hs, p->n_own, lh, ah, layer, s)) {
             return st;
         }
+        if (digest_status st = keep_input(p, layer, s))
+            return st;
         Timed t(p, K_GEMM_FWD, layer, s);
         if (narrow_out(d_in, d_out)) {
             if (digest_status st = hip_check(
@@ -2126,6 +2324,16 @@ digest_status layer_backward(digest_partition *p, int32_t layer, const float *h_
     // dW = AH^T D, D = dh_out (masked by h_out > 0 for ReLU), split over rows,
     // on stream sw.
     auto weight_grad = [&](hipStream_t sw) -> digest_status {
+        if (p->keep == DIGEST_KEEP_Q8) {
+            Timed t(p, K_GEMM_DW, layer, sw);
+            return hip_check(
+                p->q8->weight_grad(DIGEST_F32, p->n_own, d_in, d_out,
+                                   p->at<int8_t>(p->lay.ahq[layer]), digest::q8_padded(d_in),
+                                   p->at<float>(p->lay.ahs[layer]), gd, ldd,
+                                   relu && !fused ? h_out : nullptr, d_out,
+                                   p->at<float>(p->lay.gemm_part), dw, sw),
+                "dW from 8-bit rows");
+        }
         digest::GemmArgs g{};
         g.M = d_in;
         g.N = d_out;
@@ -2779,7 +2987,7 @@ digest_layer_plan layer_plan(const digest_partition &p, int32_t layer)
     } else {
         int32_t splits = 1, kchunk = 0;
         splitk_plan(d_in, d_out, p.n_own, splits, kchunk);
-        pl.dw_slices = splits;
+        pl.dw_slices = p.keep == DIGEST_KEEP_Q8 ? p.q8->grad_splits(p.n_own, d_in, d_out) : splits;
         pl.dgrad_narrow_first = !relu && d_out < d_in;
         if (const TierPlan *t = find_tiers(p, Csr::InH, padded_width(d_in))) {
             pl.tiers_fwd = t->tiers;

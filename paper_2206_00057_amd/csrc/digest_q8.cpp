@@ -158,9 +158,39 @@ size_t grad_workspace(int64_t n_rows, int32_t d_in, int32_t d_out)
     return align_up(splits > 1 ? splits * (size_t)d_in * (size_t)d_out * sizeof(float) : 1);
 }
 
+constexpr digest::Q8Ops kOps = {digest::launch_quantize_rows, digest::launch_dequantize_rows,
+                                digest::launch_q8_product, digest::q8_grad_splits,
+                                digest::launch_q8_weight_grad};
+
 }  // namespace
 
 extern "C" {
+
+digest_status digest_partition_set_keep_mode(digest_partition *p, int32_t mode)
+{
+    return digest::partition_set_keep(p, mode, &kOps);
+}
+
+digest_status digest_push_q8(digest_partition *p, int32_t level, const float *h_own,
+                             int8_t *codes, float *scales, int32_t mode, void *hip_stream)
+{
+    return digest::partition_push_q8(p, level, h_own, codes, scales, mode, kOps,
+                                     (hipStream_t)hip_stream);
+}
+
+digest_status digest_pull_q8(digest_partition *p, int32_t level, const int8_t *codes,
+                             const float *scales, void *hip_stream)
+{
+    return digest::partition_pull_q8(p, level, codes, scales, kOps, (hipStream_t)hip_stream);
+}
+
+digest_status digest_layer_forward_q8(digest_partition *p, int32_t layer, const float *h_in,
+                                      const int8_t *w_codes, const float *w_scales, float *h_out,
+                                      int32_t act, void *hip_stream)
+{
+    return digest::partition_forward_q8(p, layer, h_in, w_codes, w_scales, h_out, act,
+                                        (hipStream_t)hip_stream);
+}
 
 digest_status digest_quantize_rows(int64_t n_rows, int32_t width, int32_t type, const void *x,
                                    int64_t ldx, const int64_t *rows, int64_t n_x, int8_t *codes,

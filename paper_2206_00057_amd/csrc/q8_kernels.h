@@ -1,10 +1,13 @@
-// Internal interface between the host code of the 8-bit rows (digest_q8.cpp)
-// and their gfx950 kernels (q8_kernels.hip).  Not part of the public ABI.
+// Internal interface between the host code of the 8-bit rows (digest_q8.cpp,
+// and digest_host.cpp for a partition's calls) and their gfx950 kernels
+// (q8_kernels.hip).  Not part of the public ABI.
 #pragma once
 
 #include <hip/hip_runtime_api.h>
 
 #include <cstdint>
+
+#include "digest.h"
 
 namespace digest {
 
@@ -47,5 +50,24 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
                                  int64_t ldq, const float *s, const void *dy, int64_t lddy,
                                  const void *y, int64_t ldy, float *part, float *dw,
                                  hipStream_t st);
+
+// The launches that a partition's calls make, handed to them by digest_q8.cpp,
+// so that digest_host.cpp links without the kernels of the 8-bit rows.
+struct Q8Ops {
+    decltype(&launch_quantize_rows) quantize;
+    decltype(&launch_dequantize_rows) dequantize;
+    decltype(&launch_q8_product) product;
+    decltype(&q8_grad_splits) grad_splits;
+    decltype(&launch_q8_weight_grad) weight_grad;
+};
+digest_status partition_set_keep(digest_partition *p, int32_t mode, const Q8Ops *ops);
+digest_status partition_push_q8(digest_partition *p, int32_t level, const float *h_own,
+                                int8_t *codes, float *scales, int32_t mode, const Q8Ops &ops,
+                                hipStream_t s);
+digest_status partition_pull_q8(digest_partition *p, int32_t level, const int8_t *codes,
+                                const float *scales, const Q8Ops &ops, hipStream_t s);
+digest_status partition_forward_q8(digest_partition *p, int32_t layer, const float *h_in,
+                                   const int8_t *w_codes, const float *w_scales, float *h_out,
+                                   int32_t act, hipStream_t s);
 
 }  // namespace digest

@@ -666,9 +666,9 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     }
 }
 
-// dw = the sum of the slices: 64 vectors of four elements a workgroup, whose 16
-// waves sum a run of slices each, in their order, and then the waves' sums in
-// theirs.
+// dw = the sum of the slices: 64 vectors of four elements a workgroup, whose up
+// to 16 waves sum a run of slices each, in their order, and then the waves'
+// sums in theirs.
 constexpr int kSumWaves = 16;
 __global__ __launch_bounds__(kSumWaves *kWave) void k_q8_grad_sum(const float *__restrict__ part,
                                                                   int32_t splits, int64_t count,
@@ -678,7 +678,8 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_q8_grad_sum(const float *_
     typedef typename Vec<float, 4>::type vec;
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int64_t e = ((int64_t)blockIdx.x * kWave + lane) * 4;
-    const int32_t each = (splits + kSumWaves - 1) / kSumWaves;
+    const int waves = blockDim.x / kWave;
+    const int32_t each = (splits + waves - 1) / waves;
     const int32_t z0 = wave * each, z1 = min(splits, z0 + each);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (e + 4 <= count) {
@@ -695,8 +696,7 @@ __global__ __launch_bounds__(kSumWaves *kWave) void k_q8_grad_sum(const float *_
     __syncthreads();
     if (wave > 0)
         return;
-#pragma unroll
-    for (int w = 1; w < kSumWaves; ++w)
+    for (int w = 1; w < waves; ++w)
         v += red[w][lane];
     if (e + 4 <= count) {
         *reinterpret_cast<vec *>(dw + e) = v;
@@ -921,7 +921,8 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
     if (e != hipSuccess || splits <= 1)
         return e;
     const int64_t count = (int64_t)k * m;
-    k_q8_grad_sum<<<(uint32_t)((count + 4 * kWave - 1) / (4 * kWave)), kSumWaves * kWave, 0, st>>>(
+    const int waves = splits < 8 ? 1 : splits < 32 ? 4 : kSumWaves;
+    k_q8_grad_sum<<<(uint32_t)((count + 4 * kWave - 1) / (4 * kWave)), waves * kWave, 0, st>>>(
         part, splits, count, dw);
     return hipGetLastError();
 }

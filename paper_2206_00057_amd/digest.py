@@ -23,6 +23,7 @@ MODEL_GCN, MODEL_GAT = 0, 1
 ACT_RELU, ACT_IDENTITY = 0, 1
 PUSH_BOUNDARY, PUSH_ALL_OWNED = 0, 1
 PULL_ROWS, PULL_AGGREGATE = 0, 1
+KEEP_F32, KEEP_Q8 = 0, 1
 F32, BF16, F16 = 0, 1, 2
 
 _lib = None
@@ -742,6 +743,10 @@ def _q8_lib():
             "digest_q8_weight_grad_query": [i64, i32, i32, P],
             "digest_q8_weight_grad": [i64, i32, i32, P, i64, P, i32, P, i64, i32, P, i64, P, P, sz,
                                       P],
+            "digest_push_q8": [P, i32, P, P, P, i32, P],
+            "digest_pull_q8": [P, i32, P, P, P],
+            "digest_partition_set_keep_mode": [P, i32],
+            "digest_layer_forward_q8": [P, i32, P, P, P, P, i32, P],
         }
         for name, args in sig.items():
             f = getattr(L, name)
@@ -865,3 +870,45 @@ def digest_q8_weight_grad(codes, scales, dy, dw, workspace, act=ACT_IDENTITY, y=
     _check(_q8_lib().digest_q8_weight_grad(n, k, m, pq, ldq, ps, _TYPES[dtype], pdy, lddy, act,
                                            py, ldy, _floats(dw, k * m, dev, "dw"), ws, nbytes,
                                            _stream(stream)))
+
+
+def digest_push_q8(p, level, h_own, codes, scales, mode=PUSH_BOUNDARY, stream=None):
+    """digest_push into a store in 8 bits: codes int8 [n_global,
+    digest_q8_stride(d)], scales float32 [n_global]."""
+    import torch
+    _check_level(p, level, 1)
+    d = p.widths[level]
+    ph = _dev(h_own, torch.float32, p.n_own * d, "h_own")
+    pq = _dev(codes, torch.int8, p.n_global * digest_q8_stride(d), "codes")
+    ps = _dev(scales, torch.float32, p.n_global, "scales")
+    _check(_q8_lib().digest_push_q8(p.handle, int(level), ph, pq, ps, int(mode), _stream(stream)))
+
+
+def digest_pull_q8(p, level, codes, scales, stream=None):
+    """digest_pull out of a store in 8 bits."""
+    import torch
+    _check_level(p, level, 0)
+    pq = _dev(codes, torch.int8, p.n_global * digest_q8_stride(p.widths[level]), "codes")
+    ps = _dev(scales, torch.float32, p.n_global, "scales")
+    _check(_q8_lib().digest_pull_q8(p.handle, int(level), pq, ps, _stream(stream)))
+
+
+def digest_partition_set_keep_mode(p, mode):
+    """KEEP_F32 or KEEP_Q8; a change unbinds the workspace and changes
+    p.workspace_bytes."""
+    _check(_q8_lib().digest_partition_set_keep_mode(p.handle, int(mode)))
+    p.workspace_bytes = digest_partition_query(p)["workspace_bytes"]
+
+
+def digest_layer_forward_q8(p, layer, h_in, w_codes, w_scales, h_out, act, stream=None):
+    """The layer forward with the product in 8 bits (KEEP_Q8): w_codes int8 [d_out,
+    digest_q8_stride(d_in)], w_scales float32 [d_out] hold W's columns."""
+    import torch
+    _check_layer(p, layer)
+    di, do = p.widths[layer - 1], p.widths[layer]
+    a = _dev(h_in, torch.float32, p.n_own * di, "h_in")
+    b = _dev(w_codes, torch.int8, do * digest_q8_stride(di), "w_codes")
+    c = _dev(w_scales, torch.float32, do, "w_scales")
+    e = _dev(h_out, torch.float32, p.n_own * do, "h_out")
+    _check(_q8_lib().digest_layer_forward_q8(p.handle, int(layer), a, b, c, e, int(act),
+                                             _stream(stream)))

@@ -41,7 +41,8 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 # The sources of the profiled kernels and of their launches, with the headers
 # that they include.
 CSRC = os.path.join(ROOT, "paper_2206_00057_amd", "csrc")
-KERNEL_SOURCES = ("digest_kernels.hip", "device.h", "kernels.h", "digest_host.cpp", "status.h")
+KERNEL_SOURCES = ("digest_kernels.hip", "device.h", "kernels.h", "digest_host.cpp", "status.h",
+                  "q8_kernels.h")
 
 
 def kernel_source_hash() -> str:

@@ -28,14 +28,41 @@ import torch
 from . import digest as D
 
 
+def q8_rows(n, width, device="cuda"):
+    """Room for n rows of `width` elements in 8 bits: (codes, scales), rows of
+    zeros."""
+    return (torch.zeros(n, D.digest_q8_stride(width), dtype=torch.int8, device=device),
+            torch.zeros(n, dtype=torch.float32, device=device))
+
+
+def pull(p, level, store, stream=None):
+    """digest_pull out of a level's store: floats, or (codes, scales)."""
+    if isinstance(store, tuple):
+        D.digest_pull_q8(p, level, *store, stream=stream)
+    else:
+        D.digest_pull(p, level, store, stream=stream)
+
+
+def push(p, level, h_own, store, mode=D.PUSH_BOUNDARY, stream=None):
+    """digest_push into a level's store: floats, or (codes, scales)."""
+    if isinstance(store, tuple):
+        D.digest_push_q8(p, level, h_own, *store, mode=mode, stream=stream)
+    else:
+        D.digest_push(p, level, h_own, store, mode, stream=stream)
+
+
 class GpuPartition:
     def __init__(self, n_global, part, widths, device="cuda", overlap_io=False, model="gcn",
-                 atts=None, pull_mode=None, norms=None):
+                 atts=None, pull_mode=None, norms=None, keep="f32", product="f32"):
         """model "gcn" (Eq. 5) or "gat" (the attention layer over stale halo
         rows; atts are its per-layer [d_l, 2] attention matrices).
         norms: None, or for each hidden layer 1..L-1 its (gain, shift), device
         float32 [d_l]: a layer norm between the layer and its ReLU, so that
         H[l] = relu(norm(Z[l])) with Z[l] the layer's own output.
+        keep: "q8" holds the aggregated inputs that the backward reads in 8
+        bits; product: "q8" (with keep "q8") also multiplies them by W's
+        columns in 8 bits, which layer_forward quantises each time.  Stores
+        are float32 tensors, or (codes, scales) of q8_rows.
         pull_mode: what a pull keeps (D.PULL_ROWS or D.PULL_AGGREGATE); by
         default the halo aggregate alone for the GCN layer, the halo rows
         for the GAT layer, which reads them."""
@@ -45,7 +72,14 @@ class GpuPartition:
             raise ValueError("a GAT model needs one attention matrix per layer")
         if norms is not None and len(norms) != len(widths) - 2:
             raise ValueError("a normalised model needs (gain, shift) for each hidden layer")
+        if keep not in ("f32", "q8") or product not in ("f32", "q8"):
+            raise ValueError("keep and product are f32 or q8")
+        if model == "gat" and "q8" in (keep, product):
+            raise ValueError("inputs are kept in 8 bits by GCN layers")
+        if product == "q8" and keep != "q8":
+            raise ValueError("products in 8 bits need inputs kept in 8 bits")
         self.model, self.atts, self.norms = model, atts, norms
+        self.product = product
         self.widths = [int(w) for w in widths]
         self.L = len(self.widths) - 1
         self.device = device
@@ -54,6 +88,8 @@ class GpuPartition:
         if pull_mode is None:
             pull_mode = D.PULL_AGGREGATE if model == "gcn" else D.PULL_ROWS
         D.digest_partition_set_pull_mode(self.p, pull_mode)
+        if keep == "q8":
+            D.digest_partition_set_keep_mode(self.p, D.KEEP_Q8)
         n = self.p.n_own
         self.n_own = n
         self.workspace = torch.empty(max(self.p.workspace_bytes, 256), dtype=torch.uint8,
@@ -81,6 +117,9 @@ class GpuPartition:
             self.norm_workspace = torch.empty(
                 max([D.digest_layer_norm_query(n, self.widths[l]) for l in hidden] + [256]),
                 dtype=torch.uint8, device=device)
+        if product == "q8":
+            self.Wq = [None] + [q8_rows(self.widths[l], self.widths[l - 1], device)
+                                for l in range(1, self.L + 1)]
         self.loss = torch.zeros(1, **f32)
         self.graphs = {}
         # pulls and pushes: on their own stream (default priority) next to the
@@ -95,12 +134,18 @@ class GpuPartition:
     def normed(self, layer):
         return self.norms is not None and layer < self.L
 
-    def layer_forward(self, l, h, W, stream=None):
-        """H[l] from the rows h of level l-1."""
+    def layer_forward(self, l, h, W, stream=None, Wq=None):
+        """H[l] from the rows h of level l-1; Wq: W's columns in 8 bits, where
+        they are at hand (product "q8")."""
         normed = self.normed(l)
         out, act = (self.Z[l], D.ACT_IDENTITY) if normed else (self.H[l], self.act(l))
         if self.model == "gat":
             D.digest_gat_forward(self.p, l, h, W, self.atts[l - 1], out, act, stream=stream)
+        elif self.product == "q8":
+            if Wq is None:
+                Wq = self.Wq[l]
+                D.digest_quantize_columns(W, *Wq, stream=stream)
+            D.digest_layer_forward_q8(self.p, l, h, *Wq, out, act, stream=stream)
         else:
             D.digest_layer_forward(self.p, l, h, W, out, act, stream=stream)
         if normed:
@@ -130,7 +175,7 @@ class GpuPartition:
     def pull_all(self, stores):
         """Initial pull of every level (level 0 = features)."""
         for lev in range(self.L):
-            D.digest_pull(self.p, lev, stores[lev])
+            pull(self.p, lev, stores[lev])
 
     def forward(self, x_own, Ws, stores=None, do_pull=False, do_push=False):
         self.x_own = x_own
@@ -143,7 +188,7 @@ class GpuPartition:
             self.io.wait_stream(main)
             with torch.cuda.stream(self.io):
                 for lev in range(1, self.L):
-                    D.digest_pull(self.p, lev, stores[lev], stream=self.io)
+                    pull(self.p, lev, stores[lev], stream=self.io)
                     self.pull_done[lev].record(self.io)
         h = x_own
         for l in range(1, self.L + 1):
@@ -153,7 +198,7 @@ class GpuPartition:
             if do_push and l <= self.L - 1:
                 self.io.wait_stream(main)
                 with torch.cuda.stream(self.io):
-                    D.digest_push(self.p, l, self.H[l], stores[l], stream=self.io)
+                    push(self.p, l, self.H[l], stores[l], stream=self.io)
             h = self.H[l]
         if pulled or do_push:
             main.wait_stream(self.io)
@@ -163,10 +208,10 @@ class GpuPartition:
         h = x_own
         for l in range(1, self.L + 1):
             if do_pull and l >= 2:
-                D.digest_pull(self.p, l - 1, stores[l - 1])
+                pull(self.p, l - 1, stores[l - 1])
             self.layer_forward(l, h, Ws[l - 1])
             if do_push and l <= self.L - 1:
-                D.digest_push(self.p, l, self.H[l], stores[l])
+                push(self.p, l, self.H[l], stores[l])
             h = self.H[l]
         return self.H[self.L]
 

@@ -37,6 +37,11 @@ rows are the normalised ones); optimizer="muon" replaces the plain step of
 the weight matrices by digest_muon_average, whose momenta are global
 parameters' state (`momenta`, zero at the start).
 
+store="q8" holds the stale levels of the store in 8 bits (a scale and whole
+numbers for each row), keep="q8" the aggregated inputs that the backward reads,
+product="q8" also multiplies those by the weights' columns in 8 bits (weights
+and gradients stay float32; roundings count as constants).
+
 All arithmetic runs in libdigest.so (the layers, pulls, pushes, loss heads
 and the parameter averaging); this module owns the buffers and orders the
 calls.  ``capture`` records one round per pull/push pattern into a HIP graph.
@@ -46,7 +51,7 @@ from __future__ import annotations
 import torch
 
 from . import digest as D
-from .step import GpuPartition
+from .step import GpuPartition, pull, push, q8_rows
 
 
 def boundary_push_mode(gps, parts):
@@ -65,7 +70,7 @@ def boundary_push_mode(gps, parts):
 class DigestTrainer:
     def __init__(self, n_global, parts, widths, x, labels, weights, lr, K, device="cuda",
                  grad_exchange="none", model="gcn", atts=None, norms=None, optimizer="sgd",
-                 beta=0.95, decay=0.0):
+                 beta=0.95, decay=0.0, store="f32", keep="f32", product="f32"):
         """parts: synth-style partitions (owned, halo, CSR rows) covering the
         graph; x: device [n_global, d_0] features; labels: device int32
         [n_global]; weights: device float32 tensors W_1..W_L (the global
@@ -82,6 +87,8 @@ class DigestTrainer:
             raise ValueError("the halo-gradient exchange is defined for GCN layers")
         if optimizer not in ("sgd", "muon"):
             raise ValueError("optimizer is sgd or muon")
+        if store not in ("f32", "q8"):
+            raise ValueError("store is f32 or q8")
         self.grad_exchange = grad_exchange
         self.model, self.norms = model, norms
         self.optimizer, self.beta, self.decay = optimizer, float(beta), float(decay)
@@ -94,7 +101,7 @@ class DigestTrainer:
         # pulls keep the halo aggregate alone for GCN layers, the halo rows
         # for GAT layers (GpuPartition's default)
         self.gps = [GpuPartition(n_global, p, widths, device=device, model=model, atts=atts,
-                                 norms=norms)
+                                 norms=norms, keep=keep, product=product)
                     for p in parts]
         self.push_mode = boundary_push_mode(self.gps, parts)
         idx = [torch.from_numpy(p.owned).to(device) for p in parts]
@@ -102,8 +109,12 @@ class DigestTrainer:
         self.y_own = [labels.index_select(0, i).contiguous() for i in idx]
         f32 = dict(dtype=torch.float32, device=device)
         # the shared store: level 0 is the static features, levels 1..L-1 stale
-        self.stores = [x] + [torch.zeros(n_global, self.widths[l], **f32)
+        self.stores = [x] + [q8_rows(n_global, self.widths[l], device) if store == "q8" else
+                             torch.zeros(n_global, self.widths[l], **f32)
                              for l in range(1, self.L)]
+        # the weights' columns in 8 bits, formed once a round for all subgraphs
+        self.Wq = ([q8_rows(self.widths[l], self.widths[l - 1], device)
+                    for l in range(1, self.L + 1)] if product == "q8" else [None] * self.L)
         self.losses = torch.zeros(len(parts), **f32)
         if optimizer == "muon":
             shapes = [tuple(w.shape) for w in weights]
@@ -136,31 +147,38 @@ class DigestTrainer:
         with fresh halo rows (a round-0 pass that pulls before and pushes
         after every layer), then give every subgraph all its halo levels."""
         for gp in self.gps:
-            D.digest_pull(gp.p, 0, self.stores[0])
+            pull(gp.p, 0, self.stores[0])
+        self._quantize_weights()
         h = list(self.x_own)
         for l in range(1, self.L):
             for m, gp in enumerate(self.gps):
                 if l >= 2:
-                    D.digest_pull(gp.p, l - 1, self.stores[l - 1])
-                gp.layer_forward(l, h[m], self.W[l - 1])
+                    pull(gp.p, l - 1, self.stores[l - 1])
+                gp.layer_forward(l, h[m], self.W[l - 1], Wq=self.Wq[l - 1])
             for gp in self.gps:
-                D.digest_push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
+                push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
             h = [gp.H[l] for gp in self.gps]
         for gp in self.gps:
             for lev in range(1, self.L):
-                D.digest_pull(gp.p, lev, self.stores[lev])
+                pull(gp.p, lev, self.stores[lev])
+
+    def _quantize_weights(self):
+        for w, wq in zip(self.W, self.Wq):
+            if wq is not None:
+                D.digest_quantize_columns(w, *wq)
 
     def _round(self, do_pull, do_push):
+        self._quantize_weights()
         h = list(self.x_own)
         for l in range(1, self.L + 1):
             if do_pull and l >= 2:
                 for gp in self.gps:
-                    D.digest_pull(gp.p, l - 1, self.stores[l - 1])
+                    pull(gp.p, l - 1, self.stores[l - 1])
             for m, gp in enumerate(self.gps):
-                gp.layer_forward(l, h[m], self.W[l - 1])
+                gp.layer_forward(l, h[m], self.W[l - 1], Wq=self.Wq[l - 1])
             if do_push and l <= self.L - 1:
                 for gp in self.gps:
-                    D.digest_push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
+                    push(gp.p, l, gp.H[l], self.stores[l], self.push_mode)
             h = [gp.H[l] for gp in self.gps]
         for m, gp in enumerate(self.gps):
             D.digest_softmax_xent(gp.p, gp.H[self.L], self.y_own[m], gp.dH[self.L],

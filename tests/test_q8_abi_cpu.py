@@ -109,3 +109,39 @@ def test_weight_grad_query():
 
 def test_strides():
     assert [D.digest_q8_stride(d) for d in (1, 16, 17, 47, 64, 602)] == [16, 16, 32, 48, 64, 608]
+
+
+def partition():
+    """Three owned rows, two halo rows, 20 -> 24 -> 5."""
+    import numpy as np
+    return D.digest_partition_create(5, np.array([0, 2, 3, 5]), np.array([0, 3, 1, 2, 4]),
+                                     np.ones(5, np.float32), np.arange(3), np.array([3, 4]),
+                                     [20, 24, 5])
+
+
+def test_partition_refuses():
+    L, h = D._q8_lib(), partition()
+    q = ctypes.c_void_p(P[0])
+    for call in (lambda: L.digest_push_q8(h.handle, 1, q, q, q, 0, None),
+                 lambda: L.digest_pull_q8(h.handle, 1, q, q, None),
+                 lambda: L.digest_layer_forward_q8(h.handle, 1, q, q, q, q, 0, None)):
+        assert call() == D.ESTATE                   # no workspace
+    assert L.digest_push_q8(None, 1, q, q, q, 0, None) == D.EINVAL
+    assert L.digest_pull_q8(None, 1, q, q, None) == D.EINVAL
+    assert L.digest_partition_set_keep_mode(None, D.KEEP_Q8) == D.EINVAL
+    for mode in (-1, 2):
+        assert L.digest_partition_set_keep_mode(h.handle, mode) == D.EINVAL
+
+
+def test_keep_mode_changes_the_workspace():
+    import numpy as np
+    n = 40000
+    h = D.digest_partition_create(n, np.arange(n + 1), np.arange(n), np.ones(n, np.float32),
+                                  np.arange(n), np.zeros(0, np.int64), [256, 256, 256, 256, 7])
+    whole = h.workspace_bytes
+    D.digest_partition_set_keep_mode(h, D.KEEP_Q8)
+    # four AH of 4 bytes an element against one, codes of all and partial sums
+    assert h.workspace_bytes < whole
+    D.digest_partition_set_keep_mode(h, D.KEEP_Q8)
+    D.digest_partition_set_keep_mode(h, D.KEEP_F32)
+    assert h.workspace_bytes == whole
