@@ -508,38 +508,23 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
     }
 }
 
-// Four neighbouring elements of a row, as numbers: those below `left`.
-template <class T>
-__device__ __forceinline__ f32x4 load4(const T *p, int left)
-{
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (left >= 4) {
-        const auto t = *reinterpret_cast<const typename Vec<T, 4>::type *>(p);
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            v[i] = (float)t[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < left)
-                v[i] = (float)p[i];
-    }
-    return v;
-}
-
 // dw over rows [z chunk, (z + 1) chunk) into slice z: TC columns of codes x TJ
 // of D a workgroup of 8 waves, 32 rows a step.  The codes are exact in
 // bfloat16; s D is split into three bfloat16 by cutting off its low bits,
 // which together are exactly its 24 bits, so that the products are exact and
 // the sums fp32.
 //
-// A thread fetches four columns of four rows, a step ahead in registers, and
-// leaves them in LDS as the matrix instructions take them: [rows / 8][slot]
-// pieces of 16 bytes, slot i T / 4 + q holding column 4 q + i, so that
-// neighbouring lanes write neighbouring bytes (two lanes a piece) and a wave's
-// four tiles of D give each lane 16 columns in a row of dw to store.
+// A thread fetches four columns of four rows, two steps ahead in
+// registers, and leaves them in LDS beside the step before's instructions, as
+// the matrix instructions take them: [rows / 8][slot] pieces of 16 bytes, slot
+// i T / 4 + q holding column 4 q + i, so that neighbouring lanes write
+// neighbouring bytes (two lanes a piece) and a wave's four tiles of D give each
+// lane 16 columns in a row of dw to store.
 constexpr int kGradRows = 32, kGradThreads = 512;
-template <class T, int TC, int TJ>
+//
+// ANY: fewer than four columns, or strides whose offsets of 32 rows pass 32
+// bits; element by element.
+template <class T, bool RELU, int TC, int TJ, bool ANY>
 __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     int32_t n, int32_t k, int32_t m, int64_t chunk, int32_t tiles_c, int32_t tiles_j,
     const int8_t *__restrict__ q, int64_t ldq, const float *__restrict__ s,
@@ -558,70 +543,111 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     const int64_t rb = z * chunk, re = min((int64_t)n, rb + chunk);
 
     const int half = tid % 2;
-    const int qd = tid / 2 % (TJ / 4), od = tid / 2 / (TJ / 4);
-    const int qc = tid / 2 % (TC / 4), oc = tid / 2 / (TC / 4);
+    // (threads with nothing to fetch repeat others' fetches)
+    const int qd = tid / 2 % (TJ / 4), od = tid / 2 / (TJ / 4) % 4;
+    const int qc = tid / 2 % (TC / 4), oc = tid / 2 / (TC / 4) % 4;
     const bool does_d = UD == kGradThreads || tid < UD, does_c = UC == kGradThreads || tid < UC;
-    const int64_t jd = j0 + 4 * qd, cc = c0 + 4 * qc;
-    const int left = does_d ? (int)min((int64_t)4, m - jd) : 0;
-    const bool codes_in = does_c && cc < k;
+    // A vector that would pass the row's end lies against it instead: its columns
+    // are formed twice, alike.  Vectors behind it repeat it and are not stored.
+    const int64_t last = max(m - 4, 0);
+    const int64_t jd = min(j0 + 4 * qd, last), cc = min(c0 + 4 * qc, (int64_t)q8_padded(k) - 4);
 
-    f32x4 vd[4], vy[4];
-    float vs[4];
-    uint32_t vc[4];
-    auto fetch = [&](int64_t r0) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t rd = r0 + od * 8 + half * 4 + i, rc = r0 + oc * 8 + half * 4 + i;
-            const int here = rd < re ? left : 0;
-            vd[i] = load4(dy + rd * lddy + jd, here);
-            if (y)
-                vy[i] = load4(y + rd * ldy + jd, here);
-            vs[i] = here > 0 ? s[rd] : 0.f;
-            vc[i] = codes_in && rc < re ? *reinterpret_cast<const uint32_t *>(q + rc * ldq + cc)
-                                        : 0;
-        }
-    };
-    auto stash = [&](int b) {
-        if (does_c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                bf16x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = (__bf16)(float)(int8_t)(vc[e] >> (8 * i));
-                lc[b][oc][i * (TC / 4) + qc][half] = v;
-            }
-        if (does_d)
+    const int rd = od * 8 + half * 4, rc = oc * 8 + half * 4;
+    const uint32_t bytes_d = lddy * sizeof(T), bytes_y = ldy * sizeof(T), bytes_c = ldq;
+    const uint32_t col_d = jd * sizeof(T), col_c = cc;   // (not with ANY)
+    struct Fetched {
+        typename Vec<T, 4>::type d[4], y[RELU ? 4 : 1];
+        typename Vec<float, 4>::type s;
+        uint32_t c[4];
+    } next;
+    // The rows r0 .. r0 + 31.  Rows past the end repeat the last one with codes of
+    // zero: what it adds to its columns is nothing, or the NaN that they hold.
+    auto fetch = [&](Fetched &f, int64_t r0) {
+        const int rows = (int)min((int64_t)kGradRows, re - r0);
+        if (rows <= 0)
+            return;
+        const char *bd = (const char *)(dy + r0 * lddy), *by = (const char *)(y + r0 * ldy);
+        const char *bc = (const char *)(q + r0 * ldq), *bs = (const char *)(s + r0);
+        if constexpr (ANY) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                bf16x4 v[3];
+                const int64_t r = min(rd + i, rows - 1);
+                f.s[i] = s[r0 + r];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float D = vd[e][i];
-                    if (y && !(vy[e][i] > 0.f))
-                        D = 0.f;
-                    D *= vs[e];
-#pragma unroll
-                    for (int h = 0; h < 3; ++h) {
-                        const uint32_t top = __float_as_uint(D) & 0xffff0000u;
-                        v[h][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
-                        D -= __uint_as_float(top);
-                    }
+                    const int64_t j = min(jd + e, (int64_t)m - 1);
+                    f.d[i][e] = dy[(r0 + r) * lddy + j];
+                    if constexpr (RELU)
+                        f.y[i][e] = y[(r0 + r) * ldy + j];
                 }
-#pragma unroll
-                for (int h = 0; h < 3; ++h)
-                    ld[b][h][od][i * (TJ / 4) + qd][half] = v[h];
+                f.c[i] = rc + i < rows ? *reinterpret_cast<const uint32_t *>(
+                                             q + (r0 + rc + i) * ldq + cc)
+                                       : 0;
             }
+            return;
+        }
+        typedef typename Vec<T, 4>::type vec;
+        if (rows == kGradRows) {
+            const uint32_t at_d = rd * bytes_d + col_d, at_y = rd * bytes_y + col_d;
+            const uint32_t at_c = rc * bytes_c + col_c;
+            f.s = *reinterpret_cast<const typename Vec<float, 4>::type *>(bs + (uint32_t)rd * 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                f.d[i] = *reinterpret_cast<const vec *>(bd + (uint64_t)i * bytes_d + at_d);
+                if constexpr (RELU)
+                    f.y[i] = *reinterpret_cast<const vec *>(by + (uint64_t)i * bytes_y + at_y);
+                f.c[i] = *reinterpret_cast<const uint32_t *>(bc + (uint64_t)i * bytes_c + at_c);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t r = min(rd + i, rows - 1), h = min(rc + i, rows - 1);
+                f.s[i] = *reinterpret_cast<const float *>(bs + r * 4);
+                f.d[i] = *reinterpret_cast<const vec *>(bd + (r * bytes_d + col_d));
+                if constexpr (RELU)
+                    f.y[i] = *reinterpret_cast<const vec *>(by + (r * bytes_y + col_d));
+                f.c[i] = *reinterpret_cast<const uint32_t *>(bc + (h * bytes_c + col_c));
+                f.c[i] = rc + i < rows ? f.c[i] : 0;
+            }
+        }
+    };
+    // column i of what was fetched, into buffer b
+    auto stash_codes = [&](const Fetched &f, int b, int i) {
+        if (!does_c)
+            return;
+        bf16x4 v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            v[e] = (__bf16)(float)(int8_t)(f.c[e] >> (8 * i));
+        lc[b][oc][i * (TC / 4) + qc][half] = v;
+    };
+    auto stash_d = [&](const Fetched &f, int b, int i) {
+        if (!does_d)
+            return;
+        bf16x4 v[3];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float D = (float)f.d[e][i];
+            if constexpr (RELU)
+                if (!((float)f.y[e][i] > 0.f))
+                    D = 0.f;
+            D *= f.s[e];
+#pragma unroll
+            for (int h = 0; h < 3; ++h) {
+                const uint32_t top = __float_as_uint(D) & 0xffff0000u;
+                v[h][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+                D -= __uint_as_float(top);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 3; ++h)
+            ld[b][h][od][i * (TJ / 4) + qd][half] = v[h];
     };
 
     f32x4 acc[NI][4] = {};
     const int l = lane % 16, g = lane / 16;
     const int wj = wave % WJ, wc = wave / WJ;
-    fetch(rb);
-    int b = 0;
-    for (int64_t r0 = rb; r0 < re; r0 += kGradRows, b ^= 1) {
-        stash(b);
-        fetch(r0 + kGradRows);
+    auto step = [&](int b, Fetched &next, int64_t further) {
         lds_barrier();
         bf16x8 c[NI];
 #pragma unroll
@@ -637,7 +663,26 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
                 for (int o = 0; o < NI; ++o)
                     acc[o][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, c[o], acc[o][i], 0, 0,
                                                                         0);
+                // the next step's operands, beside the second half's instructions
+                const int slot = i * 3 + 2 - h - 4;
+                if (slot >= 0 && slot % 2 == 0)
+                    stash_d(next, b ^ 1, slot / 2);
+                else if (slot >= 0)
+                    stash_codes(next, b ^ 1, slot / 2);
+                __builtin_amdgcn_sched_barrier(0);
             }
+        fetch(next, further);
+    };
+    fetch(next, rb);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        stash_codes(next, 0, i);
+        stash_d(next, 0, i);
+    }
+    fetch(next, rb + kGradRows);
+    int b = 0;
+    for (int64_t r0 = rb; r0 < re; r0 += kGradRows, b ^= 1) {
+        step(b, next, r0 + 2 * kGradRows);
     }
     float *out = part + (int64_t)z * k * m;
 #pragma unroll
@@ -649,8 +694,10 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int64_t j = j0 + 4 * (wj * 16 + g * 4 + e);
-            float *p = out + c * m + j;
-            if (j + 4 <= m) {
+            float *p = out + c * m + min(j, last);
+            if (j >= m)
+                continue;
+            if (m >= 4) {
                 typename Vec<float, 4>::type v;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -659,7 +706,7 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
             } else {
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
-                    if (j + i < m)
+                    if (i < m)
                         p[i] = acc[o][i][e];
             }
         }
@@ -900,10 +947,13 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
     chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
     const hipError_t e = with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        auto run = [&](auto tc, auto tj) {
+        auto run = [&](auto tc, auto tj, auto any) {
             constexpr int TC = decltype(tc)::value, TJ = decltype(tj)::value;
             const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
-            k_q8_grad<T, TC, TJ><<<(uint32_t)(nc * nj * splits), kGradThreads, 0, st>>>(
+            constexpr bool ANY = decltype(any)::value;
+            const auto kernel = y ? k_q8_grad<T, true, TC, TJ, ANY>
+                                  : k_q8_grad<T, false, TC, TJ, ANY>;
+            kernel<<<(uint32_t)(nc * nj * splits), kGradThreads, 0, st>>>(
                 n, k, m, chunk, nc, nj, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy,
                 splits > 1 ? part : dw);
             return hipGetLastError();
@@ -911,12 +961,18 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
         typedef std::integral_constant<int, 64> i64;
         typedef std::integral_constant<int, 128> i128;
         typedef std::integral_constant<int, 256> i256;
-        const int tj = grad_tile_j(m);
-        if (grad_tile_c(k) == 256)
-            return tj == 256 ? run(i256{}, i256{}) : tj == 128 ? run(i256{}, i128{})
-                                                               : run(i256{}, i64{});
-        return tj == 256 ? run(i128{}, i256{}) : tj == 128 ? run(i128{}, i128{})
-                                                           : run(i128{}, i64{});
+        const int64_t pitch = std::max<int64_t>(std::max(lddy, y ? ldy : 0) * sizeof(T), ldq);
+        const int tc = grad_tile_c(k), tj = grad_tile_j(m);
+        const std::false_type no;
+        if (m < 4 || (pitch + 65536 * 4) * kGradRows > UINT32_MAX)
+            return run(i128{}, i64{}, std::true_type{});
+        if (tc == 256)
+            return tj == 256   ? run(i256{}, i256{}, no)
+                   : tj == 128 ? run(i256{}, i128{}, no)
+                               : run(i256{}, i64{}, no);
+        return tj == 256   ? run(i128{}, i256{}, no)
+               : tj == 128 ? run(i128{}, i128{}, no)
+                           : run(i128{}, i64{}, no);
     });
     if (e != hipSuccess || splits <= 1)
         return e;

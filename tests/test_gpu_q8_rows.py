@@ -292,7 +292,8 @@ def check_grad(n, k, m, t, relu, gap=0):
 
 @pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 100, 257, 1000])
 @pytest.mark.parametrize("k,m", [(1, 1), (16, 7), (17, 47), (64, 16), (65, 65), (100, 256),
-                                 (256, 256), (602, 41), (130, 300)])
+                                 (256, 256), (602, 41), (130, 300),
+                                 (20, 2), (300, 3), (129, 4), (40, 5), (200, 66)])
 def test_weight_grad(n, k, m):
     check_grad(n, k, m, TYPES[(n + k) % 3], (n + m) % 2)
 
@@ -304,6 +305,25 @@ def test_weight_grad(n, k, m):
                                        (20000, 20, 300, 0)])
 def test_weight_grad_types(n, k, m, gap, t, relu):
     check_grad(n, k, m, t, relu, gap)
+
+
+@pytest.mark.parametrize("relu", [0, 1])
+def test_weight_grad_of_far_rows(relu):
+    """Rows 128 MB apart: 32 of them pass 4 GB."""
+    n, k, m, ld = 70, 50, 90, 2 ** 25
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q, s = random_codes(n, k, g)
+    whole = torch.empty(n * ld, device="cuda")
+    dy = whole.view(n, ld)[:, 5:5 + m]
+    dy.copy_(torch.randn(n, m, generator=g, device="cuda"))
+    y = None
+    if relu:
+        y = whole.view(n, ld)[:, 1000:1000 + m]
+        y.copy_(torch.randn(n, m, generator=g, device="cuda"))
+    dw = torch.full((k, m), 7.0, device="cuda")
+    D.digest_q8_weight_grad(q, s, dy, dw, workspace(n, k, m), ACTS[relu], y)
+    want, size = grad_reference(q[:, :k], s, dy, y)
+    assert bool(((dw.cpu().double() - want).abs() <= 2 * (n + 2) * U * size).all())
 
 
 def test_weight_grad_without_rows():
