@@ -824,8 +824,7 @@ void plan_layout(digest_partition &p)
             l.ahq[k] = take((size_t)p.n_own * digest::q8_padded(di));
             l.ahs[k] = take(sizeof(float) * (size_t)p.n_own);
             widest = std::max(widest, padded_width(di));
-            q8_part = std::max<int64_t>(
-                q8_part, (int64_t)p.q8->grad_splits(p.n_own, di, dout) * di * dout);
+            q8_part = std::max(q8_part, (int64_t)p.q8->grad_floats(p.n_own, di, dout));
         }
         std::fill(l.ah.begin(), l.ah.end(), take(sizeof(float) * (size_t)p.n_own * widest));
     }
@@ -2987,7 +2986,7 @@ digest_layer_plan layer_plan(const digest_partition &p, int32_t layer)
     } else {
         int32_t splits = 1, kchunk = 0;
         splitk_plan(d_in, d_out, p.n_own, splits, kchunk);
-        pl.dw_slices = p.keep == DIGEST_KEEP_Q8 ? p.q8->grad_splits(p.n_own, d_in, d_out) : splits;
+        pl.dw_slices = splits;
         pl.dgrad_narrow_first = !relu && d_out < d_in;
         if (const TierPlan *t = find_tiers(p, Csr::InH, padded_width(d_in))) {
             pl.tiers_fwd = t->tiers;

@@ -154,12 +154,12 @@ digest_status check_grad(int64_t n_rows, int32_t d_in, int32_t d_out)
 
 size_t grad_workspace(int64_t n_rows, int32_t d_in, int32_t d_out)
 {
-    const size_t splits = (size_t)digest::q8_grad_splits((int32_t)n_rows, d_in, d_out);
-    return align_up(splits > 1 ? splits * (size_t)d_in * (size_t)d_out * sizeof(float) : 1);
+    const size_t floats = digest::q8_grad_floats((int32_t)n_rows, d_in, d_out);
+    return align_up(floats ? floats * sizeof(float) : 1);
 }
 
 constexpr digest::Q8Ops kOps = {digest::launch_quantize_rows, digest::launch_dequantize_rows,
-                                digest::launch_q8_product, digest::q8_grad_splits,
+                                digest::launch_q8_product, digest::q8_grad_floats,
                                 digest::launch_q8_weight_grad};
 
 }  // namespace

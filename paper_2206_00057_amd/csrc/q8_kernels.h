@@ -5,6 +5,7 @@
 
 #include <hip/hip_runtime_api.h>
 
+#include <cstddef>
 #include <cstdint>
 
 #include "digest.h"
@@ -44,8 +45,8 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
                              int64_t ldq, const float *s, const int8_t *p, int64_t ldp,
                              const float *t, bool relu, void *y, int64_t ldy, hipStream_t st);
 // dw[c][j] = sum_r q[r][c] s_r D[r][j], D = dy or dy 1[y > 0] (y not null);
-// splits > 1: part holds splits x k x m floats.
-int32_t q8_grad_splits(int32_t n, int32_t k, int32_t m);
+// part holds q8_grad_floats floats.
+size_t q8_grad_floats(int32_t n, int32_t k, int32_t m);
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
                                  int64_t ldq, const float *s, const void *dy, int64_t lddy,
                                  const void *y, int64_t ldy, float *part, float *dw,
@@ -57,7 +58,7 @@ struct Q8Ops {
     decltype(&launch_quantize_rows) quantize;
     decltype(&launch_dequantize_rows) dequantize;
     decltype(&launch_q8_product) product;
-    decltype(&q8_grad_splits) grad_splits;
+    decltype(&q8_grad_floats) grad_floats;
     decltype(&launch_q8_weight_grad) weight_grad;
 };
 digest_status partition_set_keep(digest_partition *p, int32_t mode, const Q8Ops *ops);

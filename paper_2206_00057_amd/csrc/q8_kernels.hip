@@ -521,13 +521,18 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
 // neighbouring bytes (two lanes a piece) and a wave's four tiles of D give each
 // lane 16 columns in a row of dw to store.
 constexpr int kGradRows = 32, kGradThreads = 512;
+template <int TILE>
+__device__ __forceinline__ int slot_column(int slot)
+{
+    return slot % (TILE / 4) * 4 + slot / (TILE / 4);
+}
 //
 // ANY: fewer than four columns, or strides whose offsets of 32 rows pass 32
 // bits; element by element.
 template <class T, bool RELU, int TC, int TJ, bool ANY>
 __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
-    int32_t n, int32_t k, int32_t m, int64_t chunk, int32_t tiles_c, int32_t tiles_j,
-    const int8_t *__restrict__ q, int64_t ldq, const float *__restrict__ s,
+    int32_t n, int32_t k, int32_t m, int64_t chunk, int32_t splits, int32_t tiles_c,
+    int32_t tiles_j, const int8_t *__restrict__ q, int64_t ldq, const float *__restrict__ s,
     const T *__restrict__ dy, int64_t lddy, const T *__restrict__ y, int64_t ldy,
     float *__restrict__ part)
 {
@@ -653,24 +658,28 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
 #pragma unroll
         for (int o = 0; o < NI; ++o)
             c[o] = *reinterpret_cast<const bf16x8 *>(&lc[b][g][wc * CW + o * 16 + l][0]);
+        // (a fragment is read beside the instructions that take the one before)
+        auto frag = [&](int slot) {
+            return *reinterpret_cast<const bf16x8 *>(
+                &ld[b][2 - slot % 3][g][slot / 3 * (TJ / 4) + wj * 16 + l][0]);
+        };
+        bf16x8 a = frag(0), ahead;
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int slot = 0; slot < 12; ++slot) {
+            if (slot < 11)
+                ahead = frag(slot + 1);
 #pragma unroll
-            for (int h = 2; h >= 0; --h) {
-                const bf16x8 a = *reinterpret_cast<const bf16x8 *>(
-                    &ld[b][h][g][i * (TJ / 4) + wj * 16 + l][0]);
-#pragma unroll
-                for (int o = 0; o < NI; ++o)
-                    acc[o][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, c[o], acc[o][i], 0, 0,
-                                                                        0);
-                // the next step's operands, beside the second half's instructions
-                const int slot = i * 3 + 2 - h - 4;
-                if (slot >= 0 && slot % 2 == 0)
-                    stash_d(next, b ^ 1, slot / 2);
-                else if (slot >= 0)
-                    stash_codes(next, b ^ 1, slot / 2);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+            for (int o = 0; o < NI; ++o)
+                acc[o][slot / 3] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    a, c[o], acc[o][slot / 3], 0, 0, 0);
+            // the next step's operands, beside the last two thirds' instructions
+            if (slot >= 4 && slot % 2 == 0)
+                stash_d(next, b ^ 1, slot / 2 - 2);
+            else if (slot >= 4)
+                stash_codes(next, b ^ 1, slot / 2 - 2);
+            a = ahead;
+            __builtin_amdgcn_sched_barrier(0);
+        }
         fetch(next, further);
     };
     fetch(next, rb);
@@ -684,17 +693,26 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     for (int64_t r0 = rb; r0 < re; r0 += kGradRows, b ^= 1) {
         step(b, next, r0 + 2 * kGradRows);
     }
-    float *out = part + (int64_t)z * k * m;
+    if (splits > 1) {
+        // as the lanes hold them
+        f32x4 *out = (f32x4 *)part + ((int64_t)z * (tiles_c * tiles_j) + tile) * (TC * TJ / 4) +
+                     wave * (NI * 4 * kWave) + lane;
+#pragma unroll
+        for (int o = 0; o < NI; ++o)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                out[(o * 4 + i) * kWave] = acc[o][i];
+        return;
+    }
 #pragma unroll
     for (int o = 0; o < NI; ++o) {
-        const int slot = wc * CW + o * 16 + l;
-        const int64_t c = c0 + slot % (TC / 4) * 4 + slot / (TC / 4);
+        const int64_t c = c0 + slot_column<TC>(wc * CW + o * 16 + l);
         if (c >= k)
             continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const int64_t j = j0 + 4 * (wj * 16 + g * 4 + e);
-            float *p = out + c * m + min(j, last);
+            float *p = part + c * m + min(j, last);
             if (j >= m)
                 continue;
             if (m >= 4) {
@@ -713,44 +731,67 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     }
 }
 
-// dw = the sum of the slices: 64 vectors of four elements a workgroup, whose up
-// to 16 waves sum a run of slices each, in their order, and then the waves'
-// sums in theirs.
-constexpr int kSumWaves = 16;
-__global__ __launch_bounds__(kSumWaves *kWave) void k_q8_grad_sum(const float *__restrict__ part,
-                                                                  int32_t splits, int64_t count,
-                                                                  float *__restrict__ dw)
+// dw = the sum of the slices, each tile's vectors as k_q8_grad's lanes hold them.
+// Many slices (FEW false): 64 vectors a workgroup, whose 16 waves sum a run of
+// slices each, in their order, and then the waves' sums in theirs.  Few: 256
+// vectors, 64 a wave, which together are whole runs of dw's rows to store.
+constexpr int kSumWaves = 16, kSumFew = 32;
+template <int TC, int TJ, bool FEW>
+__global__ __launch_bounds__(FEW ? 4 * kWave : kSumWaves *kWave) void k_q8_grad_sum(
+    const float *__restrict__ part, int32_t splits, int32_t k, int32_t m, int32_t tiles_j,
+    int64_t slice, float *__restrict__ dw)
 {
-    __shared__ f32x4 red[kSumWaves][kWave];
-    typedef typename Vec<float, 4>::type vec;
+    constexpr int WJ = TJ / 64, WC = 8 / WJ, CW = TC / WC, NI = CW / 16, EACH = 8 * NI;
+    constexpr int WAVES = FEW ? 4 : kSumWaves;
+    __shared__ f32x4 red[WAVES][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-    const int64_t e = ((int64_t)blockIdx.x * kWave + lane) * 4;
-    const int waves = blockDim.x / kWave;
-    const int32_t each = (splits + waves - 1) / waves;
-    const int32_t z0 = wave * each, z1 = min(splits, z0 + each);
+    const int block = FEW ? blockIdx.x : blockIdx.x / 4;
+    const int i = FEW ? wave : blockIdx.x % 4;   // column of four
+    const int32_t each = FEW ? splits : (splits + WAVES - 1) / WAVES;
+    const int32_t z0 = FEW ? 0 : wave * each, z1 = min(splits, z0 + each);
+    const f32x4 *src = (const f32x4 *)part + ((int64_t)block * 4 + i) * kWave + lane;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (e + 4 <= count) {
 #pragma unroll 8
-        for (int32_t z = z0; z < z1; ++z)
-            v += *reinterpret_cast<const vec *>(part + z * count + e);
-    } else {
-        for (int i = 0; i < 3; ++i)
-            if (e + i < count)
-                for (int32_t z = z0; z < z1; ++z)
-                    v[i] += part[z * count + e + i];
-    }
+    for (int32_t z = z0; z < z1; ++z)
+        v += src[z * slice];
     red[wave][lane] = v;
     __syncthreads();
-    if (wave > 0)
+    // what the lane holds there
+    const int tile = block / EACH, of = block % EACH / NI, o = block % NI;
+    const int64_t c = (int64_t)(tile / tiles_j) * TC +
+                      slot_column<TC>(of / WJ * CW + o * 16 + lane % 16);
+    if (c >= k)
         return;
-    for (int w = 1; w < waves; ++w)
-        v += red[w][lane];
-    if (e + 4 <= count) {
-        *reinterpret_cast<vec *>(dw + e) = v;
+    const int64_t last = max(m - 4, 0);
+    const int64_t j0 = (int64_t)(tile % tiles_j) * TJ + 4 * (of % WJ * 16 + lane / 16 * 4);
+    if constexpr (FEW) {
+        // row `wave` of the lane's four
+        const int64_t j = j0 + 4 * wave;
+        if (j >= m)
+            return;
+        typename Vec<float, 4>::type r;
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+            r[h] = red[h][lane][wave];
+        float *p = dw + c * m + min(j, last);
+        if (m >= 4) {
+            *reinterpret_cast<typename Vec<float, 4>::type *>(p) = r;
+        } else {
+#pragma unroll
+            for (int h = 0; h < 3; ++h)
+                if (h < m)
+                    p[h] = r[h];
+        }
     } else {
-        for (int i = 0; i < 3; ++i)
-            if (e + i < count)
-                dw[e + i] = v[i];
+        if (wave > 0)
+            return;
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w)
+            v += red[w][lane];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (j0 + 4 * e < m && i < m)
+                dw[c * m + min(j0 + 4 * e, last) + i] = v[e];
     }
 }
 
@@ -924,17 +965,60 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
     }); });
 }
 
+namespace {
+
 // Tile sides of the weight gradient: the smallest that hold the matrix, up to
 // 256.
-static int grad_tile_c(int32_t k) { return k > 128 ? 256 : 128; }
-static int grad_tile_j(int32_t m) { return m > 128 ? 256 : m > 64 ? 128 : 64; }
+int grad_tile_c(int32_t k) { return k > 128 ? 256 : 128; }
+int grad_tile_j(int32_t m) { return m > 128 ? 256 : m > 64 ? 128 : 64; }
 
 // One workgroup a compute unit.
-int32_t q8_grad_splits(int32_t n, int32_t k, int32_t m)
+int32_t grad_splits(int32_t n, int64_t tiles)
 {
-    const int tc = grad_tile_c(k), tj = grad_tile_j(m);
-    const int64_t tiles = (int64_t)((k + tc - 1) / tc) * ((m + tj - 1) / tj);
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
+}
+
+template <class T, int TC, int TJ, bool ANY>
+hipError_t weight_grad(int32_t n, int32_t k, int32_t m, const int8_t *q, int64_t ldq,
+                       const float *s, const T *dy, int64_t lddy, const T *y, int64_t ldy,
+                       float *part, float *dw, hipStream_t st)
+{
+    const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
+    const int64_t tiles = (int64_t)nc * nj;
+    const int32_t splits = grad_splits(n, tiles);
+    int64_t chunk = ((int64_t)n + splits - 1) / splits;
+    chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
+    const auto kernel = y ? k_q8_grad<T, true, TC, TJ, ANY> : k_q8_grad<T, false, TC, TJ, ANY>;
+    kernel<<<(uint32_t)(tiles * splits), kGradThreads, 0, st>>>(
+        n, k, m, chunk, splits, nc, nj, q, ldq, s, dy, lddy, y, ldy, splits > 1 ? part : dw);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || splits <= 1)
+        return e;
+    const int64_t slice = tiles * (TC * TJ / 4);
+    if (splits < kSumFew)
+        k_q8_grad_sum<TC, TJ, true><<<(uint32_t)(slice / (4 * kWave)), 4 * kWave, 0, st>>>(
+            part, splits, k, m, nj, slice, dw);
+    else
+        k_q8_grad_sum<TC, TJ, false><<<(uint32_t)(slice / kWave), kSumWaves * kWave, 0, st>>>(
+            part, splits, k, m, nj, slice, dw);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t q8_grad_floats(int32_t n, int32_t k, int32_t m)
+{
+    // with the call's tiles, or the small ones that it takes where strides are
+    // too large for them
+    size_t most = 0;
+    const int sides[2][2] = {{grad_tile_c(k), grad_tile_j(m)}, {128, 64}};
+    for (const auto &t : sides) {
+        const int64_t tiles = (int64_t)((k + t[0] - 1) / t[0]) * ((m + t[1] - 1) / t[1]);
+        const int64_t splits = grad_splits(n, tiles);
+        if (splits > 1)
+            most = std::max<size_t>(most, (size_t)(splits * tiles) * t[0] * t[1]);
+    }
+    return most;
 }
 
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
@@ -942,45 +1026,23 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
                                  const void *y, int64_t ldy, float *part, float *dw,
                                  hipStream_t st)
 {
-    const int32_t splits = q8_grad_splits(n, k, m);
-    int64_t chunk = ((int64_t)n + splits - 1) / splits;
-    chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
-    const hipError_t e = with_type(type, [&](auto tag) {
+    return with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        auto run = [&](auto tc, auto tj, auto any) {
-            constexpr int TC = decltype(tc)::value, TJ = decltype(tj)::value;
-            const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
-            constexpr bool ANY = decltype(any)::value;
-            const auto kernel = y ? k_q8_grad<T, true, TC, TJ, ANY>
-                                  : k_q8_grad<T, false, TC, TJ, ANY>;
-            kernel<<<(uint32_t)(nc * nj * splits), kGradThreads, 0, st>>>(
-                n, k, m, chunk, nc, nj, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy,
-                splits > 1 ? part : dw);
-            return hipGetLastError();
+        auto run = [&](auto f) {
+            return f(n, k, m, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy, part, dw, st);
         };
-        typedef std::integral_constant<int, 64> i64;
-        typedef std::integral_constant<int, 128> i128;
-        typedef std::integral_constant<int, 256> i256;
         const int64_t pitch = std::max<int64_t>(std::max(lddy, y ? ldy : 0) * sizeof(T), ldq);
         const int tc = grad_tile_c(k), tj = grad_tile_j(m);
-        const std::false_type no;
         if (m < 4 || (pitch + 65536 * 4) * kGradRows > UINT32_MAX)
-            return run(i128{}, i64{}, std::true_type{});
+            return run(weight_grad<T, 128, 64, true>);
         if (tc == 256)
-            return tj == 256   ? run(i256{}, i256{}, no)
-                   : tj == 128 ? run(i256{}, i128{}, no)
-                               : run(i256{}, i64{}, no);
-        return tj == 256   ? run(i128{}, i256{}, no)
-               : tj == 128 ? run(i128{}, i128{}, no)
-                           : run(i128{}, i64{}, no);
+            return tj == 256   ? run(weight_grad<T, 256, 256, false>)
+                   : tj == 128 ? run(weight_grad<T, 256, 128, false>)
+                               : run(weight_grad<T, 256, 64, false>);
+        return tj == 256   ? run(weight_grad<T, 128, 256, false>)
+               : tj == 128 ? run(weight_grad<T, 128, 128, false>)
+                           : run(weight_grad<T, 128, 64, false>);
     });
-    if (e != hipSuccess || splits <= 1)
-        return e;
-    const int64_t count = (int64_t)k * m;
-    const int waves = splits < 8 ? 1 : splits < 32 ? 4 : kSumWaves;
-    k_q8_grad_sum<<<(uint32_t)((count + 4 * kWave - 1) / (4 * kWave)), waves * kWave, 0, st>>>(
-        part, splits, count, dw);
-    return hipGetLastError();
 }
 
 }  // namespace digest
