@@ -508,6 +508,102 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
     }
 }
 
+// Many rows by a weight of at most 64 LINES of k, 16 MB channels a workgroup:
+// bound by writing y.  The weight's codes stay in LDS (in the places of
+// k_q8_gemm), and each wave takes 16 rows after another straight from memory, the
+// next ones' codes under way while these are multiplied and stored; no barrier
+// after the first.
+template <class T, int LINES, int MB, int W>
+__global__ __launch_bounds__(W *kWave) void k_q8_stream(
+    int32_t n, int32_t m, int32_t k, const int8_t *__restrict__ q, int64_t ldq,
+    const float *__restrict__ s, const int8_t *__restrict__ p, int64_t ldp,
+    const float *__restrict__ t, bool relu, T *__restrict__ y, int64_t ldy)
+{
+    static_assert(sizeof(T) == 4 || MB % 2 == 0, "pairs of blocks");
+    __shared__ i32x4 lds[LINES * MB * kWave];
+    __shared__ float lt[16 * MB];
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l = lane % 16, g = lane / 16;
+    const int64_t j0 = (int64_t)blockIdx.y * (16 * MB);
+    // the channel of row r of block b: with 16-bit outputs a pair's are dealt so
+    // that a lane holds eight in a row
+    auto channel = [](int b, int r) {
+        return sizeof(T) == 2 ? b / 2 * 32 + r / 4 * 8 + b % 2 * 4 + r % 4 : b * 16 + r;
+    };
+    const int lr = lane / 4, lc = (lane % 4 ^ lr / 2 % 4) * 16;
+    for (int i = wave; i < LINES * MB; i += W) {
+        const int64_t j = j0 + channel(i % MB, lr);
+        const int32_t c = i / MB * 64 + lc;
+        const void *from = j < m && c < k ? (const void *)(p + j * ldp + c) : (const void *)&kZeros;
+        __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)(&lds[i * kWave]), 16, 0,
+                                         0);
+    }
+    for (int i = threadIdx.x; i < 16 * MB; i += W * kWave)
+        lt[i] = j0 + i < m ? t[j0 + i] : 0.f;
+    __syncthreads();
+    const int read = l * 4 + (g ^ l / 2 % 4);
+
+    struct Rows {
+        i32x4 q[LINES];
+        float s;
+    };
+    // (codes past k meet the weight's zeros)
+    auto fetch = [&](int64_t r0, Rows &f) {
+        const int64_t r = min(r0 + l, (int64_t)n - 1);
+        f.s = s[r];
+#pragma unroll
+        for (int u = 0; u < LINES; ++u)
+            f.q[u] = *reinterpret_cast<const i32x4 *>(q + r * ldq + min(u * 64 + g * 16, k - 16));
+    };
+    const int64_t stride = (int64_t)gridDim.x * W * 16;
+    int64_t r0 = ((int64_t)blockIdx.x * W + wave) * 16;
+    Rows now, next;
+    if (r0 < n)
+        fetch(r0, now);
+    for (; r0 < n; r0 += stride) {
+        fetch(min(r0 + stride, (int64_t)n - 1), next);
+        // (the weight's codes are read again for each 16 rows, not kept in registers)
+        asm volatile("" ::: "memory");
+        i32x4 acc[MB] = {};
+#pragma unroll
+        for (int u = 0; u < LINES; ++u)
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                acc[b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(lds[(u * MB + b) * kWave + read],
+                                                               now.q[u], acc[b], 0, 0, 0);
+                if (b % 4 == 3)
+                    __builtin_amdgcn_sched_barrier(0);   // (no more reads ahead)
+            }
+        if (r0 + l < n) {
+            T *yr = y + (r0 + l) * ldy + j0;
+            // (what the stores need is formed here, not kept through the loop)
+            int32_t left = (int32_t)(m - j0);
+            int at = g;
+            asm volatile("" : "+s"(left), "+v"(at));
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int b = 0; b < MB; b += 2) {
+                    const int sum[8] = {acc[b][0], acc[b][1], acc[b][2], acc[b][3],
+                                        acc[b + 1][0], acc[b + 1][1], acc[b + 1][2],
+                                        acc[b + 1][3]};
+                    store_row(sum, now.s, lt, relu, b * 16 + at * 8, left, yr);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    const int sum[4] = {acc[b][0], acc[b][1], acc[b][2], acc[b][3]};
+                    store_row(sum, now.s, lt, relu, b * 16 + at * 4, left, yr);
+                    if (b % 4 == 3)
+                        __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        }
+        now = next;
+    }
+}
+
 // dw over rows [z chunk, (z + 1) chunk) into slice z: TC columns of codes x TJ
 // of D a workgroup of 8 waves, 32 rows a step.  The codes are exact in
 // bfloat16; s D is split into three bfloat16 by cutting off its low bits,
@@ -956,6 +1052,29 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
         typedef std::integral_constant<int, 2> i2;
         typedef std::integral_constant<int, 4> i4;
         typedef std::integral_constant<int, 8> i8;
+        typedef std::integral_constant<int, 16> i16;
+        auto stream = [&](auto lines, auto mb) {
+            constexpr int LINES = decltype(lines)::value, MB = decltype(mb)::value;
+            constexpr int W = 8;
+            const int32_t nm = (m + 16 * MB - 1) / (16 * MB);
+            const int32_t blocks = (n + 16 * W - 1) / (16 * W), most = 512;
+            const dim3 grid(std::max(1, std::min(blocks, most / nm)), nm);
+            k_q8_stream<T, LINES, MB, W><<<grid, W * kWave, 0, st>>>(n, m, k, q, ldq, s, p, ldp, t,
+                                                                    relu, out, ldy);
+            return hipGetLastError();
+        };
+        // The most channels a workgroup that leave every compute unit one (us, 256
+        // channels of 256 k, float32, with 256 / 64 channels: 2,048 rows 8.6 / 4.1,
+        // 8,192 rows 9.8 / 5.4).  Against tiles through the ring: 8,192 rows 10.4,
+        // 29,125 rows 17 against 11, 306,250 rows 140 against 89 (4.4 TB/s).
+        auto stream_lines = [&](auto lines) {
+            const int64_t blocks = (n + 127) / 128;
+            return m > 128 && blocks * ((m + 255) / 256) >= 256  ? stream(lines, i16{})
+                   : m > 64 && blocks * ((m + 127) / 128) >= 256 ? stream(lines, i8{})
+                                                                 : stream(lines, i4{});
+        };
+        if (k <= 256)
+            return k <= 128 ? stream_lines(i2{}) : stream_lines(i4{});
         const int64_t tiles = (int64_t)((m + 255) / 256) * ((n + 255) / 256);
         if (tiles >= 256 && k >= 1024)
             return gemm(i2{}, i4{}, i8{});   // 256 x 256
