@@ -325,10 +325,10 @@ __device__ __forceinline__ void store_row(const int (&sum)[N], float sr,
     }
 }
 
-// Few rows (up to 16 NT): bound by reading the weight's codes, 16 channels a
+// Few rows: bound by reading the weight's codes, 16 MT channels and 16 NT rows a
 // workgroup, its W waves a share of k each, straight from memory; the waves'
 // sums, whole numbers, are added through LDS.
-template <class T, int NT, int W>
+template <class T, int MT, int NT, int W>
 __global__ __launch_bounds__(W *kWave) void k_q8_few(int32_t n, int32_t m, int32_t k,
                                                      const int8_t *__restrict__ q, int64_t ldq,
                                                      const float *__restrict__ s,
@@ -336,42 +336,55 @@ __global__ __launch_bounds__(W *kWave) void k_q8_few(int32_t n, int32_t m, int32
                                                      const float *__restrict__ t, bool relu,
                                                      T *__restrict__ y, int64_t ldy)
 {
-    __shared__ i32x4 red[W][NT][kWave];
+    __shared__ i32x4 red[W][MT * NT][kWave];
     const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int l = lane % 16, g = lane / 16;
-    const int64_t j0 = (int64_t)blockIdx.x * 16;
+    const int64_t j0 = (int64_t)blockIdx.x * (16 * MT), r0 = (int64_t)blockIdx.y * (16 * NT);
     const i32x4 zero = {0, 0, 0, 0};
-    const int8_t *pj = p + min(j0 + l, (int64_t)m - 1) * ldp;
-    const int8_t *qr[NT];
+    const int8_t *pj[MT], *qr[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+        pj[i] = p + min(j0 + 16 * i + l, (int64_t)m - 1) * ldp;
 #pragma unroll
     for (int i = 0; i < NT; ++i)
-        qr[i] = q + min(16 * i + l, n - 1) * ldq;
-    i32x4 acc[NT] = {};
+        qr[i] = q + min(r0 + 16 * i + l, (int64_t)n - 1) * ldq;
+    i32x4 acc[MT][NT] = {};
     // (a lane's k past the end: a zero code on the weight's side is enough)
     const int32_t steps = (k + 63) / 64, each = (steps + W - 1) / W;
     const int32_t u1 = min(steps, (wave + 1) * each);
-#pragma unroll 4
+#pragma unroll(MT *NT > 4 ? 2 : 4)
     for (int32_t u = wave * each; u < u1; ++u) {
         const int32_t c = u * 64 + g * 16, at = min(c, k - 16);
-        const i32x4 a = c < k ? *reinterpret_cast<const i32x4 *>(pj + at) : zero;
+        i32x4 a[MT], b[NT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            a[i] = *reinterpret_cast<const i32x4 *>(pj[i] + at);
+            a[i] = c < k ? a[i] : zero;
+        }
 #pragma unroll
         for (int i = 0; i < NT; ++i)
-            acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(
-                a, *reinterpret_cast<const i32x4 *>(qr[i] + at), acc[i], 0, 0, 0);
+            b[i] = *reinterpret_cast<const i32x4 *>(qr[i] + at);
+#pragma unroll
+        for (int h = 0; h < MT; ++h)
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+                acc[h][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[h], b[i], acc[h][i], 0, 0, 0);
     }
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
-        red[wave][i][lane] = acc[i];
+    for (int h = 0; h < MT; ++h)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            red[wave][h * NT + i][lane] = acc[h][i];
     __syncthreads();
-    for (int i = wave; i < NT; i += W) {
-        i32x4 v = red[0][i][lane];
+    for (int x = wave; x < MT * NT; x += W) {
+        i32x4 v = red[0][x][lane];
 #pragma unroll
         for (int w = 1; w < W; ++w)
-            v += red[w][i][lane];
-        const int64_t r = 16 * i + l;
+            v += red[w][x][lane];
+        const int64_t r = r0 + x % NT * 16 + l;
         const int sum[4] = {v[0], v[1], v[2], v[3]};
         if (r < n)
-            store_row(sum, s[r], t, relu, j0 + 4 * g, m, y + r * ldy);
+            store_row(sum, s[r], t, relu, j0 + x / NT * 16 + 4 * g, m, y + r * ldy);
     }
 }
 
@@ -1030,17 +1043,25 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
         typedef typename decltype(tag)::type T;
         q += r0 * ldq, s += r0;
         T *out = (T *)y + r0 * ldy;
-        auto few = [&](auto nt) {
-            k_q8_few<T, decltype(nt)::value, 8><<<(m + 15) / 16, 8 * kWave, 0, st>>>(
-                n, m, k, q, ldq, s, p, ldp, t, relu, out, ldy);
+        auto few = [&](auto mt, auto nt) {
+            constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
+            const dim3 grid((m + 16 * MT - 1) / (16 * MT), (n + 16 * NT - 1) / (16 * NT));
+            k_q8_few<T, MT, NT, 8><<<grid, 8 * kWave, 0, st>>>(n, m, k, q, ldq, s, p, ldp, t, relu,
+                                                              out, ldy);
             return hipGetLastError();
         };
+        typedef std::integral_constant<int, 1> i1;
+        typedef std::integral_constant<int, 2> i2;
+        typedef std::integral_constant<int, 4> i4;
+        typedef std::integral_constant<int, 8> i8;
+        typedef std::integral_constant<int, 10> i10;
+        typedef std::integral_constant<int, 16> i16;
         if (n <= 16)
-            return few(std::integral_constant<int, 1>{});
+            return few(i1{}, i1{});
         if (n <= 32)
-            return few(std::integral_constant<int, 2>{});
+            return few(i1{}, i2{});
         if (n <= 64)
-            return few(std::integral_constant<int, 4>{});
+            return few(i1{}, i4{});
         auto gemm = [&](auto wm, auto wn, auto tm) {
             constexpr int WM = decltype(wm)::value, WN = decltype(wn)::value;
             constexpr int TM = decltype(tm)::value, BM = WM * TM * 16, BN = WN * 64;
@@ -1049,10 +1070,6 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
                 n, m, k, nm, q, ldq, s, p, ldp, t, relu, out, ldy);
             return hipGetLastError();
         };
-        typedef std::integral_constant<int, 2> i2;
-        typedef std::integral_constant<int, 4> i4;
-        typedef std::integral_constant<int, 8> i8;
-        typedef std::integral_constant<int, 16> i16;
         auto stream = [&](auto lines, auto mb) {
             constexpr int LINES = decltype(lines)::value, MB = decltype(mb)::value;
             constexpr int W = 8;
@@ -1075,11 +1092,28 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
         };
         if (k <= 256)
             return k <= 128 ? stream_lines(i2{}) : stream_lines(i4{});
-        const int64_t tiles = (int64_t)((m + 255) / 256) * ((n + 255) / 256);
-        if (tiles >= 256 && k >= 1024)
+        // Workgroups of a tile.  The largest tile that gives every compute unit one
+        // reads operands the fewest times (us at 256 x 256 / 128 x 128: 16,384 x 640
+        // x 4,096 bfloat16 86 / 111, 2,048 x 640 x 2,048 18 / 9; 256 x 128 / 128 x
+        // 128: 2,048 x 4,096 x 4,096 49 / 57).  Below that, weights of up to 640 k
+        // stay in LDS for few channels, whose rows are read again from L2 (29,125 x
+        // 602 x 256 float32 20.9 against 22.9, 8,192 rows 7.2 / 10.2; 2,048 x 640 x
+        // 2,048 12.7 / 8.7, hence the line at 512), and where tiles are few the
+        // waves share k (1,000 x 2,000 x 300 10.9 / 17.3, 512 x 1,024 x 1,024 8.3 /
+        // 9.9, 512 x 4,096 x 4,096, 512 workgroups, 36 / 21).
+        auto tiles = [&](int bm, int bn) {
+            return (int64_t)((m + bm - 1) / bm) * ((n + bn - 1) / bn);
+        };
+        if (tiles(256, 256) >= 256)
             return gemm(i2{}, i4{}, i8{});   // 256 x 256
+        if (k <= 640 && m <= 512)
+            return stream(i10{}, i4{});
+        if (tiles(64, 64) <= 256)
+            return few(i4{}, i4{});
+        if (tiles(256, 128) >= 192)
+            return gemm(i4{}, i2{}, i4{});   // 256 channels x 128 rows
         if (m > 64)
-            return gemm(i2{}, i2{}, i4{});   // 128 x 128
+            return gemm(i4{}, i2{}, i2{});   // 128 x 128
         return gemm(i2{}, i2{}, i2{});       // 64 channels x 128 rows
     }); });
 }

@@ -214,7 +214,11 @@ def test_product_types(n, k, m, gap, t, act):
     check_product(n, k, m, t, act, gap)
 
 
-@pytest.mark.parametrize("n,k,m", [(4100, 1040, 4099), (3900, 1216, 4352), (70000, 130, 250)])
+@pytest.mark.parametrize("n,k,m", [(4100, 1040, 4099), (3900, 1216, 4352), (70000, 130, 250),
+                                   (70000, 100, 250), (70001, 256, 40), (30000, 250, 600),
+                                   (33000, 70, 1100), (9000, 600, 500), (29125, 602, 256),
+                                   (1000, 2000, 300), (2047, 1100, 4095), (1500, 700, 1300),
+                                   (20000, 900, 33), (800, 4100, 1000)])
 def test_product_large(n, k, m):
     """Against float64 products on the GPU: sums below 2^31, exact there."""
     g = torch.Generator(device="cuda").manual_seed(n)
