@@ -637,9 +637,10 @@ digest_status digest_q8_weight_grad(int64_t n_rows, int32_t d_in, int32_t d_out,
  * level is held as codes [n_global, DIGEST_Q8_STRIDE(d_level)] (contiguous,
  * 16-byte aligned) and scales [n_global], instead of floats.  A push writes
  * the codes and scales of its rows, a pull reads the halo rows' values into
- * the halo buffer and forms the halo aggregate from them, in both pull modes
- * (in DIGEST_PULL_AGGREGATE the halo buffer may be written, but not read).  A
- * level may be pulled from either kind of store.
+ * the halo buffer and forms the halo aggregate from them, or in
+ * DIGEST_PULL_AGGREGATE forms it from the codes and scales directly (each
+ * entry's weight times the row's scale rounded to fp32, sums in fp32).  A level
+ * may be pulled from either kind of store.
  * Errors: those of digest_push and digest_pull.
  */
 digest_status digest_push_q8(digest_partition *p, int32_t level, const float *h_own,

@@ -1875,8 +1875,18 @@ digest_status partition_pull_q8(digest_partition *p, int32_t level, const int8_t
     if (!codes || !scales || (uintptr_t)codes % kQ8Align)
         return fail(DIGEST_EINVAL, "codes or scales is NULL or codes not %d-byte aligned",
                     kQ8Align);
-    if (p->n_halo > 0) {
-        const int32_t d = p->widths[level];
+    const int32_t d = p->widths[level];
+    if (p->n_halo > 0 && p->pull_mode == DIGEST_PULL_AGGREGATE) {
+        // the halo aggregate straight from the store's codes
+        Timed t(p, K_HALO_AGG, level, s);
+        if (digest_status st = hip_check(
+                ops.aggregate(p->at<SpmmBlock>(p->lay.blocks_b), (int32_t)p->blocks_b.size(),
+                              p->at<int32_t>(p->lay.b_rowptr), p->at<int32_t>(p->lay.b_gcol),
+                              p->at<float>(p->lay.b_val), codes, q8_padded(d), scales, d,
+                              p->at<float>(p->lay.hagg[level]), padded_width(d), s),
+                "halo aggregate from 8 bits"))
+            return st;
+    } else if (p->n_halo > 0) {
         {
             Timed t(p, K_PULL, level, s);
             if (digest_status st = hip_check(
@@ -1886,7 +1896,7 @@ digest_status partition_pull_q8(digest_partition *p, int32_t level, const int8_t
                     "pull from 8 bits"))
                 return st;
         }
-        if (!p->gws || p->pull_mode == DIGEST_PULL_AGGREGATE)
+        if (!p->gws)
             if (digest_status st = halo_aggregate(p, level, s))
                 return st;
     }

@@ -11,6 +11,7 @@
 #include <cfloat>
 
 #include "device.h"
+#include "kernels.h"
 #include "q8_kernels.h"
 #include "train_kernels.h"
 
@@ -288,6 +289,90 @@ __global__ __launch_bounds__(kThreads) void k_dequantize_rows(
                     if (c + j < d)
                         yr[c + j] = out[j];
             }
+        }
+    }
+}
+
+// out[r] = sum over the entries e of row r of val[e] scale[col e] codes[col e]: a
+// store's rows in 8 bits gathered into the sums that are wanted of them.  Bound
+// by the random reads of the rows.  A wave a short row, a workgroup's waves a
+// long one's entries each (the blocks of launch_spmm); GL lanes take an entry's
+// 16 GL columns, the wave's 64 / GL groups every so many'th entry, U of them
+// under way; the groups' sums, then the waves', are added in their order.
+template <int GL, int U>
+__global__ __launch_bounds__(kSpmmThreads) void k_q8_aggregate(
+    const SpmmBlock *__restrict__ blocks, const int32_t *__restrict__ rowptr,
+    const int32_t *__restrict__ col, const float *__restrict__ val,
+    const int8_t *__restrict__ codes, int64_t ldq, const float *__restrict__ scales, int32_t d,
+    float *__restrict__ out, int64_t ldo)
+{
+    constexpr int W = kSpmmThreads / kWave, G = kWave / GL;
+    __shared__ float red[W][GL * 16];
+    const SpmmBlock blk = blocks[blockIdx.x];
+    const bool whole = blk.nrows == 0;   // one long row
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int gl = lane % GL, g = lane / GL;
+    if (!whole && wave >= blk.nrows)
+        return;
+    const int32_t row = whole ? blk.row : blk.row + wave;
+    int32_t k0 = whole ? blk.kb : rowptr[row], k1 = whole ? blk.ke : rowptr[row + 1];
+    if (whole) {
+        const int32_t each = (k1 - k0 + W - 1) / W;
+        k0 = min(k1, k0 + wave * each);
+        k1 = min(k1, k0 + each);
+    }
+    for (int32_t c0 = 0; c0 < d; c0 += GL * 16) {
+        const int32_t c = c0 + gl * 16;
+        float acc[16] = {};
+        for (int32_t k = k0 + g; k < k1; k += G * U) {
+            i32x4 q[U];
+            float w[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int32_t e = k + u * G;
+                const i32x4 zero = {0, 0, 0, 0};
+                w[u] = 0.f, q[u] = zero;
+                if (e < k1) {
+                    const int64_t r = col[e];
+                    w[u] = val[e] * scales[r];
+                    if (c < d)
+                        q[u] = *reinterpret_cast<const i32x4 *>(codes + r * ldq + c);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    acc[i] = __builtin_fmaf(w[u], (float)(int8_t)(q[u][i / 4] >> (8 * (i % 4))),
+                                            acc[i]);
+        }
+#pragma unroll
+        for (int m = GL; m < kWave; m *= 2)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                acc[i] += __shfl_xor(acc[i], m);
+        float *o = out + row * ldo;
+        if (!whole) {
+            if (g == 0)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (c + i < d)
+                        o[c + i] = acc[i];
+            continue;
+        }
+        __syncthreads();
+        if (g == 0)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                red[wave][gl * 16 + i] = acc[i];
+        __syncthreads();
+        for (int i = threadIdx.x; i < GL * 16 && c0 + i < d; i += kSpmmThreads) {
+            float v = red[0][i];
+#pragma unroll
+            for (int w = 1; w < W; ++w)
+                v += red[w][i];
+            o[c0 + i] = v;
         }
     }
 }
@@ -1033,6 +1118,33 @@ hipError_t launch_dequantize_rows(int32_t type, int32_t n, int32_t d, const int8
             return run(std::integral_constant<int, 32>{});
         return run(std::integral_constant<int, 64>{});
     }); });
+}
+
+hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, const int32_t *rowptr,
+                               const int32_t *col, const float *val, const int8_t *codes,
+                               int64_t ldq, const float *scales, int32_t d, float *out,
+                               int64_t ldo, hipStream_t s)
+{
+    if (n_blocks <= 0)
+        return hipSuccess;
+    auto run = [&](auto gl, auto u) {
+        k_q8_aggregate<decltype(gl)::value, decltype(u)::value>
+            <<<n_blocks, kSpmmThreads, 0, s>>>(blocks, rowptr, col, val, codes, ldq, scales, d, out,
+                                               ldo);
+        return hipGetLastError();
+    };
+    typedef std::integral_constant<int, 2> i2;
+    typedef std::integral_constant<int, 4> i4;
+    const int32_t pieces = (d + 15) / 16;
+    if (pieces <= 4)
+        return run(i4{}, i2{});
+    if (pieces <= 8)
+        return run(std::integral_constant<int, 8>{}, i2{});
+    if (pieces <= 16)
+        return run(std::integral_constant<int, 16>{}, i4{});
+    if (pieces <= 32)
+        return run(std::integral_constant<int, 32>{}, i4{});
+    return run(std::integral_constant<int, 64>{}, i4{});
 }
 
 hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, const int8_t *q,

@@ -726,13 +726,16 @@ def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0,
 # Rows held in 8 bits.
 
 _q8 = None
+_I8 = _F32T = None   # torch.int8, torch.float32
 
 
 def _q8_lib():
     """The library with the calls on rows held in 8 bits; raises if this build
     of the ABI lacks them."""
-    global _q8
-    if _q8 is None or _q8 is not lib():
+    global _q8, _I8, _F32T
+    if _q8 is None or _q8 is not _lib:
+        import torch
+        _I8, _F32T = torch.int8, torch.float32
         L = lib()
         P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         sig = {
@@ -761,12 +764,25 @@ def digest_q8_stride(width):
     return (int(width) + 15) // 16 * 16
 
 
+# (The checks below take the common case first, a contiguous tensor of what is
+# asked for: they cost as much as a launch.)
+
+def _row_array(t, shape, dtype, dev, name):
+    """As _rows."""
+    if (getattr(t, "dtype", None) is dtype and t.shape == shape and t.get_device() == dev and
+            t.is_contiguous()):
+        return t.data_ptr(), shape[1]
+    return _rows(t, shape, dtype, dev, name)
+
+
 def _codes(t, scales, n, width, dev, name, scales_name):
     """(pointer, row stride, pointer of the scales) of the codes [n,
     digest_q8_stride(width)] and scales [n] of n rows."""
-    import torch
-    return (*_rows(t, (n, digest_q8_stride(width)), torch.int8, dev, name),
-            _need(_floats(scales, n, dev, scales_name), scales_name))
+    p, ld = _row_array(t, (n, (width + 15) // 16 * 16), _I8, dev, name)
+    if (getattr(scales, "dtype", None) is _F32T and scales.numel() == n and
+            scales.get_device() == dev and scales.is_contiguous()):
+        return p, ld, scales.data_ptr()
+    return p, ld, _need(_floats(scales, n, dev, scales_name), scales_name)
 
 
 def _need(p, name):
@@ -792,38 +808,38 @@ def digest_quantize_rows(x, codes, scales, rows=None, stream=None):
     """codes, scales = the rows of x [m, d] (those that rows, int64, lists, in
     its order) held in 8 bits: codes int8 [n, digest_q8_stride(d)], scales
     float32 [n]."""
-    dev = _device()
+    L, dev = _q8_lib(), _device()
     shape, dtype = _matrix(x, dev, "x")
     m, d = shape
     n = m if rows is None else rows.numel()
-    px, ldx = _rows(x, shape, dtype, dev, "x")
+    px, ldx = _row_array(x, shape, dtype, dev, "x")
     pq, ldq, ps = _codes(codes, scales, n, d, dev, "codes", "scales")
-    _check(_q8_lib().digest_quantize_rows(n, d, _TYPES[dtype], px, ldx, _list(rows, n, dev), m, pq,
+    _check(L.digest_quantize_rows(n, d, _TYPES[dtype], px, ldx, _list(rows, n, dev), m, pq,
                                           ldq, ps, _stream(stream)))
 
 
 def digest_quantize_columns(w, codes, scales, stream=None):
     """codes, scales = the columns of w [k, m] held in 8 bits: codes int8 [m,
     digest_q8_stride(k)], scales float32 [m]."""
-    dev = _device()
+    L, dev = _q8_lib(), _device()
     shape, dtype = _matrix(w, dev, "w")
     k, m = shape
-    pw, ldw = _rows(w, shape, dtype, dev, "w")
+    pw, ldw = _row_array(w, shape, dtype, dev, "w")
     pq, ldq, ps = _codes(codes, scales, m, k, dev, "codes", "scales")
-    _check(_q8_lib().digest_quantize_columns(k, m, _TYPES[dtype], pw, ldw, pq, ldq, ps,
+    _check(L.digest_quantize_columns(k, m, _TYPES[dtype], pw, ldw, pq, ldq, ps,
                                              _stream(stream)))
 
 
 def digest_dequantize_rows(codes, scales, y, rows=None, stream=None):
     """y [n, d] = the values of the rows (those that rows, int64, lists, in its
     order) that codes [m, digest_q8_stride(d)] and scales [m] hold."""
-    dev = _device()
+    L, dev = _q8_lib(), _device()
     shape, dtype = _matrix(y, dev, "y")
     n, d = shape
     m = n if rows is None else codes.shape[0]
     pq, ldq, ps = _codes(codes, scales, m, d, dev, "codes", "scales")
-    py, ldy = _rows(y, shape, dtype, dev, "y")
-    _check(_q8_lib().digest_dequantize_rows(n, d, pq, ldq, ps, _list(rows, n, dev), m,
+    py, ldy = _row_array(y, shape, dtype, dev, "y")
+    _check(L.digest_dequantize_rows(n, d, pq, ldq, ps, _list(rows, n, dev), m,
                                             _TYPES[dtype], py, ldy, _stream(stream)))
 
 
@@ -831,14 +847,14 @@ def digest_q8_product(codes, scales, w_codes, w_scales, y, act=ACT_IDENTITY, str
     """y [n, d_out] = act(the product of the rows in 8 bits (codes [n, k], scales
     [n]) by the weight matrix whose columns w_codes [d_out, k], w_scales [d_out]
     hold)."""
-    dev = _device()
+    L, dev = _q8_lib(), _device()
     shape, dtype = _matrix(y, dev, "y")
     n, m = shape
     k = codes.shape[-1]
     pq, ldq, ps = _codes(codes, scales, n, k, dev, "codes", "scales")
     pw, ldw, pt = _codes(w_codes, w_scales, m, k, dev, "w_codes", "w_scales")
-    py, ldy = _rows(y, shape, dtype, dev, "y")
-    _check(_q8_lib().digest_q8_product(n, k, m, pq, ldq, ps, pw, ldw, pt, act, _TYPES[dtype], py,
+    py, ldy = _row_array(y, shape, dtype, dev, "y")
+    _check(L.digest_q8_product(n, k, m, pq, ldq, ps, pw, ldw, pt, act, _TYPES[dtype], py,
                                        ldy, _stream(stream)))
 
 
@@ -855,19 +871,19 @@ def digest_q8_weight_grad(codes, scales, dy, dw, workspace, act=ACT_IDENTITY, y=
     digest_q8_stride(d_in)] and scales [n] hold, times dy [n, d_out], with
     ACT_RELU masked by y > 0; workspace: a CUDA tensor of at least
     digest_q8_weight_grad_query(n, d_in, d_out) bytes."""
-    dev = _device()
+    L, dev = _q8_lib(), _device()
     shape, dtype = _matrix(dy, dev, "dy")
     n, m = shape
     if getattr(dw, "ndim", 0) != 2 or dw.shape[1] != m:
         raise ValueError(f"dw must be [d_in, {m}]")
     k = dw.shape[0]
     pq, ldq, ps = _codes(codes, scales, n, k, dev, "codes", "scales")
-    pdy, lddy = _rows(dy, shape, dtype, dev, "dy")
+    pdy, lddy = _row_array(dy, shape, dtype, dev, "dy")
     if act == ACT_RELU and y is None:
         raise ValueError("y is required with ACT_RELU")
-    py, ldy = _rows(y, shape, dtype, dev, "y") if act == ACT_RELU else (None, 0)
+    py, ldy = _row_array(y, shape, dtype, dev, "y") if act == ACT_RELU else (None, 0)
     ws, nbytes = _workspace(workspace, dev)
-    _check(_q8_lib().digest_q8_weight_grad(n, k, m, pq, ldq, ps, _TYPES[dtype], pdy, lddy, act,
+    _check(L.digest_q8_weight_grad(n, k, m, pq, ldq, ps, _TYPES[dtype], pdy, lddy, act,
                                            py, ldy, _floats(dw, k * m, dev, "dw"), ws, nbytes,
                                            _stream(stream)))
 

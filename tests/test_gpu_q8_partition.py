@@ -51,7 +51,7 @@ def held_rows(x):
     return codes, scales
 
 
-def values(codes, scales, d):
+def values_of(codes, scales, d):
     return codes[:, :d].double() * scales.double()[:, None]
 
 
@@ -81,7 +81,7 @@ def test_pull(d, pull_mode):
     p, dense = make(widths=(d, d, 4), pull_mode=pull_mode)
     codes, scales = held_rows(rnd(p.n_global, d, seed=1))
     D.digest_pull_q8(p, 0, codes, scales)
-    halo = values(codes, scales, d)[p.n_own + 50:]
+    halo = values_of(codes, scales, d)[p.n_own + 50:]
     if pull_mode == D.PULL_ROWS:
         out = torch.empty(p.n_halo, d, device="cuda")
         D.digest_partition_read_halo(p, 0, out)
@@ -97,8 +97,45 @@ def test_pull(d, pull_mode):
     assert bool((err <= 220 * U * size + 1e-30).all()), float((err / size.clamp_min(1e-30)).max())
 
 
-def test_pull_of_rows_that_are_nan():
-    p, dense = make(widths=(12, 9, 4))
+@pytest.mark.parametrize("pull_mode", [D.PULL_ROWS, D.PULL_AGGREGATE])
+@pytest.mark.parametrize("d", [3, 47, 64, 65, 256, 602, 1100])
+def test_pull_of_long_rows(d, pull_mode):
+    """Rows of up to 1,000 halo entries, repeated ones among them, and one without
+    an entry; the same bits each time."""
+    rng = np.random.default_rng(d)
+    n, n_halo = 40, 500
+    deg = np.array([0, 1, 2, 63, 64, 65, 66, 500, 511, 512, 513, 1000] + [5] * (n - 12))
+    cols = n + rng.integers(0, n_halo, deg.sum())
+    indptr = np.concatenate([[0], np.cumsum(deg)])
+    values = rng.uniform(-1, 1, deg.sum()).astype(np.float32)
+    p = D.digest_partition_create(n + n_halo, indptr, cols, values, np.arange(n),
+                                  np.arange(n, n + n_halo), [d, 5])
+    D.digest_partition_set_pull_mode(p, pull_mode)
+    bind(p)
+    codes, scales = held_rows(rnd(p.n_global, d, seed=1))
+    dense = np.zeros((n, n_halo))
+    np.add.at(dense, (np.repeat(np.arange(n), deg), cols - n), values)
+    size = np.zeros((n, n_halo))
+    np.add.at(size, (np.repeat(np.arange(n), deg), cols - n), np.abs(values))
+    halo = values_of(codes, scales, d)[n:].cpu()
+    want, size = torch.from_numpy(dense) @ halo, torch.from_numpy(size) @ halo.abs()
+    w = rnd(d, 5, seed=2)
+    h = torch.zeros(n, d, device="cuda")
+    ys = []
+    for _ in range(2):
+        D.digest_pull_q8(p, 0, codes, scales)
+        ys.append(torch.empty(n, 5, device="cuda"))
+        D.digest_layer_forward(p, 1, h, w, ys[-1], D.ACT_IDENTITY)
+    assert torch.equal(*ys)
+    W = w.cpu().double()
+    # terms rounded three times at most, 1,001 sums, then the product over d
+    bound = (1010 + d) * U * (size @ W.abs())
+    assert bool(((ys[0].cpu().double() - want @ W).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("pull_mode", [D.PULL_ROWS, D.PULL_AGGREGATE])
+def test_pull_of_rows_that_are_nan(pull_mode):
+    p, dense = make(widths=(12, 9, 4), pull_mode=pull_mode)
     x = rnd(p.n_global, 12)
     x[50 + p.n_own + 4, 3] = float("inf")
     D.digest_pull_q8(p, 0, *held_rows(x))
@@ -197,7 +234,7 @@ def test_forward_q8(n, d, act, halo):
     fwd = lambda y: D.digest_layer_forward_q8(p, 2, h, *wq, y, act)
     outs = run_layer(p, 2, h, w, dy, fwd, act, halo)
     y, dw, dh = outs[:3]
-    W = values(*wq, d).cpu().t()
+    W = values_of(*wq, d).cpu().t()
     want = torch.mm(A, W)
     size = torch.mm(A.abs(), W.abs())
     got = y.cpu().double()
