@@ -1881,7 +1881,7 @@ digest_status partition_pull_q8(digest_partition *p, int32_t level, const int8_t
         Timed t(p, K_HALO_AGG, level, s);
         if (digest_status st = hip_check(
                 ops.aggregate(p->at<SpmmBlock>(p->lay.blocks_b), (int32_t)p->blocks_b.size(),
-                              p->at<int32_t>(p->lay.b_rowptr), p->at<int32_t>(p->lay.b_gcol),
+                              p->long_b, p->at<int32_t>(p->lay.b_rowptr), p->at<int32_t>(p->lay.b_gcol),
                               p->at<float>(p->lay.b_val), codes, q8_padded(d), scales, d,
                               p->at<float>(p->lay.hagg[level]), padded_width(d), s),
                 "halo aggregate from 8 bits"))

@@ -40,12 +40,14 @@ hipError_t launch_dequantize_rows(int32_t type, int32_t n, int32_t d, const int8
                                   int64_t ldq, const float *scales, RowList src, int64_t n_x,
                                   void *y, int64_t ldy, hipStream_t s);
 // out[r] = sum over row r's entries of val scale codes[col] for the rows that
-// the blocks name (as launch_spmm), out rows ldo apart.
+// the blocks name (as launch_spmm, the n_long long rows first); out is 16-byte
+// aligned, its rows ldo apart, a multiple of 4 and at least d, and written up
+// to the next multiple of 4 columns.
 struct SpmmBlock;
-hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, const int32_t *rowptr,
-                               const int32_t *col, const float *val, const int8_t *codes,
-                               int64_t ldq, const float *scales, int32_t d, float *out,
-                               int64_t ldo, hipStream_t s);
+hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, int32_t n_long,
+                               const int32_t *rowptr, const int32_t *col, const float *val,
+                               const int8_t *codes, int64_t ldq, const float *scales, int32_t d,
+                               float *out, int64_t ldo, hipStream_t s);
 // y[r][j] = act(s_r t_j sum_c q[r][c] p[j][c]) over k columns of codes, k a
 // multiple of kQ8Align and at most 65536.
 hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, const int8_t *q,

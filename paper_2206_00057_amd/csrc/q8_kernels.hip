@@ -295,33 +295,81 @@ __global__ __launch_bounds__(kThreads) void k_dequantize_rows(
 
 // out[r] = sum over the entries e of row r of val[e] scale[col e] codes[col e]: a
 // store's rows in 8 bits gathered into the sums that are wanted of them.  Bound
-// by the random reads of the rows.  A wave a short row, a workgroup's waves a
-// long one's entries each (the blocks of launch_spmm); GL lanes take an entry's
-// 16 GL columns, the wave's 64 / GL groups every so many'th entry, U of them
-// under way; the groups' sums, then the waves', are added in their order.
-template <int GL, int U>
-__global__ __launch_bounds__(kSpmmThreads) void k_q8_aggregate(
+// by the latency of few random reads a row.  GL lanes take a row's 16 GL
+// columns.  Short rows (the blocks' runs of at most 8): all of one by GL
+// lanes, which first fetch GL entries with their scales at once and then the
+// entries' codes, U under way.  (A wave a row with the entries dealt to its
+// groups of lanes: 492 us against 260 for 304,051 rows of 256 columns with 7.5
+// entries each; from a float32 store 404.)
+template <int GL>
+__global__ __launch_bounds__(8 * GL) void k_q8_aggregate(
     const SpmmBlock *__restrict__ blocks, const int32_t *__restrict__ rowptr,
     const int32_t *__restrict__ col, const float *__restrict__ val,
     const int8_t *__restrict__ codes, int64_t ldq, const float *__restrict__ scales, int32_t d,
     float *__restrict__ out, int64_t ldo)
 {
-    constexpr int W = kSpmmThreads / kWave, G = kWave / GL;
+    constexpr int U = 4;
+    const SpmmBlock blk = blocks[blockIdx.x];
+    const int gl = threadIdx.x % GL, g = threadIdx.x / GL;
+    if (g >= blk.nrows)
+        return;
+    const int32_t row = blk.row + g, k0 = rowptr[row], k1 = rowptr[row + 1];
+    for (int32_t c0 = 0; c0 < d; c0 += GL * 16) {
+        const int32_t c = c0 + gl * 16;
+        float acc[16] = {};
+        for (int32_t kb = k0; kb < k1; kb += GL) {
+            const int32_t mine = kb + gl < k1 ? col[kb + gl] : 0;
+            const float w_mine = kb + gl < k1 ? val[kb + gl] * scales[mine] : 0.f;
+            const int count = min(GL, k1 - kb);
+            for (int j = 0; j < count; j += U) {
+                i32x4 q[U];
+                float w[U];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int at = min(j + u, GL - 1);
+                    const int64_t r = __shfl(mine, at, GL);
+                    w[u] = __shfl(w_mine, at, GL);
+                    const i32x4 zero = {0, 0, 0, 0};
+                    q[u] = zero;
+                    if (j + u >= count)
+                        w[u] = 0.f;
+                    else if (c < d)
+                        q[u] = *reinterpret_cast<const i32x4 *>(codes + r * ldq + c);
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        acc[i] = __builtin_fmaf(
+                            w[u], (float)(int8_t)(q[u][i / 4] >> (8 * (i % 4))), acc[i]);
+            }
+        }
+        // (rows of out are 16-byte aligned: d rounded up to 4 floats apart)
+        float *o = out + row * ldo + c;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4)
+            if (c + i < d)
+                *reinterpret_cast<f32x4 *>(o + i) = f32x4{acc[i], acc[i + 1], acc[i + 2],
+                                                          acc[i + 3]};
+    }
+}
+
+// The long rows, a workgroup each: its waves a run of entries, GL lanes every
+// 64 / GL-th of them; the lanes' groups' sums, then the waves', are added in their
+// order.
+template <int GL>
+__global__ __launch_bounds__(kSpmmThreads) void k_q8_aggregate_long(
+    const SpmmBlock *__restrict__ blocks, const int32_t *__restrict__ col,
+    const float *__restrict__ val, const int8_t *__restrict__ codes, int64_t ldq,
+    const float *__restrict__ scales, int32_t d, float *__restrict__ out, int64_t ldo)
+{
+    constexpr int W = kSpmmThreads / kWave, G = kWave / GL, U = 4;
     __shared__ float red[W][GL * 16];
     const SpmmBlock blk = blocks[blockIdx.x];
-    const bool whole = blk.nrows == 0;   // one long row
-    const int lane = threadIdx.x % kWave;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
     const int gl = lane % GL, g = lane / GL;
-    if (!whole && wave >= blk.nrows)
-        return;
-    const int32_t row = whole ? blk.row : blk.row + wave;
-    int32_t k0 = whole ? blk.kb : rowptr[row], k1 = whole ? blk.ke : rowptr[row + 1];
-    if (whole) {
-        const int32_t each = (k1 - k0 + W - 1) / W;
-        k0 = min(k1, k0 + wave * each);
-        k1 = min(k1, k0 + each);
-    }
+    const int32_t each = (blk.ke - blk.kb + W - 1) / W;
+    const int32_t k0 = min(blk.ke, blk.kb + wave * each), k1 = min(blk.ke, k0 + each);
     for (int32_t c0 = 0; c0 < d; c0 += GL * 16) {
         const int32_t c = c0 + gl * 16;
         float acc[16] = {};
@@ -352,15 +400,6 @@ __global__ __launch_bounds__(kSpmmThreads) void k_q8_aggregate(
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 acc[i] += __shfl_xor(acc[i], m);
-        float *o = out + row * ldo;
-        if (!whole) {
-            if (g == 0)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (c + i < d)
-                        o[c + i] = acc[i];
-            continue;
-        }
         __syncthreads();
         if (g == 0)
 #pragma unroll
@@ -372,7 +411,7 @@ __global__ __launch_bounds__(kSpmmThreads) void k_q8_aggregate(
 #pragma unroll
             for (int w = 1; w < W; ++w)
                 v += red[w][i];
-            o[c0 + i] = v;
+            out[blk.row * ldo + c0 + i] = v;
         }
     }
 }
@@ -639,6 +678,7 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
     }
     for (int i = threadIdx.x; i < 16 * MB; i += W * kWave)
         lt[i] = j0 + i < m ? t[j0 + i] : 0.f;
+    __builtin_amdgcn_s_waitcnt(0);   // (the loads to LDS)
     __syncthreads();
     const int read = l * 4 + (g ^ l / 2 % 4);
 
@@ -1120,31 +1160,28 @@ hipError_t launch_dequantize_rows(int32_t type, int32_t n, int32_t d, const int8
     }); });
 }
 
-hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, const int32_t *rowptr,
-                               const int32_t *col, const float *val, const int8_t *codes,
-                               int64_t ldq, const float *scales, int32_t d, float *out,
-                               int64_t ldo, hipStream_t s)
+hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, int32_t n_long,
+                               const int32_t *rowptr, const int32_t *col, const float *val,
+                               const int8_t *codes, int64_t ldq, const float *scales, int32_t d,
+                               float *out, int64_t ldo, hipStream_t s)
 {
-    if (n_blocks <= 0)
-        return hipSuccess;
-    auto run = [&](auto gl, auto u) {
-        k_q8_aggregate<decltype(gl)::value, decltype(u)::value>
-            <<<n_blocks, kSpmmThreads, 0, s>>>(blocks, rowptr, col, val, codes, ldq, scales, d, out,
-                                               ldo);
+    auto run = [&](auto gl) {
+        constexpr int GL = decltype(gl)::value;
+        if (n_long > 0)
+            k_q8_aggregate_long<GL><<<n_long, kSpmmThreads, 0, s>>>(blocks, col, val, codes, ldq,
+                                                                   scales, d, out, ldo);
+        if (hipError_t e = hipGetLastError())
+            return e;
+        if (n_blocks > n_long)
+            k_q8_aggregate<GL><<<n_blocks - n_long, 8 * GL, 0, s>>>(
+                blocks + n_long, rowptr, col, val, codes, ldq, scales, d, out, ldo);
         return hipGetLastError();
     };
-    typedef std::integral_constant<int, 2> i2;
-    typedef std::integral_constant<int, 4> i4;
     const int32_t pieces = (d + 15) / 16;
-    if (pieces <= 4)
-        return run(i4{}, i2{});
-    if (pieces <= 8)
-        return run(std::integral_constant<int, 8>{}, i2{});
-    if (pieces <= 16)
-        return run(std::integral_constant<int, 16>{}, i4{});
-    if (pieces <= 32)
-        return run(std::integral_constant<int, 32>{}, i4{});
-    return run(std::integral_constant<int, 64>{}, i4{});
+    return pieces <= 8    ? run(std::integral_constant<int, 8>{})
+           : pieces <= 16 ? run(std::integral_constant<int, 16>{})
+           : pieces <= 32 ? run(std::integral_constant<int, 32>{})
+                          : run(std::integral_constant<int, 64>{});
 }
 
 hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, const int8_t *q,

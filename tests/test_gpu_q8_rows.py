@@ -434,6 +434,52 @@ def test_run_of_them():
     assert bool(((dw.cpu().double() - want).abs() <= 2 * 302 * U * size).all())
 
 
+def test_two_streams_at_once():
+    """Calls on two streams over the same inputs, each with its outputs and workspace."""
+    g = torch.Generator(device="cuda").manual_seed(13)
+    n, k, m = 20000, 300, 256
+    q, s = random_codes(n, k, g)
+    p, t = random_codes(m, k, g)
+    dy = torch.randn(n, m, generator=g, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [(torch.zeros(n, m, device="cuda"), torch.zeros(k, m, device="cuda"),
+             workspace(n, k, m)) for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for st, (y, dw, ws) in zip(streams, outs):
+            D.digest_q8_product(q, s, p, t, y, D.ACT_RELU, stream=st)
+            D.digest_q8_weight_grad(q, s, dy, dw, ws, D.ACT_RELU, y, stream=st)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    want, size = grad_reference(q[:, :k], s, dy, outs[0][0])
+    assert bool(((outs[0][1].cpu().double() - want).abs() <= 2 * (n + 2) * U * size).all())
+
+
+def test_offsets_past_32_bits():
+    """Codes, rows and outputs beyond 4 GB."""
+    n, d = 1100, 2_000_000
+    base = torch.empty(n * d, dtype=torch.int8, device="cuda")      # 2.2 GB
+    codes = base.view(n, d)[:, :48]
+    whole = torch.empty(n * d, device="cuda")                       # 8.8 GB
+    x, y = whole.view(n, d)[:, :47], whole.view(n, d)[:, 1000:1047]
+    x.copy_(torch.randn(n, 47, generator=torch.Generator(device="cuda").manual_seed(2),
+                        device="cuda"))
+    scales = torch.empty(n, device="cuda")
+    plain, ps = quantize(x.contiguous())
+    D.digest_quantize_rows(x, codes, scales)
+    assert torch.equal(codes, plain) and torch.equal(scales, ps)
+    D.digest_dequantize_rows(codes, scales, y)
+    back = torch.empty(n, 47, device="cuda")
+    D.digest_dequantize_rows(plain, ps, back)
+    assert torch.equal(y, back)
+    w, t = random_codes(40, 47, torch.Generator(device="cuda").manual_seed(3))
+    out = whole.view(n, d)[:, 5000:5040]
+    D.digest_q8_product(codes, scales, w, t, out)
+    near = torch.empty(n, 40, device="cuda")
+    D.digest_q8_product(plain, ps, w, t, near)
+    assert torch.equal(out, near)
+
+
 def test_binding_refuses():
     x = torch.randn(8, 20, device="cuda")
     codes = torch.zeros(8, 32, dtype=torch.int8, device="cuda")
