@@ -965,6 +965,120 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     }
 }
 
+// Few rows: 64 columns of codes x 64 of D a workgroup, its 8 waves a run of the
+// rows each, straight from memory into the matrix instructions' operands (four
+// columns a lane and load, as above); the waves' sums are added in their order
+// through LDS, and dw is written at once.
+template <class T, bool RELU>
+__global__ __launch_bounds__(kGradThreads) void k_q8_grad_few(
+    int32_t n, int32_t k, int32_t m, const int8_t *__restrict__ q, int64_t ldq,
+    const float *__restrict__ s, const T *__restrict__ dy, int64_t lddy, const T *__restrict__ y,
+    int64_t ldy, float *__restrict__ dw)
+{
+    constexpr int W = kGradThreads / kWave;
+    typedef typename Vec<T, 4>::type vec;
+    __shared__ f32x4 red[W][4][4][kWave];
+    const int lane = threadIdx.x % kWave;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int l = lane % 16, g = lane / 16;
+    const int64_t c0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
+    const int64_t last = max(m - 4, 0);
+    const int64_t jd = min(j0 + 4 * l, last), cc = min(c0 + 4 * l, (int64_t)q8_padded(k) - 4);
+    const int64_t each = ((int64_t)n + W * kGradRows - 1) / (W * kGradRows) * kGradRows;
+    const int64_t rb = wave * each, re = min((int64_t)n, rb + each);
+    f32x4 acc[4][4] = {};
+    for (int64_t r0 = rb; r0 < re; r0 += kGradRows) {
+        vec d[8], h[RELU ? 8 : 1];
+        uint32_t c[8];
+        float sr[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            // (rows past the end repeat the last one, with codes of zero)
+            const bool there = r0 + g * 8 + e < re;
+            const int64_t r = min(r0 + g * 8 + e, re - 1);
+            sr[e] = s[r];
+            c[e] = there ? *reinterpret_cast<const uint32_t *>(q + r * ldq + cc) : 0;
+            if (m >= 4) {
+                d[e] = *reinterpret_cast<const vec *>(dy + r * lddy + jd);
+                if constexpr (RELU)
+                    h[e] = *reinterpret_cast<const vec *>(y + r * ldy + jd);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    d[e][i] = dy[r * lddy + min(i, m - 1)];
+                    if constexpr (RELU)
+                        h[e][i] = y[r * ldy + min(i, m - 1)];
+                }
+            }
+        }
+        bf16x8 cf[4];
+#pragma unroll
+        for (int o = 0; o < 4; ++o)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                cf[o][e] = (__bf16)(float)(int8_t)(c[e] >> (8 * o));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf16x8 a[3];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float D = (float)d[e][i];
+                if constexpr (RELU)
+                    if (!((float)h[e][i] > 0.f))
+                        D = 0.f;
+                D *= sr[e];
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    const uint32_t top = __float_as_uint(D) & 0xffff0000u;
+                    a[p][e] = __builtin_bit_cast(__bf16, (uint16_t)(top >> 16));
+                    D -= __uint_as_float(top);
+                }
+            }
+#pragma unroll
+            for (int p = 2; p >= 0; --p)
+#pragma unroll
+                for (int o = 0; o < 4; ++o)
+                    acc[o][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[p], cf[o], acc[o][i], 0,
+                                                                        0, 0);
+        }
+    }
+#pragma unroll
+    for (int o = 0; o < 4; ++o)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            red[wave][o][i][lane] = acc[o][i];
+    __syncthreads();
+    if (wave >= 4)
+        return;
+    f32x4 v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = red[0][wave][i][lane];
+#pragma unroll
+        for (int w = 1; w < W; ++w)
+            v[i] += red[w][wave][i][lane];
+    }
+    const int64_t c = c0 + 4 * l + wave;
+    if (c >= k)
+        return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int64_t j = j0 + 4 * (g * 4 + e);
+        float *p = dw + c * m + min(j, last);
+        if (j >= m)
+            continue;
+        if (m >= 4) {
+            const typename Vec<float, 4>::type r = {v[0][e], v[1][e], v[2][e], v[3][e]};
+            *reinterpret_cast<typename Vec<float, 4>::type *>(p) = r;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < m)
+                    p[i] = v[i][e];
+        }
+    }
+}
+
 // dw = the sum of the slices, each tile's vectors as k_q8_grad's lanes hold them.
 // Many slices (FEW false): 64 vectors a workgroup, whose 16 waves sum a run of
 // slices each, in their order, and then the waves' sums in theirs.  Few: 256
@@ -1274,10 +1388,32 @@ namespace {
 int grad_tile_c(int32_t k) { return k > 128 ? 256 : 128; }
 int grad_tile_j(int32_t m) { return m > 128 ? 256 : m > 64 ? 128 : 64; }
 
-// One workgroup a compute unit.
-int32_t grad_splits(int32_t n, int64_t tiles)
+// Few rows go without slices (k_q8_grad_few), one workgroup for 64 x 64 of dw
+// (us with slices / without: 500 x 64 x 16 float32 9.5 / 7.2, 20 x 1,000 x 1,000 14 /
+// 6.1, 500 x 256 x 256 15.4 / 7.7, 1,000 x 1,024 x 1,024 bfloat16 27 / 15, 2,000 rows
+// 35 / 25; but 1,000 x 256 x 256 15.7 / 16.7, 2,000 x 602 x 256 20 / 30: few tiles
+// of more rows; 1 x 2,000 x 2,000 16 / 19, 1,000 x 4,096 x 4,096 98 / 199: many tiles).
+bool grad_few(int32_t n, int32_t k, int32_t m)
 {
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
+    const int64_t tiles = (int64_t)((k + 63) / 64) * ((m + 63) / 64);
+    return tiles <= 512 && (n <= 512 || (n <= 2048 && tiles >= 64));
+}
+
+// Slices of the rows: at most one workgroup a compute unit, and fewer where the
+// slices' sums would cost more (written and read once each at about 4.5 TB/s,
+// floats of a slice) than the steps that they save (about 2 us each).
+int32_t grad_splits(int32_t n, int64_t tiles, int64_t floats)
+{
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
+    int64_t best = 1;
+    double least = 0;
+    for (int64_t z = 1; z <= most; ++z) {
+        const int64_t steps = ((int64_t)n + z * kGradRows - 1) / (z * kGradRows);
+        const double us = 2.0 * steps + (z > 1 ? 4.0 + z * floats * 8 / 4.5e6 : 0.0);
+        if (z == 1 || us < least)
+            best = z, least = us;
+    }
+    return (int32_t)best;
 }
 
 template <class T, int TC, int TJ, bool ANY>
@@ -1287,7 +1423,7 @@ hipError_t weight_grad(int32_t n, int32_t k, int32_t m, const int8_t *q, int64_t
 {
     const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
     const int64_t tiles = (int64_t)nc * nj;
-    const int32_t splits = grad_splits(n, tiles);
+    const int32_t splits = grad_splits(n, tiles, tiles * TC * TJ);
     int64_t chunk = ((int64_t)n + splits - 1) / splits;
     chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
     const auto kernel = y ? k_q8_grad<T, true, TC, TJ, ANY> : k_q8_grad<T, false, TC, TJ, ANY>;
@@ -1310,13 +1446,15 @@ hipError_t weight_grad(int32_t n, int32_t k, int32_t m, const int8_t *q, int64_t
 
 size_t q8_grad_floats(int32_t n, int32_t k, int32_t m)
 {
+    if (grad_few(n, k, m))
+        return 0;
     // with the call's tiles, or the small ones that it takes where strides are
     // too large for them
     size_t most = 0;
     const int sides[2][2] = {{grad_tile_c(k), grad_tile_j(m)}, {128, 64}};
     for (const auto &t : sides) {
         const int64_t tiles = (int64_t)((k + t[0] - 1) / t[0]) * ((m + t[1] - 1) / t[1]);
-        const int64_t splits = grad_splits(n, tiles);
+        const int64_t splits = grad_splits(n, tiles, tiles * t[0] * t[1]);
         if (splits > 1)
             most = std::max<size_t>(most, (size_t)(splits * tiles) * t[0] * t[1]);
     }
@@ -1333,6 +1471,12 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
         auto run = [&](auto f) {
             return f(n, k, m, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy, part, dw, st);
         };
+        if (grad_few(n, k, m)) {
+            const auto kernel = y ? k_q8_grad_few<T, true> : k_q8_grad_few<T, false>;
+            kernel<<<dim3((k + 63) / 64, (m + 63) / 64), kGradThreads, 0, st>>>(
+                n, k, m, q, ldq, s, (const T *)dy, lddy, (const T *)y, ldy, dw);
+            return hipGetLastError();
+        }
         const int64_t pitch = std::max<int64_t>(std::max(lddy, y ? ldy : 0) * sizeof(T), ldq);
         const int tc = grad_tile_c(k), tj = grad_tile_j(m);
         if (m < 4 || (pitch + 65536 * 4) * kGradRows > UINT32_MAX)

@@ -305,16 +305,18 @@ def test_weight_grad(n, k, m):
 @pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("relu", [0, 1])
 @pytest.mark.parametrize("n,k,m,gap", [(500, 64, 16, 0), (700, 602, 256, 3), (5000, 256, 256, 0),
-                                       (333, 1025, 130, 2), (3000, 47, 33, 1), (64, 40, 1030, 5),
+                                       (333, 1025, 130, 2), (3000, 47, 33, 1), (64, 40, 1030, 5), (1500, 700, 600, 1),
+                                       (30, 2000, 1900, 0),
                                        (20000, 20, 300, 0)])
 def test_weight_grad_types(n, k, m, gap, t, relu):
     check_grad(n, k, m, t, relu, gap)
 
 
 @pytest.mark.parametrize("relu", [0, 1])
-def test_weight_grad_of_far_rows(relu):
+@pytest.mark.parametrize("n", [70, 530])
+def test_weight_grad_of_far_rows(n, relu):
     """Rows 128 MB apart: 32 of them pass 4 GB."""
-    n, k, m, ld = 70, 50, 90, 2 ** 25
+    n, k, m, ld = n, 50, 90, 2 ** 25
     g = torch.Generator(device="cuda").manual_seed(1)
     q, s = random_codes(n, k, g)
     whole = torch.empty(n * ld, device="cuda")

@@ -32,12 +32,12 @@ for trial in range(2000):
         ldq = min(ldq, 2 ** 31 - 16)
     t = int(rng.integers(0, 3))
     # a byte too small
-    st = L.digest_q8_weight_grad(n, k, m, at(1), ldq, at(2), t, at(3), ld, 0, None, 0, at(4), at(5),
+    st = L.digest_q8_weight_grad(n, k, m, at(1), ldq, at(2), t, at(3), ld, 1, None, 0, at(4), at(5),
                                  need - 1, None)
     assert st == D.ENOMEM, st
     # outputs on inputs, at their last element
     last = ((n - 1) * ldq + D.digest_q8_stride(k) - 1) // 4 * 4
-    st = L.digest_q8_weight_grad(n, k, m, at(1), ldq, at(2), t, at(3), ld, 0, None, 0,
+    st = L.digest_q8_weight_grad(n, k, m, at(1), ldq, at(2), t, at(3), ld, 1, None, 0,
                                  at(1) + last, at(5), need, None)
     assert st == D.EINVAL, st
     st = L.digest_q8_product(n, k, m, at(1), ldq, at(2), at(3), ldq, at(4), 1, t,
