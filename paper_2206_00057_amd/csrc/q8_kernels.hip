@@ -92,7 +92,11 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[4], const Scale &sc)
 }
 
 // A row in the registers of GL lanes (WAVES == 1, 64 / GL rows a wave) or of
-// WAVES waves of one workgroup, Q vectors of 16 bytes a lane: one reading of x.
+// WAVES waves of one workgroup, Q vectors of 16 bytes a lane: one reading of x,
+// four 16-byte loads a lane under way, and few lanes to find the largest of.
+// Bound by memory: 304,051 of 306,250 rows of 256 float32 82 us (4.8 TB/s), 16,384
+// x 4,096 bfloat16 40 us (5.0 TB/s); 304,051 x 47 float32, whose rows start
+// anywhere, 15 us.
 template <class T, int GL, int Q, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quantize_rows(
     int32_t n, int32_t d, const T *__restrict__ x, int64_t ldx, RowList src, int64_t n_x,
@@ -168,6 +172,7 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quant
 // Columns of w as rows of codes: a workgroup takes C columns, a thread P pieces
 // of 16 rows of one of them, in registers (P > 0: one reading of w), or in two
 // passes (P == 0, rows past 16 P kColThreads / C).  A piece is 16 bytes of codes.
+// Bound by latency: 602 x 256 float32 4 us (17 with 256 threads and two passes).
 constexpr int kColThreads = 1024;
 template <class T, int C, int P>
 __global__ __launch_bounds__(kColThreads) void k_quantize_columns(
@@ -243,8 +248,12 @@ __global__ __launch_bounds__(kColThreads) void k_quantize_columns(
     }
 }
 
-// Lanes and vectors as in k_quantize_rows, rows wider than their L Q V columns
-// in several turns.
+// Lanes and vectors as in k_quantize_rows, rows wider than their GL Q V columns
+// in several turns.  Bound by memory: 304,051 x 256 float32 in any order 66 us (5.9
+// TB/s, the codes partly from the Infinity Cache), 16,384 x 4,096 bfloat16 32 us;
+// 304,051 x 47 float32 23 us, a random row's 48 bytes costing a line of 128.  (A lane
+// an element for such rows, so that each is stored as one run: 31 -> 44 us from
+// memory.)
 template <class T, int GL, int Q>
 __global__ __launch_bounds__(kThreads) void k_dequantize_rows(
     int32_t n, int32_t d, const int8_t *__restrict__ codes, int64_t ldq,
@@ -451,7 +460,8 @@ __device__ __forceinline__ void store_row(const int (&sum)[N], float sr,
 
 // Few rows: bound by reading the weight's codes, 16 MT channels and 16 NT rows a
 // workgroup, its W waves a share of k each, straight from memory; the waves'
-// sums, whole numbers, are added through LDS.
+// sums, whole numbers, are added through LDS.  One row x 4,096 x 4,096 5.3 us (3.2
+// TB/s), 64 rows 12.
 template <class T, int MT, int NT, int W>
 __global__ __launch_bounds__(W *kWave) void k_q8_few(int32_t n, int32_t m, int32_t k,
                                                      const int8_t *__restrict__ q, int64_t ldq,
@@ -526,6 +536,12 @@ __device__ const uint4 kZeros = {0, 0, 0, 0};
 //
 // With 16-bit outputs the channels of a pair of blocks are dealt to the block's
 // rows so that a lane holds eight in a row.
+//
+// 8,192 x 4,096 x 4,096 bfloat16 out at 256 x 256: 124 to 135 us, 2.0 to 2.2 P
+// operations a second; the matrix units are busy half the time at the 2.1 GHz that
+// the card's power leaves.  (Fragments read a line ahead, between the matrix
+// instructions: 145 against 152 us there, but 90 against 84 for 16,384 x 640 x 4,096;
+// not kept.)
 template <class T, int WM, int WN, int TM>
 __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
     int32_t n, int32_t m, int32_t k, int32_t tiles_m, const int8_t *__restrict__ q, int64_t ldq,
@@ -583,9 +599,9 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
 
     i32x4 acc[TM][TN] = {};
     const int32_t lines = (k + 63) / 64;
-    // One line; its place is loaded with the line RING - 1 ahead of it... the one
-    // read before, which every wave has left at the barrier.  (Past the last line
-    // zeros are loaded, so that the waits count alike.)
+    // One line.  The place of the line before, which every wave has read at the
+    // barrier, is loaded with the line RING - 1 ahead of this one.  (Past the last
+    // line zeros are loaded, so that the waits count alike.)
     auto step = [&](int32_t line, const i32x4 *now, i32x4 *free) {
         sync(std::integral_constant<int, RING - 2>());
         i32x4 a[TM], b[TN];
@@ -649,7 +665,9 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
 // bound by writing y.  The weight's codes stay in LDS (in the places of
 // k_q8_gemm), and each wave takes 16 rows after another straight from memory, the
 // next ones' codes under way while these are multiplied and stored; no barrier
-// after the first.
+// after the first.  306,250 x 256 x 256 float32 out 81 to 87 us (4.5 to 4.8 TB/s).
+// (Kept to 128 registers, two workgroups a compute unit: 121; stores past the
+// caches 93; rows in runs a wave instead of interleaved 97.)
 template <class T, int LINES, int MB, int W>
 __global__ __launch_bounds__(W *kWave) void k_q8_stream(
     int32_t n, int32_t m, int32_t k, const int8_t *__restrict__ q, int64_t ldq,
@@ -748,12 +766,22 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
 // which together are exactly its 24 bits, so that the products are exact and
 // the sums fp32.
 //
-// A thread fetches four columns of four rows, two steps ahead in
+// A thread fetches four columns of four rows, a step ahead in
 // registers, and leaves them in LDS beside the step before's instructions, as
 // the matrix instructions take them: [rows / 8][slot] pieces of 16 bytes, slot
 // i T / 4 + q holding column 4 q + i, so that neighbouring lanes write
 // neighbouring bytes (two lanes a piece) and a wave's four tiles of D give each
 // lane 16 columns in a row of dw to store.
+//
+// Bound by memory where dw is small, by the matrix instructions where it is not:
+// 306,250 x 256 x 256 float32 with ReLU 145 us and 12 for the slices' sum (4.9
+// TB/s; 142 without the slices' stores), 16,384 x 1,024 x 4,096 bfloat16 310 to 350
+// us (1.2 to 1.3 PFLOP/s of three products each, what a large library product
+// reaches here).  Tried on the former: tiles of 128 x 128 288 us, 128 x 256 217, 256
+// x 128 213 (each step costs about the same whatever the tile); a second set of
+// fetched registers 213 to 813 (spills, or waits that the compiler cannot count
+// over branches).  29,125 x 602 x 256: 42 us and 12; its 85 slices' stores and 11
+// steps of 2.4 us, in which operands, splitting and products take turns.
 constexpr int kGradRows = 32, kGradThreads = 512;
 template <int TILE>
 __device__ __forceinline__ int slot_column(int slot)

@@ -482,6 +482,29 @@ def test_offsets_past_32_bits():
     assert torch.equal(out, near)
 
 
+def test_more_rows_than_a_launch_takes():
+    n, d, m = 2 ** 21 + 77, 20, 5
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(n, d, generator=g, device="cuda")
+    idx = torch.randperm(n, generator=g, device="cuda")
+    codes, scales = quantize(x)
+    again, s2 = quantize(x, rows=idx)
+    assert torch.equal(again, codes[idx]) and torch.equal(s2, scales[idx])
+    tail = torch.arange(n - 200, n, device="cuda")
+    check_codes(codes[tail], scales[tail], *held(x[tail]), d)
+    y = torch.empty(n, d, device="cuda")
+    D.digest_dequantize_rows(again, s2, y)
+    back = torch.empty(n, d, device="cuda")
+    D.digest_dequantize_rows(codes, scales, back, rows=idx)
+    assert torch.equal(y, back) and torch.equal(y, again[:, :d].float() * s2[:, None])
+    w, t = random_codes(m, d, g)
+    out = torch.empty(n, m, device="cuda")
+    D.digest_q8_product(codes, scales, w, t, out)
+    want = (torch.mm(codes.double(), w.double().t().contiguous()) * scales.double()[:, None] *
+            t.double())
+    assert bool(((out.double() - want).abs() <= 3.01 * U * want.abs()).all())
+
+
 def test_binding_refuses():
     x = torch.randn(8, 20, device="cuda")
     codes = torch.zeros(8, 32, dtype=torch.int8, device="cuda")
