@@ -9,6 +9,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <cmath>
 
 #include "device.h"
 #include "kernels.h"
@@ -1433,14 +1434,20 @@ bool grad_few(int32_t n, int32_t k, int32_t m)
 int32_t grad_splits(int32_t n, int64_t tiles, int64_t floats)
 {
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
+    const double slice = floats * 8 / 4.5e6, blocks = (double)n / kGradRows;
     int64_t best = 1;
-    double least = 0;
-    for (int64_t z = 1; z <= most; ++z) {
-        const int64_t steps = ((int64_t)n + z * kGradRows - 1) / (z * kGradRows);
-        const double us = 2.0 * steps + (z > 1 ? 4.0 + z * floats * 8 / 4.5e6 : 0.0);
-        if (z == 1 || us < least)
+    double least = 2.0 * std::ceil(blocks);
+    auto consider = [&](int64_t z) {
+        const double us = 2.0 * std::ceil(blocks / z) + 4.0 + z * slice;
+        if (z > 1 && us < least)
             best = z, least = us;
-    }
+    };
+    // the fewest slices of each number of steps about where the two costs meet
+    const double steps = std::ceil(std::sqrt(blocks * slice / 2));
+    for (int i = -2; i <= 2; ++i)
+        consider(std::min<int64_t>(most,
+                                   (int64_t)std::ceil(blocks / std::max(1.0, steps + i))));
+    consider(most);
     return (int32_t)best;
 }
 
