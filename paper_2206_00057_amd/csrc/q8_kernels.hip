@@ -762,7 +762,7 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
 }
 
 // dw over rows [z chunk, (z + 1) chunk) into slice z: TC columns of codes x TJ
-// of D a workgroup of 8 waves, 32 rows a step.  The codes are exact in
+// of D a workgroup of 8 waves, 32 rows a step, 64 for the smaller tiles.  The codes are exact in
 // bfloat16; s D is split into three bfloat16 by cutting off its low bits,
 // which together are exactly its 24 bits, so that the products are exact and
 // the sums fp32.
@@ -784,13 +784,14 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
 // over branches).  29,125 x 602 x 256: 42 us and 12; its 85 slices' stores and 11
 // steps of 2.4 us, in which operands, splitting and products take turns.
 constexpr int kGradRows = 32, kGradThreads = 512;
+// 32s of rows in a step: a step costs about the same whatever it holds.
+constexpr int grad_blocks(int tc, int tj) { return tc * tj <= 16384 ? 2 : 1; }
 template <int TILE>
 __device__ __forceinline__ int slot_column(int slot)
 {
     return slot % (TILE / 4) * 4 + slot / (TILE / 4);
 }
-//
-// ANY: fewer than four columns, or strides whose offsets of 32 rows pass 32
+// ANY: fewer than four columns, or strides whose offsets of a step's rows pass 32
 // bits; element by element.
 template <class T, bool RELU, int TC, int TJ, bool ANY>
 __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
@@ -800,9 +801,15 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     float *__restrict__ part)
 {
     constexpr int WJ = TJ / 64, WC = 8 / WJ, CW = TC / WC, NI = CW / 16;
-    constexpr int UD = TJ * 2, UC = TC * 2;   // threads that fetch D and codes
-    static_assert(UD <= kGradThreads && UC <= kGradThreads && NI >= 1, "one unit a thread");
-    __shared__ bf16x4 lc[2][4][TC][2], ld[2][3][4][TJ][2];   // [buffer](part)[octet][slot][half]
+    constexpr int R = grad_blocks(TC, TJ), ROWS = R * kGradRows;
+    // vectors of four columns x four rows of D and of codes, and a thread's
+    constexpr int UD = TJ * 2 * R, UC = TC * 2 * R;
+    constexpr int ND = UD > kGradThreads ? UD / kGradThreads : 1;
+    constexpr int NC = UC > kGradThreads ? UC / kGradThreads : 1;
+    constexpr int HD = 2 * kGradThreads / TJ, HC = 2 * kGradThreads / TC;   // octets apart
+    static_assert(NI >= 1 && ND <= R && NC <= R, "a place for each beside the products");
+    // [buffer](part)[octet][slot][half]
+    __shared__ bf16x4 lc[2][4 * R][TC][2], ld[2][3][4 * R][TJ][2];
 
     const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
     const uint32_t id = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -812,9 +819,9 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
 
     const int half = tid % 2;
     // (threads with nothing to fetch repeat others' fetches)
-    const int qd = tid / 2 % (TJ / 4), od = tid / 2 / (TJ / 4) % 4;
-    const int qc = tid / 2 % (TC / 4), oc = tid / 2 / (TC / 4) % 4;
-    const bool does_d = UD == kGradThreads || tid < UD, does_c = UC == kGradThreads || tid < UC;
+    const int qd = tid / 2 % (TJ / 4), od = tid / 2 / (TJ / 4) % (4 * R);
+    const int qc = tid / 2 % (TC / 4), oc = tid / 2 / (TC / 4) % (4 * R);
+    const bool does_d = UD >= kGradThreads || tid < UD, does_c = UC >= kGradThreads || tid < UC;
     // A vector that would pass the row's end lies against it instead: its columns
     // are formed twice, alike.  Vectors behind it repeat it and are not stored.
     const int64_t last = max(m - 4, 0);
@@ -824,82 +831,110 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     const uint32_t bytes_d = lddy * sizeof(T), bytes_y = ldy * sizeof(T), bytes_c = ldq;
     const uint32_t col_d = jd * sizeof(T), col_c = cc;   // (not with ANY)
     struct Fetched {
-        typename Vec<T, 4>::type d[4], y[RELU ? 4 : 1];
-        typename Vec<float, 4>::type s;
-        uint32_t c[4];
+        typename Vec<T, 4>::type d[ND][4], y[RELU ? ND : 1][4];
+        typename Vec<float, 4>::type s[ND];
+        uint32_t c[NC][4];
     } next;
-    // The rows r0 .. r0 + 31.  Rows past the end repeat the last one with codes of
-    // zero: what it adds to its columns is nothing, or the NaN that they hold.
+    // The rows r0 .. r0 + ROWS - 1.  Rows past the end repeat the last one with
+    // codes of zero: what it adds to its columns is nothing, or the NaN that they
+    // hold.
     auto fetch = [&](Fetched &f, int64_t r0) {
-        const int rows = (int)min((int64_t)kGradRows, re - r0);
+        const int rows = (int)min((int64_t)ROWS, re - r0);
         if (rows <= 0)
             return;
         const char *bd = (const char *)(dy + r0 * lddy), *by = (const char *)(y + r0 * ldy);
         const char *bc = (const char *)(q + r0 * ldq), *bs = (const char *)(s + r0);
         if constexpr (ANY) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int64_t r = min(rd + i, rows - 1);
-                f.s[i] = s[r0 + r];
+            for (int x = 0; x < ND; ++x)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int64_t j = min(jd + e, (int64_t)m - 1);
-                    f.d[i][e] = dy[(r0 + r) * lddy + j];
-                    if constexpr (RELU)
-                        f.y[i][e] = y[(r0 + r) * ldy + j];
+                for (int i = 0; i < 4; ++i) {
+                    const int64_t r = r0 + min(rd + x * HD * 8 + i, rows - 1);
+                    f.s[x][i] = s[r];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const int64_t j = min(jd + e, (int64_t)m - 1);
+                        f.d[x][i][e] = dy[r * lddy + j];
+                        if constexpr (RELU)
+                            f.y[x][i][e] = y[r * ldy + j];
+                    }
                 }
-                f.c[i] = rc + i < rows ? *reinterpret_cast<const uint32_t *>(
-                                             q + (r0 + rc + i) * ldq + cc)
-                                       : 0;
-            }
+#pragma unroll
+            for (int x = 0; x < NC; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = rc + x * HC * 8 + i;
+                    f.c[x][i] = r < rows ? *reinterpret_cast<const uint32_t *>(
+                                               q + (r0 + r) * ldq + cc)
+                                         : 0;
+                }
             return;
         }
         typedef typename Vec<T, 4>::type vec;
-        if (rows == kGradRows) {
+        if (rows == ROWS) {
             const uint32_t at_d = rd * bytes_d + col_d, at_y = rd * bytes_y + col_d;
             const uint32_t at_c = rc * bytes_c + col_c;
-            f.s = *reinterpret_cast<const typename Vec<float, 4>::type *>(bs + (uint32_t)rd * 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                f.d[i] = *reinterpret_cast<const vec *>(bd + (uint64_t)i * bytes_d + at_d);
-                if constexpr (RELU)
-                    f.y[i] = *reinterpret_cast<const vec *>(by + (uint64_t)i * bytes_y + at_y);
-                f.c[i] = *reinterpret_cast<const uint32_t *>(bc + (uint64_t)i * bytes_c + at_c);
+            for (int x = 0; x < ND; ++x) {
+                f.s[x] = *reinterpret_cast<const typename Vec<float, 4>::type *>(
+                    bs + x * HD * 32 + (uint32_t)rd * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint64_t r = x * HD * 8 + i;
+                    f.d[x][i] = *reinterpret_cast<const vec *>(bd + r * bytes_d + at_d);
+                    if constexpr (RELU)
+                        f.y[x][i] = *reinterpret_cast<const vec *>(by + r * bytes_y + at_y);
+                }
             }
+#pragma unroll
+            for (int x = 0; x < NC; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    f.c[x][i] = *reinterpret_cast<const uint32_t *>(
+                        bc + (uint64_t)(x * HC * 8 + i) * bytes_c + at_c);
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t r = min(rd + i, rows - 1), h = min(rc + i, rows - 1);
-                f.s[i] = *reinterpret_cast<const float *>(bs + r * 4);
-                f.d[i] = *reinterpret_cast<const vec *>(bd + (r * bytes_d + col_d));
-                if constexpr (RELU)
-                    f.y[i] = *reinterpret_cast<const vec *>(by + (r * bytes_y + col_d));
-                f.c[i] = *reinterpret_cast<const uint32_t *>(bc + (h * bytes_c + col_c));
-                f.c[i] = rc + i < rows ? f.c[i] : 0;
-            }
+            for (int x = 0; x < ND; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t r = min(rd + x * HD * 8 + i, rows - 1);
+                    f.s[x][i] = *reinterpret_cast<const float *>(bs + r * 4);
+                    f.d[x][i] = *reinterpret_cast<const vec *>(bd + (r * bytes_d + col_d));
+                    if constexpr (RELU)
+                        f.y[x][i] = *reinterpret_cast<const vec *>(by + (r * bytes_y + col_d));
+                }
+#pragma unroll
+            for (int x = 0; x < NC; ++x)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = rc + x * HC * 8 + i;
+                    const uint32_t h = min(r, rows - 1);
+                    f.c[x][i] = *reinterpret_cast<const uint32_t *>(bc + (h * bytes_c + col_c));
+                    f.c[x][i] = r < rows ? f.c[x][i] : 0;
+                }
         }
     };
     // column i of what was fetched, into buffer b
-    auto stash_codes = [&](const Fetched &f, int b, int i) {
+    auto stash_codes = [&](const Fetched &f, int b, int x, int i) {
         if (!does_c)
             return;
         bf16x4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            v[e] = (__bf16)(float)(int8_t)(f.c[e] >> (8 * i));
-        lc[b][oc][i * (TC / 4) + qc][half] = v;
+            v[e] = (__bf16)(float)(int8_t)(f.c[x][e] >> (8 * i));
+        lc[b][oc + x * HC][i * (TC / 4) + qc][half] = v;
     };
-    auto stash_d = [&](const Fetched &f, int b, int i) {
+    auto stash_d = [&](const Fetched &f, int b, int x, int i) {
         if (!does_d)
             return;
         bf16x4 v[3];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            float D = (float)f.d[e][i];
+            float D = (float)f.d[x][e][i];
             if constexpr (RELU)
-                if (!((float)f.y[e][i] > 0.f))
+                if (!((float)f.y[x][e][i] > 0.f))
                     D = 0.f;
-            D *= f.s[e];
+            D *= f.s[x][e];
 #pragma unroll
             for (int h = 0; h < 3; ++h) {
                 const uint32_t top = __float_as_uint(D) & 0xffff0000u;
@@ -909,7 +944,16 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
         }
 #pragma unroll
         for (int h = 0; h < 3; ++h)
-            ld[b][h][od][i * (TJ / 4) + qd][half] = v[h];
+            ld[b][h][od + x * HD][i * (TJ / 4) + qd][half] = v[h];
+    };
+    // the parts of a step's stash: a column of each of the thread's vectors
+    constexpr int PARTS = 4 * (ND + NC);
+    auto stash = [&](const Fetched &f, int b, int part) {
+        const int i = part % 4, x = part / 4;
+        if (x < ND)
+            stash_d(f, b, x, i);
+        else
+            stash_codes(f, b, x - ND, i);
     };
 
     f32x4 acc[NI][4] = {};
@@ -918,28 +962,32 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     auto step = [&](int b, Fetched &next, int64_t further) {
         lds_barrier();
         bf16x8 c[NI];
+        auto codes = [&](int sub) {
 #pragma unroll
-        for (int o = 0; o < NI; ++o)
-            c[o] = *reinterpret_cast<const bf16x8 *>(&lc[b][g][wc * CW + o * 16 + l][0]);
+            for (int o = 0; o < NI; ++o)
+                c[o] = *reinterpret_cast<const bf16x8 *>(
+                    &lc[b][4 * sub + g][wc * CW + o * 16 + l][0]);
+        };
         // (a fragment is read beside the instructions that take the one before)
         auto frag = [&](int slot) {
             return *reinterpret_cast<const bf16x8 *>(
-                &ld[b][2 - slot % 3][g][slot / 3 * (TJ / 4) + wj * 16 + l][0]);
+                &ld[b][2 - slot % 3][slot / 12 * 4 + g][slot % 12 / 3 * (TJ / 4) + wj * 16 + l][0]);
         };
+        codes(0);
         bf16x8 a = frag(0), ahead;
 #pragma unroll
-        for (int slot = 0; slot < 12; ++slot) {
-            if (slot < 11)
+        for (int slot = 0; slot < 12 * R; ++slot) {
+            if (slot > 0 && slot % 12 == 0)
+                codes(slot / 12);
+            if (slot < 12 * R - 1)
                 ahead = frag(slot + 1);
 #pragma unroll
             for (int o = 0; o < NI; ++o)
-                acc[o][slot / 3] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    a, c[o], acc[o][slot / 3], 0, 0, 0);
-            // the next step's operands, beside the last two thirds' instructions
-            if (slot >= 4 && slot % 2 == 0)
-                stash_d(next, b ^ 1, slot / 2 - 2);
-            else if (slot >= 4)
-                stash_codes(next, b ^ 1, slot / 2 - 2);
+                acc[o][slot % 12 / 3] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    a, c[o], acc[o][slot % 12 / 3], 0, 0, 0);
+            // the next step's operands, beside the last instructions
+            if (slot >= 12 * R - PARTS)
+                stash(next, b ^ 1, slot - (12 * R - PARTS));
             a = ahead;
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -947,15 +995,12 @@ __global__ __launch_bounds__(kGradThreads) void k_q8_grad(
     };
     fetch(next, rb);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        stash_codes(next, 0, i);
-        stash_d(next, 0, i);
-    }
-    fetch(next, rb + kGradRows);
+    for (int part = 0; part < PARTS; ++part)
+        stash(next, 0, part);
+    fetch(next, rb + ROWS);
     int b = 0;
-    for (int64_t r0 = rb; r0 < re; r0 += kGradRows, b ^= 1) {
-        step(b, next, r0 + 2 * kGradRows);
-    }
+    for (int64_t r0 = rb; r0 < re; r0 += ROWS, b ^= 1)
+        step(b, next, r0 + 2 * ROWS);
     if (splits > 1) {
         // as the lanes hold them
         f32x4 *out = (f32x4 *)part + ((int64_t)z * (tiles_c * tiles_j) + tile) * (TC * TJ / 4) +
@@ -1431,10 +1476,10 @@ bool grad_few(int32_t n, int32_t k, int32_t m)
 // Slices of the rows: at most one workgroup a compute unit, and fewer where the
 // slices' sums would cost more (written and read once each at about 4.5 TB/s,
 // floats of a slice) than the steps that they save (about 2 us each).
-int32_t grad_splits(int32_t n, int64_t tiles, int64_t floats)
+int32_t grad_splits(int32_t n, int64_t tiles, int rows, int64_t floats)
 {
-    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / 64));
-    const double slice = floats * 8 / 4.5e6, blocks = (double)n / kGradRows;
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256 / tiles, (int64_t)n / (2 * kGradRows)));
+    const double slice = floats * 8 / 4.5e6, blocks = (double)n / rows;
     int64_t best = 1;
     double least = 2.0 * std::ceil(blocks);
     auto consider = [&](int64_t z) {
@@ -1458,9 +1503,10 @@ hipError_t weight_grad(int32_t n, int32_t k, int32_t m, const int8_t *q, int64_t
 {
     const int32_t nc = (k + TC - 1) / TC, nj = (m + TJ - 1) / TJ;
     const int64_t tiles = (int64_t)nc * nj;
-    const int32_t splits = grad_splits(n, tiles, tiles * TC * TJ);
+    constexpr int rows = grad_blocks(TC, TJ) * kGradRows;
+    const int32_t splits = grad_splits(n, tiles, rows, tiles * TC * TJ);
     int64_t chunk = ((int64_t)n + splits - 1) / splits;
-    chunk = (chunk + kGradRows - 1) / kGradRows * kGradRows;
+    chunk = (chunk + rows - 1) / rows * rows;
     const auto kernel = y ? k_q8_grad<T, true, TC, TJ, ANY> : k_q8_grad<T, false, TC, TJ, ANY>;
     kernel<<<(uint32_t)(tiles * splits), kGradThreads, 0, st>>>(
         n, k, m, chunk, splits, nc, nj, q, ldq, s, dy, lddy, y, ldy, splits > 1 ? part : dw);
@@ -1489,7 +1535,8 @@ size_t q8_grad_floats(int32_t n, int32_t k, int32_t m)
     const int sides[2][2] = {{grad_tile_c(k), grad_tile_j(m)}, {128, 64}};
     for (const auto &t : sides) {
         const int64_t tiles = (int64_t)((k + t[0] - 1) / t[0]) * ((m + t[1] - 1) / t[1]);
-        const int64_t splits = grad_splits(n, tiles, tiles * t[0] * t[1]);
+        const int64_t splits = grad_splits(n, tiles, grad_blocks(t[0], t[1]) * kGradRows,
+                                           tiles * t[0] * t[1]);
         if (splits > 1)
             most = std::max<size_t>(most, (size_t)(splits * tiles) * t[0] * t[1]);
     }
@@ -1514,7 +1561,7 @@ hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, 
         }
         const int64_t pitch = std::max<int64_t>(std::max(lddy, y ? ldy : 0) * sizeof(T), ldq);
         const int tc = grad_tile_c(k), tj = grad_tile_j(m);
-        if (m < 4 || (pitch + 65536 * 4) * kGradRows > UINT32_MAX)
+        if (m < 4 || (pitch + 65536 * 4) * (2 * kGradRows) > UINT32_MAX)
             return run(weight_grad<T, 128, 64, true>);
         if (tc == 256)
             return tj == 256   ? run(weight_grad<T, 256, 256, false>)
