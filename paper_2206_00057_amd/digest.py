@@ -726,16 +726,18 @@ def digest_muon_average(ws, momenta, grads, workspace, lr, beta=0.95, decay=0.0,
 # Rows held in 8 bits.
 
 _q8 = None
-_I8 = _F32T = None   # torch.int8, torch.float32
+_I8 = _F32T = _I64 = None   # torch.int8, torch.float32, torch.int64
+_raw_stream = None           # a device's current stream, as a number
 
 
 def _q8_lib():
     """The library with the calls on rows held in 8 bits; raises if this build
     of the ABI lacks them."""
-    global _q8, _I8, _F32T
+    global _q8, _I8, _F32T, _I64, _raw_stream
     if _q8 is None or _q8 is not _lib:
         import torch
-        _I8, _F32T = torch.int8, torch.float32
+        _I8, _F32T, _I64 = torch.int8, torch.float32, torch.int64
+        _raw_stream = torch._C._cuda_getCurrentRawStream
         L = lib()
         P, i32, i64, sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
         sig = {
@@ -785,6 +787,11 @@ def _codes(t, scales, n, width, dev, name, scales_name):
     return p, ld, _need(_floats(scales, n, dev, scales_name), scales_name)
 
 
+def _stream_of(stream, dev):
+    """As _stream, of the device dev, the current one."""
+    return _raw_stream(dev) if stream is None else _stream(stream)
+
+
 def _need(p, name):
     if p is None:
         raise ValueError(f"{name} is required")
@@ -793,11 +800,10 @@ def _need(p, name):
 
 def _list(rows, n, dev):
     """Pointer of n row numbers (int64), None for None."""
-    import torch
     if rows is None:
         return None
     _here(rows, dev, "rows")
-    if rows.dtype != torch.int64:
+    if rows.dtype is not _I64:
         raise TypeError(f"rows must be torch.int64, got {rows.dtype}")
     if rows.dim() != 1 or not rows.is_contiguous() or rows.numel() != n:
         raise ValueError(f"rows must be {n} contiguous numbers")
@@ -815,7 +821,7 @@ def digest_quantize_rows(x, codes, scales, rows=None, stream=None):
     px, ldx = _row_array(x, shape, dtype, dev, "x")
     pq, ldq, ps = _codes(codes, scales, n, d, dev, "codes", "scales")
     _check(L.digest_quantize_rows(n, d, _TYPES[dtype], px, ldx, _list(rows, n, dev), m, pq,
-                                          ldq, ps, _stream(stream)))
+                                          ldq, ps, _stream_of(stream, dev)))
 
 
 def digest_quantize_columns(w, codes, scales, stream=None):
@@ -827,7 +833,7 @@ def digest_quantize_columns(w, codes, scales, stream=None):
     pw, ldw = _row_array(w, shape, dtype, dev, "w")
     pq, ldq, ps = _codes(codes, scales, m, k, dev, "codes", "scales")
     _check(L.digest_quantize_columns(k, m, _TYPES[dtype], pw, ldw, pq, ldq, ps,
-                                             _stream(stream)))
+                                             _stream_of(stream, dev)))
 
 
 def digest_dequantize_rows(codes, scales, y, rows=None, stream=None):
@@ -840,7 +846,7 @@ def digest_dequantize_rows(codes, scales, y, rows=None, stream=None):
     pq, ldq, ps = _codes(codes, scales, m, d, dev, "codes", "scales")
     py, ldy = _row_array(y, shape, dtype, dev, "y")
     _check(L.digest_dequantize_rows(n, d, pq, ldq, ps, _list(rows, n, dev), m,
-                                            _TYPES[dtype], py, ldy, _stream(stream)))
+                                            _TYPES[dtype], py, ldy, _stream_of(stream, dev)))
 
 
 def digest_q8_product(codes, scales, w_codes, w_scales, y, act=ACT_IDENTITY, stream=None):
@@ -855,7 +861,7 @@ def digest_q8_product(codes, scales, w_codes, w_scales, y, act=ACT_IDENTITY, str
     pw, ldw, pt = _codes(w_codes, w_scales, m, k, dev, "w_codes", "w_scales")
     py, ldy = _row_array(y, shape, dtype, dev, "y")
     _check(L.digest_q8_product(n, k, m, pq, ldq, ps, pw, ldw, pt, act, _TYPES[dtype], py,
-                                       ldy, _stream(stream)))
+                                       ldy, _stream_of(stream, dev)))
 
 
 def digest_q8_weight_grad_query(n_rows, d_in, d_out):
@@ -885,7 +891,7 @@ def digest_q8_weight_grad(codes, scales, dy, dw, workspace, act=ACT_IDENTITY, y=
     ws, nbytes = _workspace(workspace, dev)
     _check(L.digest_q8_weight_grad(n, k, m, pq, ldq, ps, _TYPES[dtype], pdy, lddy, act,
                                            py, ldy, _floats(dw, k * m, dev, "dw"), ws, nbytes,
-                                           _stream(stream)))
+                                           _stream_of(stream, dev)))
 
 
 def digest_push_q8(p, level, h_own, codes, scales, mode=PUSH_BOUNDARY, stream=None):
