@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "device.h"
 #include "kernels.h"
@@ -40,6 +41,16 @@ __device__ __forceinline__ int64_t row_number(const RowList &l, int64_t i)
     if (!l.p)
         return i;
     return l.wide ? ((const int64_t *)l.p)[i] : ((const int32_t *)l.p)[i];
+}
+
+// v, a number in fp32, rounded to T.  (Without the barrier the compiler folds a
+// product into the conversion to fp16, which then rounds it once.)
+template <class T>
+__device__ __forceinline__ T rounded(float v)
+{
+    if constexpr (std::is_same<T, _Float16>::value)
+        asm("" : "+v"(v));
+    return (T)v;
 }
 
 __device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
@@ -252,9 +263,8 @@ __global__ __launch_bounds__(kColThreads) void k_quantize_columns(
 // Lanes and vectors as in k_quantize_rows, rows wider than their GL Q V columns
 // in several turns.  Bound by memory: 304,051 x 256 float32 in any order 66 us (5.9
 // TB/s, the codes partly from the Infinity Cache), 16,384 x 4,096 bfloat16 32 us;
-// 304,051 x 47 float32 23 us, a random row's 48 bytes costing a line of 128.  (A lane
-// an element for such rows, so that each is stored as one run: 31 -> 44 us from
-// memory.)
+// rows that are not whole vectors, 304,051 x 47, 31 us.  (A lane an element for
+// them, so that each is stored as one run: 44 us.)
 template <class T, int GL, int Q>
 __global__ __launch_bounds__(kThreads) void k_dequantize_rows(
     int32_t n, int32_t d, const int8_t *__restrict__ codes, int64_t ldq,
@@ -290,7 +300,7 @@ __global__ __launch_bounds__(kThreads) void k_dequantize_rows(
             vec out;
 #pragma unroll
             for (int j = 0; j < V; ++j)
-                out[j] = (T)((float)(int8_t)(w[q][j / 4] >> (8 * (j % 4))) * s);
+                out[j] = rounded<T>((float)(int8_t)(w[q][j / 4] >> (8 * (j % 4))) * s);
             if (c + V <= d) {
                 *reinterpret_cast<vec *>(yr + c) = out;
             } else {
@@ -449,13 +459,13 @@ __device__ __forceinline__ void store_row(const int (&sum)[N], float sr,
         typename Vec<T, N>::type v;
 #pragma unroll
         for (int e = 0; e < N; ++e)
-            v[e] = (T)relu_of(scaled(sum[e], sr, t[j + e]), relu);
+            v[e] = rounded<T>(relu_of(scaled(sum[e], sr, t[j + e]), relu));
         *reinterpret_cast<typename Vec<T, N>::type *>(yr + j) = v;
     } else {
 #pragma unroll
         for (int e = 0; e < N; ++e)
             if (j + e < m)
-                yr[j + e] = (T)relu_of(scaled(sum[e], sr, t[j + e]), relu);
+                yr[j + e] = rounded<T>(relu_of(scaled(sum[e], sr, t[j + e]), relu));
     }
 }
 

@@ -97,6 +97,32 @@ def test_rows(d, t):
         assert (np.abs(got[i] - want) <= (U + half(t)) * 1.001 * np.abs(want) + tiny).all(), (i, r)
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,d", [(1, 1), (5, 3), (9, 47), (300, 47), (5000, 7), (3000, 101),
+                                 (40000, 33), (9001, 250), (20000, 17), (31, 255), (3, 259),
+                                 (131072, 47), (131075, 33), (140001, 250), (131077, 7), (131073, 1),
+                                 (150001, 127), (131071, 31), (132001, 255)])
+def test_read_whole(n, d, t):
+    """Contiguous outputs, at whole vectors and shifted by an element, in order and
+    in another: each value is the product, rounded to fp32 and from there to the type."""
+    g = torch.Generator(device="cuda").manual_seed(n + d)
+    q, s = random_codes(n, d, g, gap=1)
+    want = (q[:, :d].float() * s[:, None]).to(t)
+    idx = torch.randint(0, n, (n + 3,), generator=g, device="cuda")
+    for shift in (0, 1):
+        for rows in (None, idx):
+            m = n if rows is None else n + 3
+            base = torch.full((m * d + shift + 9,), 7.0, dtype=t, device="cuda")
+            y = base[shift:shift + m * d].view(m, d)
+            D.digest_dequantize_rows(q, s, y, rows=rows)
+            assert torch.equal(y, want if rows is None else want[rows])
+            assert bool((base[:shift] == 7).all()) and bool((base[shift + m * d:] == 7).all())
+    idx[n // 2] = n
+    y = torch.empty(n + 3, d, dtype=t, device="cuda")
+    D.digest_dequantize_rows(q, s, y, rows=idx)
+    assert torch.isnan(y).all(1).nonzero()[:, 0].tolist() == [n // 2]
+
+
 def test_rows_behind_are_left():
     x = torch.randn(6, 40, device="cuda")
     codes = torch.full((9, 48), 3, dtype=torch.int8, device="cuda")
