@@ -734,7 +734,9 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
 // bound by writing y.  The weight's codes stay in LDS (in the places of
 // k_q8_gemm), and each wave takes 16 rows after another straight from memory, the
 // next ones' codes under way while these are multiplied and stored; no barrier
-// after the first.  306,250 x 256 x 256 float32 out 81 to 87 us (4.5 to 4.8 TB/s).
+// after the first.  306,250 x 256 x 256 float32 out 81 to 87 us (4.5 to 4.8 TB/s),
+// 300,000 x 600 x 256 bfloat16 89 (3.8), 16,384 x 640 x 4,096 74 (1.2 P operations a
+// second, of which 27 to store y).
 // (Kept to 128 registers, two workgroups a compute unit: 121; stores past the
 // caches 93; rows in runs a wave instead of interleaved 97.)
 template <class T, int LINES, int MB, int W>
@@ -1470,8 +1472,10 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
         typedef std::integral_constant<int, 1> i1;
         typedef std::integral_constant<int, 2> i2;
         typedef std::integral_constant<int, 4> i4;
+        typedef std::integral_constant<int, 6> i6;
         typedef std::integral_constant<int, 8> i8;
         typedef std::integral_constant<int, 10> i10;
+        typedef std::integral_constant<int, 12> i12;
         typedef std::integral_constant<int, 16> i16;
         if (n <= 16)
             return few(i1{}, i1{});
@@ -1487,11 +1491,18 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
                 n, m, k, nm, q, ldq, s, p, ldp, t, relu, out, ldy);
             return hipGetLastError();
         };
+        // The workgroups that the compute units hold at once; where they are no
+        // multiple of the groups of channels, more of them with fewer rows each, if
+        // there are rows to share (us, once / up to four times: 8,192 x 640 x 20,000
+        // bfloat16 235 / 180, 4,096 x 300 x 40,000 145 / 111; 300 x 600 x 20,000 15.0
+        // / 17.5, hence the line).
         auto stream = [&](auto lines, auto mb) {
             constexpr int LINES = decltype(lines)::value, MB = decltype(mb)::value;
             constexpr int W = 8;
-            const int32_t nm = (m + 16 * MB - 1) / (16 * MB);
-            const int32_t blocks = (n + 16 * W - 1) / (16 * W), most = 512;
+            const int32_t nm = (m + 16 * MB - 1) / (16 * MB), blocks = (n + 16 * W - 1) / (16 * W);
+            int32_t most = LINES > 4 ? 256 : 512;
+            while (LINES > 4 && blocks >= 8 && most < 1024 && most / nm * nm < most / 5 * 4)
+                most *= 2;
             const dim3 grid(std::max(1, std::min(blocks, most / nm)), nm);
             k_q8_stream<T, LINES, MB, W><<<grid, W * kWave, 0, st>>>(n, m, k, q, ldq, s, p, ldp, t,
                                                                     relu, out, ldy);
@@ -1499,35 +1510,44 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
         };
         // The most channels a workgroup that leave every compute unit one (us, 256
         // channels of 256 k, float32, with 256 / 64 channels: 2,048 rows 8.6 / 4.1,
-        // 8,192 rows 9.8 / 5.4).  Against tiles through the ring: 8,192 rows 10.4,
-        // 29,125 rows 17 against 11, 306,250 rows 140 against 89 (4.4 TB/s).
+        // 8,192 rows 9.8 / 5.4; of 602 k, with 128 / 64: 8,192 rows 9.2 / 7.3, 29,125
+        // rows 18.1 / 21.0; with 256 there, all of LDS, 23.4).  Against tiles through
+        // the ring: 29,125 x 256 x 256 float32 11 / 17, 306,250 rows 89 / 140 (4.4
+        // TB/s), 300,000 x 600 x 256 bfloat16 89 / 131, 16,384 x 640 x 4,096 74 / 89,
+        // 100,000 x 602 x 41 float32 23 / 41, 4,096 x 512 x 4,096 bfloat16 21 / 21.
         auto stream_lines = [&](auto lines) {
             const int64_t blocks = (n + 127) / 128;
-            return m > 128 && blocks * ((m + 255) / 256) >= 256  ? stream(lines, i16{})
-                   : m > 64 && blocks * ((m + 127) / 128) >= 256 ? stream(lines, i8{})
-                                                                 : stream(lines, i4{});
+            if constexpr (decltype(lines)::value <= 4)
+                if (m > 128 && blocks * ((m + 255) / 256) >= 256)
+                    return stream(lines, i16{});
+            return m > 64 && blocks * ((m + 127) / 128) >= 256 ? stream(lines, i8{})
+                                                               : stream(lines, i4{});
         };
-        if (k <= 256)
-            return k <= 128 ? stream_lines(i2{}) : stream_lines(i4{});
+        if (k <= 640)
+            return k <= 128   ? stream_lines(i2{})
+                   : k <= 256 ? stream_lines(i4{})
+                   : k <= 384 ? stream_lines(i6{})
+                   : k <= 512 ? stream_lines(i8{})
+                              : stream_lines(i10{});
         // Workgroups of a tile.  The largest tile that gives every compute unit one
-        // reads operands the fewest times (us at 256 x 256 / 128 x 128: 16,384 x 640
-        // x 4,096 bfloat16 86 / 111, 2,048 x 640 x 2,048 18 / 9; 256 x 128 / 128 x
-        // 128: 2,048 x 4,096 x 4,096 49 / 57).  Below that, weights of up to 640 k
-        // stay in LDS for few channels, whose rows are read again from L2 (29,125 x
-        // 602 x 256 float32 20.9 against 22.9, 8,192 rows 7.2 / 10.2; 2,048 x 640 x
-        // 2,048 12.7 / 8.7, hence the line at 512), and where tiles are few the
-        // waves share k (1,000 x 2,000 x 300 10.9 / 17.3, 512 x 1,024 x 1,024 8.3 /
-        // 9.9, 512 x 4,096 x 4,096, 512 workgroups, 36 / 21).
+        // reads operands the fewest times (us at 256 x 128 / 128 x 128: 2,048 x 4,096
+        // x 4,096 49 / 57); up to 768 k the weight still fits into LDS (100,000 x 768
+        // x 256 float32 54 against 65, 16,384 x 768 x 4,096 bfloat16 81 / 95, but
+        // 8,192 x 768 x 768 15.9 / 13.4; of 1,024 k 0.96 to 1.17 times as fast).  Where
+        // tiles are few the waves share k (1,000 x 2,000 x 300 10.9 / 17.3, 512 x 4,096
+        // x 4,096, 512 workgroups, 36 / 21), and no tile is wider than 64 or 128 channels
+        // that are all (40,000 x 4,096 x 47 bfloat16 60 / 76, 100,000 x 1,000 x 128
+        // float32 65 / 71).
         auto tiles = [&](int bm, int bn) {
             return (int64_t)((m + bm - 1) / bm) * ((n + bn - 1) / bn);
         };
-        if (tiles(256, 256) >= 256)
+        if (k <= 768 && tiles(256, 256) >= 256)
+            return stream_lines(i12{});
+        if (m > 128 && tiles(256, 256) >= 256)
             return gemm(i2{}, i4{}, i8{});   // 256 x 256
-        if (k <= 640 && m <= 512)
-            return stream(i10{}, i4{});
         if (tiles(64, 64) <= 256)
             return few(i4{}, i4{});
-        if (tiles(256, 128) >= 192)
+        if (m > 128 && tiles(256, 128) >= 192)
             return gemm(i4{}, i2{}, i4{});   // 256 channels x 128 rows
         if (m > 64)
             return gemm(i4{}, i2{}, i2{});   // 128 x 128

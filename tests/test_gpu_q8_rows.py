@@ -232,6 +232,14 @@ def test_product(n, k, m):
 
 
 @pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("n,k,m,gap", [(4100, 383, 1030, 1), (130, 385, 47, 2), (2200, 512, 2051, 3),
+                                       (2100, 513, 2049, 1)])
+def test_product_of_strided_rows(n, k, m, gap, t):
+    """Weights kept in LDS, rows and outputs with gaps between them."""
+    check_product(n, k, m, t, ACTS[1], gap)
+
+
+@pytest.mark.parametrize("t", TYPES)
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("n,k,m,gap", [(1, 4096, 4096, 0), (5, 640, 1030, 3), (33, 100, 47, 1),
                                        (513, 256, 256, 0), (1030, 1024, 520, 0), (400, 602, 256, 5),
@@ -244,7 +252,12 @@ def test_product_types(n, k, m, gap, t, act):
                                    (70000, 100, 250), (70001, 256, 40), (30000, 250, 600),
                                    (33000, 70, 1100), (9000, 600, 500), (29125, 602, 256),
                                    (1000, 2000, 300), (2047, 1100, 4095), (1500, 700, 1300),
-                                   (20000, 900, 33), (800, 4100, 1000)])
+                                   (20000, 900, 33), (800, 4100, 1000), (4001, 300, 1100),
+                                   (501, 300, 70), (3000, 400, 1500), (203, 500, 100),
+                                   (2501, 640, 2000), (5000, 602, 41), (65541, 768, 200),
+                                   (70001, 700, 64), (1100, 300, 11000), (1031, 500, 16500),
+                                   (300, 600, 20000), (17000, 650, 1025), (40000, 1000, 47),
+                                   (33001, 790, 127), (257, 257, 129), (70, 385, 65)])
 def test_product_large(n, k, m):
     """Against float64 products on the GPU: sums below 2^31, exact there."""
     g = torch.Generator(device="cuda").manual_seed(n)
