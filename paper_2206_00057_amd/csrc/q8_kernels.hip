@@ -1460,13 +1460,15 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
 {
     return in_turns(n, [&](int64_t r0, int32_t n) { return with_type(type, [&](auto tag) {
         typedef typename decltype(tag)::type T;
-        q += r0 * ldq, s += r0;
-        T *out = (T *)y + r0 * ldy;
+        // (the turn's rows)
+        const int8_t *const qt = q + r0 * ldq;
+        const float *const sr = s + r0;
+        T *const out = (T *)y + r0 * ldy;
         auto few = [&](auto mt, auto nt) {
             constexpr int MT = decltype(mt)::value, NT = decltype(nt)::value;
             const dim3 grid((m + 16 * MT - 1) / (16 * MT), (n + 16 * NT - 1) / (16 * NT));
-            k_q8_few<T, MT, NT, 8><<<grid, 8 * kWave, 0, st>>>(n, m, k, q, ldq, s, p, ldp, t, relu,
-                                                              out, ldy);
+            k_q8_few<T, MT, NT, 8><<<grid, 8 * kWave, 0, st>>>(n, m, k, qt, ldq, sr, p, ldp, t,
+                                                              relu, out, ldy);
             return hipGetLastError();
         };
         typedef std::integral_constant<int, 1> i1;
@@ -1488,7 +1490,7 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
             constexpr int TM = decltype(tm)::value, BM = WM * TM * 16, BN = WN * 64;
             const int32_t nm = (m + BM - 1) / BM, nn = (n + BN - 1) / BN;
             k_q8_gemm<T, WM, WN, TM><<<(uint32_t)nm * nn, WM * WN * kWave, 0, st>>>(
-                n, m, k, nm, q, ldq, s, p, ldp, t, relu, out, ldy);
+                n, m, k, nm, qt, ldq, sr, p, ldp, t, relu, out, ldy);
             return hipGetLastError();
         };
         // The workgroups that the compute units hold at once; where they are no
@@ -1504,8 +1506,8 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
             while (LINES > 4 && blocks >= 8 && most < 1024 && most / nm * nm < most / 5 * 4)
                 most *= 2;
             const dim3 grid(std::max(1, std::min(blocks, most / nm)), nm);
-            k_q8_stream<T, LINES, MB, W><<<grid, W * kWave, 0, st>>>(n, m, k, q, ldq, s, p, ldp, t,
-                                                                    relu, out, ldy);
+            k_q8_stream<T, LINES, MB, W><<<grid, W * kWave, 0, st>>>(n, m, k, qt, ldq, sr, p, ldp,
+                                                                    t, relu, out, ldy);
             return hipGetLastError();
         };
         // The most channels a workgroup that leave every compute unit one (us, 256

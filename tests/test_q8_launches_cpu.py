@@ -1,0 +1,90 @@
+"""Which rows each launch of the calls on rows held in 8 bits is handed, on the
+CPU: the host half of the kernels' file over a runtime that records launches
+(``recorded_launches.cpp``).  A call's rows go to the kernels in turns of 2^21;
+every turn starts where the one before ended."""
+import ctypes
+import os
+import subprocess
+
+import numpy as np
+import pytest
+
+from conftest import ROOT
+from paper_2206_00057_amd import build as B
+from paper_2206_00057_amd import digest as D
+
+TURN = 2 ** 21
+# fake addresses, far apart and never read
+X, Q, S, R, P, T, Y = [(i + 1) << 48 for i in range(7)]
+
+
+@pytest.fixture(scope="module")
+def library(tmp_path_factory):
+    d = tmp_path_factory.mktemp("launches")
+    obj, lib = str(d / "q8_kernels.o"), str(d / "libdigest_launches.so")
+    tests = os.path.join(ROOT, "tests")
+    subprocess.run([os.path.join(B.ROCM, "bin", "hipcc"), *B.HIPCC_FLAGS, "--offload-host-only",
+                    "-fuse-cuid=none", "-w", "-O1", "-c", os.path.join(B.CSRC, "q8_kernels.hip"),
+                    "-o", obj], check=True)
+    subprocess.run(["g++", *B.CXX_FLAGS, "-fopenmp", "-shared", "-Wl,-Bsymbolic",
+                    os.path.join(B.CSRC, "digest_host.cpp"), os.path.join(B.CSRC, "digest_q8.cpp"),
+                    os.path.join(tests, "host_kernels.cpp"),
+                    os.path.join(tests, "recorded_launches.cpp"), obj, "-o", lib], check=True)
+    return lib
+
+
+@pytest.fixture
+def launches(library, monkeypatch):
+    """The library, and what it has launched since the last call: rows, input,
+    scales, output, list of each."""
+    monkeypatch.setattr(D, "LIB_PATH", library)
+    monkeypatch.setattr(D, "_lib", None)
+    L = D._q8_lib()
+
+    def recorded():
+        out = np.zeros((64, 5), np.int64)
+        n = L.recorded_launches(out.ctypes.data_as(ctypes.c_void_p), 64)
+        return out[:n].tolist()
+    yield L, recorded
+    monkeypatch.undo()
+    D._q8 = None
+
+
+def turns(n):
+    return [(r, min(TURN, n - r)) for r in range(0, n, TURN)]
+
+
+ROWS = [1, TURN, TURN + 1, 2 * TURN + 77, 3 * TURN + 77, 5 * TURN]
+
+
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("t", [D.F32, D.BF16])
+# (weights in LDS; tiles of 64, 128 and 256 channels)
+@pytest.mark.parametrize("k,m", [(16, 5), (256, 256), (700, 300), (1024, 40), (1024, 100),
+                                 (1024, 600)])
+def test_product(launches, n, k, m, t):
+    L, recorded = launches
+    ldp, ldy = D.digest_q8_stride(k), m + 3
+    ldq = ldp + 16
+    assert L.digest_q8_product(n, k, m, Q, ldq, S, P, ldp, T, D.ACT_RELU, t, Y, ldy, None) == D.OK
+    size = 4 if t == D.F32 else 2
+    assert recorded() == [[c, Q + r * ldq, S + 4 * r, Y + size * r * ldy, 0] for r, c in turns(n)]
+
+
+@pytest.mark.parametrize("n", ROWS)
+@pytest.mark.parametrize("t", [D.F32, D.F16])
+@pytest.mark.parametrize("d", [20, 5000])
+@pytest.mark.parametrize("listed", [False, True])
+def test_rows_into_codes_and_back(launches, n, d, t, listed):
+    L, recorded = launches
+    ldx, ldq, size = d + 1, D.digest_q8_stride(d) + 16, 4 if t == D.F32 else 2
+    rows, n_x = (R, 50) if listed else (None, 0)
+    take = lambda a, step: a if listed else a + step
+    lists = lambda r: R + 8 * r if listed else 0
+    assert L.digest_quantize_rows(n, d, t, X, ldx, rows, n_x, Q, ldq, S, None) == D.OK
+    assert recorded() == [[c, take(X, size * r * ldx), S + 4 * r, Q + r * ldq, lists(r)]
+                          for r, c in turns(n)]
+    for ldy in (d, d + 1):
+        assert L.digest_dequantize_rows(n, d, Q, ldq, S, rows, n_x, t, Y, ldy, None) == D.OK
+        assert recorded() == [[c, take(Q, r * ldq), take(S, 4 * r), Y + size * r * ldy, lists(r)]
+                              for r, c in turns(n)]
