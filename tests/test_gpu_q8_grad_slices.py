@@ -1,0 +1,114 @@
+"""The weight gradient of rows held in 8 bits, in slices of the rows: every tile
+shape and the variant element by element, on gradients that are nonzero in few
+rows, so that the bound is a few roundings, and with values that are not finite.
+
+A term s D q: s D rounded once, u = 2^-24; it is held as three parts whose products
+by q are exact and added one after another, each at most 2 u of the sum (which
+may cut off); c terms and their slices' sums: (1 + 6 c + c) u of the terms'
+magnitudes.  (Without the last part a term is off by up to 2^-16 of itself, 256 u.)
+"""
+import pytest
+import torch
+
+from paper_2206_00057_amd import digest as D
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+ACTS = [D.ACT_IDENTITY, D.ACT_RELU]
+# codes' and D's columns: each pair of tile sides, some filled and some not; fewer
+# than four columns of D go element by element
+SIDES = [(100, 50), (128, 64), (17, 90), (100, 200), (300, 50), (256, 100), (602, 256), (300, 300),
+         (130, 1), (300, 2), (40, 3)]
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def random_codes(n, d, g):
+    codes = torch.zeros(n, D.digest_q8_stride(d), dtype=torch.int8, device="cuda")
+    codes[:, :d] = torch.randint(-127, 128, (n, d), generator=g, device="cuda").to(torch.int8)
+    return codes, torch.exp(torch.randn(n, generator=g, device="cuda")) * 1e-2
+
+
+def run(q, s, dy, y, k):
+    n, m = dy.shape
+    ws = torch.full((D.digest_q8_weight_grad_query(n, k, m),), 255, dtype=torch.uint8,
+                    device="cuda")
+    dw = torch.full((k, m), 7.0, device="cuda")
+    D.digest_q8_weight_grad(q, s, dy, dw, ws, ACTS[y is not None], y)
+    return dw
+
+
+def check_few_rows(q, s, dy, y, k, rows):
+    dw = run(q, s, dy, y, k)
+    r = torch.tensor(rows, device="cuda")
+    D64 = dy[r].double()
+    if y is not None:
+        D64 = D64 * (y[r] > 0)
+    a = q[r, :k].double() * s[r].double()[:, None]
+    want = torch.mm(a.t().contiguous(), D64)
+    size = torch.mm(a.abs().t().contiguous(), D64.abs())
+    err = (dw.double() - want).abs()
+    assert bool((err <= (1 + 7 * len(rows)) * U * size).all()), \
+        float((err / size.clamp_min(1e-30)).max() / U)
+
+
+@pytest.mark.parametrize("relu", [0, 1])
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("k,m", SIDES)
+def test_few_rows_of_many(k, m, t, relu):
+    for n in (1000, 5003):
+        g = gen(n + k + m)
+        q, s = random_codes(n, k, g)
+        for rows in ((0, n // 2, n - 1), (31, n // 3, n - 2), (n - 1,), (64, 32, n - 33)):
+            dy = torch.zeros(n, m, dtype=t, device="cuda")
+            dy[list(rows)] = torch.randn(len(rows), m, generator=g, device="cuda").to(t)
+            y = None
+            if relu:
+                y = torch.randn(n, m, generator=g, device="cuda").to(t)
+            check_few_rows(q, s, dy, y, k, rows)
+
+
+@pytest.mark.parametrize("relu", [0, 1])
+def test_few_rows_far_apart(relu):
+    """Rows 64 MB apart, element by element for the offsets' sake."""
+    n, k, m, ld = 700, 50, 90, 2 ** 25
+    g = gen(3)
+    q, s = random_codes(n, k, g)
+    whole = torch.empty(n * ld, dtype=torch.bfloat16, device="cuda").view(n, ld)
+    dy, y = whole[:, 5:5 + m], None
+    if relu:
+        y = whole[:, 1000:1000 + m]
+        y.copy_(torch.randn(n, m, generator=g, device="cuda"))
+    for rows in ((0, n // 2, n - 1), (31, n // 3, n - 2)):
+        dy.zero_()
+        dy[list(rows)] = torch.randn(len(rows), m, generator=g, device="cuda").bfloat16()
+        check_few_rows(q, s, dy, y, k, rows)
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1000, 5003])
+@pytest.mark.parametrize("k,m", [(40, 70), (100, 50), (300, 300), (602, 256), (130, 3)])
+def test_not_finite(k, m, n, t):
+    g = gen(n + m)
+    q, s = random_codes(n, k, g)
+    q[n - 1, :k] = 0                                  # (a zero code keeps its row's NaN)
+    dy = torch.randn(n, m, generator=g, device="cuda").to(t)
+    dy[5, 0], dy[n - 1, m - 1], dy[n // 2, 1] = float("inf"), float("nan"), float("-inf")
+    dw = run(q, s, dy, None, k)
+    cols = torch.isnan(dw).all(0)
+    assert cols.nonzero()[:, 0].tolist() == sorted({0, 1, m - 1})
+    assert bool(torch.isfinite(dw[:, ~cols]).all())
+    # what a mask leaves out is zero, whatever it is
+    y = torch.ones_like(dy)
+    y[5, 0] = y[n - 1, m - 1] = y[n // 2, 1] = 0
+    dw = run(q, s, dy, y, k)
+    clean = torch.where(torch.isfinite(dy), dy, torch.zeros_like(dy))
+    assert torch.equal(dw, run(q, s, clean, y, k)) and bool(torch.isfinite(dw).all())
+    y[:] = 0                                          # a mask that leaves nothing
+    assert bool((run(q, s, dy, y, k) == 0).all())
+    for r in (7, n - 1):                              # a row of NaN, the last one too
+        bad = s.clone()
+        bad[r] = float("nan")
+        assert bool(torch.isnan(run(q, bad, torch.ones_like(dy), None, k)).all())
