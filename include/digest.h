@@ -669,9 +669,11 @@ digest_status digest_partition_set_keep_mode(digest_partition *p, int32_t mode);
  * h_in + P_out halo_buf[layer-1] aggregated in fp32 and held in 8 bits (Q),
  * W given by its columns in 8 bits (digest_quantize_columns of W [d_{layer-1},
  * d_layer]).  Always aggregates first.  Needs DIGEST_KEEP_Q8: Q(AH) is what is
- * kept, so that the layer's backward (digest_layer_backward[_halo], with the
- * fp32 W) takes dw from the same rows; roundings count as constants (the
- * gradient of the values goes through to AH and W).
+ * kept, so that the layer's backward (digest_layer_backward[_halo]) takes dw
+ * from the same rows.  Its dh_in and dh_halo are taken with the fp32 W that it
+ * is given: with the values that w_codes and w_scales stand for they are the
+ * gradients of this product, its roundings as constants; with the W that was
+ * quantised, D W^T is off by at most sum_j |D[r][j]| w_scales[j] / 2.
  *   w_codes  device [d_layer, DIGEST_Q8_STRIDE(d_{layer-1})], contiguous;
  *   w_scales device [d_layer];  other arguments as for digest_layer_forward.
  * Errors: those of digest_layer_forward; DIGEST_ESTATE without DIGEST_KEEP_Q8.

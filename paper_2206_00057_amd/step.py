@@ -35,6 +35,26 @@ def q8_rows(n, width, device="cuda"):
             torch.zeros(n, dtype=torch.float32, device=device))
 
 
+class Q8Weight:
+    """A weight matrix W [d_in, d_out] in 8 bits: its columns' codes and scales,
+    which the product takes, and the values [d_in, d_out] that they stand for,
+    which the input gradients are taken with."""
+
+    def __init__(self, d_in, d_out, device="cuda"):
+        self.codes, self.scales = q8_rows(d_out, d_in, device)
+        self.values = torch.zeros(d_in, d_out, dtype=torch.float32, device=device)
+        self.columns = torch.zeros(d_out, d_in, dtype=torch.float32, device=device)
+
+    def set(self, W, stream=None):
+        """Hold W."""
+        D.digest_quantize_columns(W, self.codes, self.scales, stream=stream)
+        D.digest_dequantize_rows(self.codes, self.scales, self.columns, stream=stream)
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream)
+        with torch.cuda.stream(stream):
+            self.values.copy_(self.columns.t())
+
+
 def pull(p, level, store, stream=None):
     """digest_pull out of a level's store: floats, or (codes, scales)."""
     if isinstance(store, tuple):
@@ -61,8 +81,10 @@ class GpuPartition:
         H[l] = relu(norm(Z[l])) with Z[l] the layer's own output.
         keep: "q8" holds the aggregated inputs that the backward reads in 8
         bits; product: "q8" (with keep "q8") also multiplies them by W's
-        columns in 8 bits, which layer_forward quantises each time.  Stores
-        are float32 tensors, or (codes, scales) of q8_rows.
+        columns in 8 bits, which layer_forward quantises each time; the
+        layer's backward takes its input gradients with the values that it
+        multiplied by.  Stores are float32 tensors, or (codes, scales) of
+        q8_rows.
         pull_mode: what a pull keeps (D.PULL_ROWS or D.PULL_AGGREGATE); by
         default the halo aggregate alone for the GCN layer, the halo rows
         for the GAT layer, which reads them."""
@@ -118,8 +140,9 @@ class GpuPartition:
                 max([D.digest_layer_norm_query(n, self.widths[l]) for l in hidden] + [256]),
                 dtype=torch.uint8, device=device)
         if product == "q8":
-            self.Wq = [None] + [q8_rows(self.widths[l], self.widths[l - 1], device)
+            self.Wq = [None] + [Q8Weight(self.widths[l - 1], self.widths[l], device)
                                 for l in range(1, self.L + 1)]
+            self.held = list(self.Wq)   # what each layer's last forward multiplied by
         self.loss = torch.zeros(1, **f32)
         self.graphs = {}
         # pulls and pushes: on their own stream (default priority) next to the
@@ -135,8 +158,8 @@ class GpuPartition:
         return self.norms is not None and layer < self.L
 
     def layer_forward(self, l, h, W, stream=None, Wq=None):
-        """H[l] from the rows h of level l-1; Wq: W's columns in 8 bits, where
-        they are at hand (product "q8")."""
+        """H[l] from the rows h of level l-1; Wq: the Q8Weight that holds W,
+        where it is at hand (product "q8")."""
         normed = self.normed(l)
         out, act = (self.Z[l], D.ACT_IDENTITY) if normed else (self.H[l], self.act(l))
         if self.model == "gat":
@@ -144,8 +167,9 @@ class GpuPartition:
         elif self.product == "q8":
             if Wq is None:
                 Wq = self.Wq[l]
-                D.digest_quantize_columns(W, *Wq, stream=stream)
-            D.digest_layer_forward_q8(self.p, l, h, *Wq, out, act, stream=stream)
+                Wq.set(W, stream=stream)
+            self.held[l] = Wq
+            D.digest_layer_forward_q8(self.p, l, h, Wq.codes, Wq.scales, out, act, stream=stream)
         else:
             D.digest_layer_forward(self.p, l, h, W, out, act, stream=stream)
         if normed:
@@ -156,8 +180,11 @@ class GpuPartition:
     def layer_backward(self, l, h_in, W, dh_in, dh_halo=None):
         """dW[l] (with the norm's and the attention's gradients) and dh_in, if
         not None, from dH[l], which a normalised layer replaces by dZ[l];
-        dh_halo: also the halo rows' gradient (GCN layers)."""
+        dh_halo: also the halo rows' gradient (GCN layers).  With product
+        "q8" the values that the forward multiplied by take W's place."""
         out = self.H[l]
+        if self.product == "q8":
+            W = self.held[l].values
         if self.normed(l):
             out = self.Z[l]
             D.digest_layer_norm_backward(out, self.norms[l - 1][0], self.H[l], self.dH[l],

@@ -40,7 +40,9 @@ parameters' state (`momenta`, zero at the start).
 store="q8" holds the stale levels of the store in 8 bits (a scale and whole
 numbers for each row), keep="q8" the aggregated inputs that the backward reads,
 product="q8" also multiplies those by the weights' columns in 8 bits (weights
-and gradients stay float32; roundings count as constants).
+and gradients stay float32).  The gradients are those of the products that ran,
+with the roundings as constants: a weight's from the rows as they are held, an
+input's and a halo row's with the weights as they are held.
 
 All arithmetic runs in libdigest.so (the layers, pulls, pushes, loss heads
 and the parameter averaging); this module owns the buffers and orders the
@@ -51,7 +53,7 @@ from __future__ import annotations
 import torch
 
 from . import digest as D
-from .step import GpuPartition, pull, push, q8_rows
+from .step import GpuPartition, Q8Weight, pull, push, q8_rows
 
 
 def boundary_push_mode(gps, parts):
@@ -112,8 +114,8 @@ class DigestTrainer:
         self.stores = [x] + [q8_rows(n_global, self.widths[l], device) if store == "q8" else
                              torch.zeros(n_global, self.widths[l], **f32)
                              for l in range(1, self.L)]
-        # the weights' columns in 8 bits, formed once a round for all subgraphs
-        self.Wq = ([q8_rows(self.widths[l], self.widths[l - 1], device)
+        # the weights in 8 bits, formed once a round for all subgraphs
+        self.Wq = ([Q8Weight(self.widths[l - 1], self.widths[l], device)
                     for l in range(1, self.L + 1)] if product == "q8" else [None] * self.L)
         self.losses = torch.zeros(len(parts), **f32)
         if optimizer == "muon":
@@ -165,7 +167,7 @@ class DigestTrainer:
     def _quantize_weights(self):
         for w, wq in zip(self.W, self.Wq):
             if wq is not None:
-                D.digest_quantize_columns(w, *wq)
+                wq.set(w)
 
     def _round(self, do_pull, do_push):
         self._quantize_weights()

@@ -5,7 +5,7 @@ rows, so that the bound is a few roundings, and with values that are not finite.
 A term s D q: s D rounded once, u = 2^-24; it is held as three parts whose products
 by q are exact and added one after another, each at most 2 u of the sum (which
 may cut off); c terms and their slices' sums: (1 + 6 c + c) u of the terms'
-magnitudes.  (Without the last part a term is off by up to 2^-16 of itself, 256 u.)
+magnitudes.  (Without the last part a term is off by up to 2^-15 of itself, 512 u.)
 """
 import pytest
 import torch
