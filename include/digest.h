@@ -708,7 +708,9 @@ const char *digest_profile_kernel_name(int32_t kind);
 
 /*
  * Launch plan of one layer as the library runs it (host only; a pure
- * function of the partition's sizes and widths), for tests and measurement.
+ * function of the partition's sizes and widths and of its keep mode), for
+ * tests and measurement; a layer run by digest_layer_forward_q8 aggregates
+ * first, in a pass of its own.
  * The two products of Eq. 5 associate either way; the plan records which
  * order and which kernels the layer calls use.
  *   transform_first     1: an identity layer runs as P_m ([h_in; halo] W)
@@ -718,7 +720,8 @@ const char *digest_profile_kernel_name(int32_t kind);
  *                       kernel (W held in LDS); 0: the MFMA GEMM, or the
  *                       fused pass when forward_fused is 1.
  *   dw_slices           split-K slices of the weight gradient, summed in
- *                       slice order (1: no split).
+ *                       slice order (1: no split); with DIGEST_KEEP_Q8 and
+ *                       aggregate-first those of digest_q8_weight_grad.
  *   dgrad_narrow_first  aggregate-first layers: 1 if the input gradient is
  *                       (P_in^T D) W^T (aggregated at width d_layer), 0 if
  *                       P_in^T (D W^T).
@@ -791,9 +794,11 @@ digest_status digest_partition_plan(const digest_partition *p, int32_t layer,
 /*
  * Algorithmic cost of one launch of each instrumented (kernel kind, slot),
  * indexed like digest_profile_read, for the launches that one round of the
- * GCN layers (model DIGEST_MODEL_GCN: every forward with act ReLU below
- * layer L and identity at L, the loss head, every backward with dh_in for
- * layers >= 2, the pulls of levels 0..L-1 and pushes of levels 1..L-1) or
+ * GCN layers (model DIGEST_MODEL_GCN: every digest_layer_forward with act
+ * ReLU below layer L and identity at L, the loss head, every backward with
+ * dh_in for layers >= 2, the pulls of levels 0..L-1 and pushes of levels
+ * 1..L-1, out of and into stores of floats; with DIGEST_KEEP_Q8 also the
+ * quantising of AH, and the weight gradients from its codes) or
  * of the GAT layers (DIGEST_MODEL_GAT) makes under the plan above:
  *   bytes    the bytes that must move if every operand is read once and
  *            every output written once (the compulsory traffic: a source

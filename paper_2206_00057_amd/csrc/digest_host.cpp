@@ -2995,7 +2995,10 @@ digest_layer_plan layer_plan(const digest_partition &p, int32_t layer)
                          digest::spmm_epilogue_ok(d_out, d_in, nullptr);
     } else {
         int32_t splits = 1, kchunk = 0;
-        splitk_plan(d_in, d_out, p.n_own, splits, kchunk);
+        if (p.keep == DIGEST_KEEP_Q8)
+            splits = p.q8->grad_slices(p.n_own, d_in, d_out);
+        else
+            splitk_plan(d_in, d_out, p.n_own, splits, kchunk);
         pl.dw_slices = splits;
         pl.dgrad_narrow_first = !relu && d_out < d_in;
         if (const TierPlan *t = find_tiers(p, Csr::InH, padded_width(d_in))) {
@@ -3118,10 +3121,17 @@ digest_status digest_profile_model(const digest_partition *p, int32_t model, dou
         if (p->widths[l - 1] % 4 &&   // the padded copy of h_in
             (pl.forward_fused || !use_sliced(*p, Csr::InH, p->widths[l - 1])))
             put(K_PAD_ROWS, l, 4 * n * (di + padded_width(p->widths[l - 1])));
-        put(K_GEMM_DW, l, 4 * (n * di + n * dout * (relu && !pl.backward_fused ? 2 : 1) + di * dout),
-            2 * n * di * dout);
-        if (pl.dw_slices > 1)
-            put(K_REDUCE_DW, l, 4 * (pl.dw_slices + 1) * di * dout);
+        // D, and what its mask reads, and dW; AH's codes and scales, or AH
+        const double dw = 4 * (n * dout * (relu && !pl.backward_fused ? 2 : 1) + di * dout);
+        if (p->keep == DIGEST_KEEP_Q8) {
+            const double held = n * digest::q8_padded(p->widths[l - 1]) + 4 * n;
+            put(K_QUANTIZE, l, 4 * n * di + held);
+            put(K_GEMM_DW, l, held + dw, 2 * n * di * dout);   // (with the slices' sum)
+        } else {
+            put(K_GEMM_DW, l, 4 * n * di + dw, 2 * n * di * dout);
+            if (pl.dw_slices > 1)
+                put(K_REDUCE_DW, l, 4 * (pl.dw_slices + 1) * di * dout);
+        }
         if (l > 1 && pl.backward_fused) {
             // D formed once; the long rows of P_in^T over D, then the fused
             // pass: the short rows' entries and distinct sources, the long

@@ -160,7 +160,8 @@ size_t grad_workspace(int64_t n_rows, int32_t d_in, int32_t d_out)
 
 constexpr digest::Q8Ops kOps = {digest::launch_quantize_rows, digest::launch_dequantize_rows,
                                 digest::launch_q8_aggregate, digest::launch_q8_product,
-                                digest::q8_grad_floats, digest::launch_q8_weight_grad};
+                                digest::q8_grad_floats, digest::q8_grad_slices,
+                                digest::launch_q8_weight_grad};
 
 }  // namespace
 

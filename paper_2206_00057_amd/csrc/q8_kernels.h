@@ -56,6 +56,8 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
 // dw[c][j] = sum_r q[r][c] s_r D[r][j], D = dy or dy 1[y > 0] (y not null);
 // part holds q8_grad_floats floats.
 size_t q8_grad_floats(int32_t n, int32_t k, int32_t m);
+// Slices of the rows that it sums, for rows of 4 to 65,536 floats or less apart.
+int32_t q8_grad_slices(int32_t n, int32_t k, int32_t m);
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
                                  int64_t ldq, const float *s, const void *dy, int64_t lddy,
                                  const void *y, int64_t ldy, float *part, float *dw,
@@ -69,6 +71,7 @@ struct Q8Ops {
     decltype(&launch_q8_aggregate) aggregate;
     decltype(&launch_q8_product) product;
     decltype(&q8_grad_floats) grad_floats;
+    decltype(&q8_grad_slices) grad_slices;
     decltype(&launch_q8_weight_grad) weight_grad;
 };
 digest_status partition_set_keep(digest_partition *p, int32_t mode, const Q8Ops *ops);

@@ -1564,6 +1564,11 @@ namespace {
 int grad_tile_c(int32_t k) { return k > 128 ? 256 : 128; }
 int grad_tile_j(int32_t m) { return m > 128 ? 256 : m > 64 ? 128 : 64; }
 
+int64_t grad_tiles(int32_t k, int32_t m, int tc, int tj)
+{
+    return (int64_t)((k + tc - 1) / tc) * ((m + tj - 1) / tj);
+}
+
 // Few rows go without slices (k_q8_grad_few), one workgroup for 64 x 64 of dw
 // (us with slices / without: 500 x 64 x 16 float32 9.5 / 7.2, 20 x 1,000 x 1,000 14 /
 // 6.1, 500 x 256 x 256 15.4 / 7.7, 1,000 x 1,024 x 1,024 bfloat16 27 / 15, 2,000 rows
@@ -1636,13 +1641,22 @@ size_t q8_grad_floats(int32_t n, int32_t k, int32_t m)
     size_t most = 0;
     const int sides[2][2] = {{grad_tile_c(k), grad_tile_j(m)}, {128, 64}};
     for (const auto &t : sides) {
-        const int64_t tiles = (int64_t)((k + t[0] - 1) / t[0]) * ((m + t[1] - 1) / t[1]);
+        const int64_t tiles = grad_tiles(k, m, t[0], t[1]);
         const int64_t splits = grad_splits(n, tiles, grad_blocks(t[0], t[1]) * kGradRows,
                                            tiles * t[0] * t[1]);
         if (splits > 1)
             most = std::max<size_t>(most, (size_t)(splits * tiles) * t[0] * t[1]);
     }
     return most;
+}
+
+int32_t q8_grad_slices(int32_t n, int32_t k, int32_t m)
+{
+    if (grad_few(n, k, m))
+        return 1;
+    const int tc = m < 4 ? 128 : grad_tile_c(k), tj = grad_tile_j(m);
+    const int64_t tiles = grad_tiles(k, m, tc, tj);
+    return grad_splits(n, tiles, grad_blocks(tc, tj) * kGradRows, tiles * tc * tj);
 }
 
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,

@@ -14,7 +14,8 @@ namespace {
 
 std::map<const void *, std::string> names;
 
-// A launch: its rows, and where the first of them lies in the arrays.
+// A launch: its rows, and where the first of them lies in the arrays; list is a
+// weight gradient's number of slices.
 struct Launch {
     int64_t rows, in, scales, out, list;
 };
@@ -27,15 +28,16 @@ struct Call {
 } pending;
 
 // Places of the arguments in a kernel's list: input, scales, output, row list
-// (-1: none).
+// (-1: none), slices.
 struct Kernel {
     const char *name;
-    int in, scales, out, list;
+    int in, scales, out, list, slices;
 };
 constexpr Kernel kernels[] = {
-    {"k_quantize_rows", 2, 8, 6, 4},   {"k_dequantize_rows", 2, 4, 7, 5},
-    {"k_dequantize_flat", 3, 5, 8, 6}, {"k_q8_few", 3, 5, 10, -1},
-    {"k_q8_gemm", 4, 6, 11, -1},       {"k_q8_stream", 3, 5, 10, -1},
+    {"k_quantize_rows", 2, 8, 6, 4, 0},   {"k_dequantize_rows", 2, 4, 7, 5, 0},
+    {"k_dequantize_flat", 3, 5, 8, 6, 0}, {"k_q8_fewI", 3, 5, 10, -1, 0},
+    {"k_q8_gemm", 4, 6, 11, -1, 0},       {"k_q8_stream", 3, 5, 10, -1, 0},
+    {"k_q8_gradI", 7, 9, 14, -1, 4},
 };
 
 }  // namespace
@@ -71,10 +73,14 @@ hipError_t hipLaunchKernel(const void *f, dim3 grid, dim3 block, void **args, si
         if (names[f].find(k.name) != std::string::npos) {
             auto at = [&](int i) { return *(const int64_t *)args[i]; };
             launches.push_back({*(const int32_t *)args[0], at(k.in), at(k.scales), at(k.out),
-                                k.list < 0 ? 0
-                                           : (int64_t)((const digest::RowList *)args[k.list])->p});
+                                k.slices     ? *(const int32_t *)args[k.slices]
+                                : k.list < 0 ? 0
+                                             : (int64_t)((const digest::RowList *)args[k.list])->p});
             return hipSuccess;
         }
+    if (names[f].find("k_q8_grad_few") != std::string::npos ||
+        names[f].find("k_q8_grad_sum") != std::string::npos)
+        return hipSuccess;
     return hipErrorInvalidDeviceFunction;
 }
 

@@ -36,7 +36,7 @@ def library(tmp_path_factory):
 @pytest.fixture
 def launches(library, monkeypatch):
     """The library, and what it has launched since the last call: rows, input,
-    scales, output, list of each."""
+    scales, output, list (or slices) of each."""
     monkeypatch.setattr(D, "LIB_PATH", library)
     monkeypatch.setattr(D, "_lib", None)
     L = D._q8_lib()
@@ -88,3 +88,56 @@ def test_rows_into_codes_and_back(launches, n, d, t, listed):
         assert L.digest_dequantize_rows(n, d, Q, ldq, S, rows, n_x, t, Y, ldy, None) == D.OK
         assert recorded() == [[c, take(Q, r * ldq), take(S, 4 * r), Y + size * r * ldy, lists(r)]
                               for r, c in turns(n)]
+
+
+def star(n, widths):
+    """n owned rows of one entry each, their own."""
+    return D.digest_partition_create(n, np.arange(n + 1), np.arange(n), np.ones(n, np.float32),
+                                     np.arange(n), np.zeros(0, np.int64), widths)
+
+
+@pytest.mark.parametrize("n,k,m", [(500, 64, 64), (513, 30, 64), (1000, 2, 3), (5000, 256, 256),
+                                   (20000, 300, 300), (29125, 602, 602), (60000, 100, 128),
+                                   (30, 4000, 4000)])
+def test_planned_slices(launches, n, k, m):
+    """digest_partition_plan's slices of a weight gradient from kept codes are the
+    call's."""
+    L, recorded = launches
+    p = star(n, [k, m, m])
+    D.digest_partition_set_keep_mode(p, D.KEEP_Q8)
+    pl = D.digest_partition_plan(p, 1)
+    assert pl["transform_first"] == 0
+    need = D.digest_q8_weight_grad_query(n, k, m)
+    assert L.digest_q8_weight_grad(n, k, m, Q, D.digest_q8_stride(k), S, D.F32, X, m, D.ACT_RELU, Y,
+                                   m, P, T, need, None) == D.OK
+    assert [r[4] for r in recorded()] == ([] if n <= 512 and k * m < 10 ** 6 else [pl["dw_slices"]])
+    assert pl["dw_slices"] == 1 or n > 512
+
+
+def test_modelled_costs():
+    """The cost model under both keep modes: rows of 100, 256 and 250 floats, the
+    last layer transform-first (no inputs kept)."""
+    n, widths = 20000, [100, 256, 250, 256, 5]
+    p = star(n, widths)
+    plain = D.digest_profile_model(p)
+    assert not any(key.startswith("quantize_rows") for key in plain)
+    D.digest_partition_set_keep_mode(p, D.KEEP_Q8)
+    kept = D.digest_profile_model(p)
+    for l in range(1, 5):
+        k, m = widths[l - 1:l + 1]
+        dw, rows = f"gemm_dw_splitk.l{l}", f"quantize_rows.l{l}"
+        if D.digest_partition_plan(p, l)["transform_first"]:
+            assert rows not in kept and kept[dw] == plain[dw]
+            assert kept[f"splitk_reduce_dw.l{l}"] == plain[f"splitk_reduce_dw.l{l}"]
+            continue
+        held = n * D.digest_q8_stride(k) + 4 * n
+        assert kept[rows] == (4 * n * k + held, 0, 0)
+        # the codes and scales in AH's place
+        assert kept[dw] == (plain[dw][0] - 4 * n * k + held, 2 * n * k * m, 0)
+        assert f"splitk_reduce_dw.l{l}" not in kept
+    assert D.digest_partition_plan(p, 4)["transform_first"] == 1
+    same = lambda d: {k: v for k, v in d.items()
+                      if not k.startswith(("gemm_dw", "quantize", "splitk"))}
+    assert same(plain) == same(kept)
+    D.digest_partition_set_keep_mode(p, D.KEEP_F32)
+    assert D.digest_profile_model(p) == plain
