@@ -660,7 +660,8 @@ digest_status digest_pull_q8(digest_partition *p, int32_t level, const int8_t *c
  * A change of mode changes the workspace that the handle needs and unbinds
  * it: query and bind it again.  Callers that capture graphs set the mode
  * before the capture.
- * Errors: DIGEST_EINVAL (NULL, unknown mode), DIGEST_ENOMEM (host memory).
+ * Errors: DIGEST_EINVAL (NULL, unknown mode), DIGEST_ENOMEM (host memory;
+ * the mode, the workspace and its binding are as before).
  */
 digest_status digest_partition_set_keep_mode(digest_partition *p, int32_t mode);
 

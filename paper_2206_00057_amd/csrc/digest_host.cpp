@@ -1825,14 +1825,19 @@ digest_status partition_set_keep(digest_partition *p, int32_t mode, const Q8Ops 
     if (mode == p->keep)
         return DIGEST_OK;
     const int32_t before = p->keep;
-    p->keep = mode;
-    p->q8 = ops;
     try {
-        plan_layout(*p);
+        auto planned = p->lay;
+        p->keep = mode;
+        p->q8 = ops;
+        try {
+            plan_layout(*p);
+        } catch (...) {
+            // (planned half way: the layout and the mode are as they were)
+            std::swap(p->lay, planned);
+            p->keep = before;
+            throw;
+        }
     } catch (const std::bad_alloc &) {
-        p->keep = before;
-        p->ws = nullptr;   // the layout may be half planned: nothing can be bound or run
-        p->lay.total = SIZE_MAX;
         return fail(DIGEST_ENOMEM, "host allocation failed");
     }
     p->ws = nullptr;

@@ -1,8 +1,11 @@
 // A HIP runtime that records the launches of the 8-bit rows' kernels instead of
 // making them: linked with the host half of csrc/q8_kernels.hip, so that what
-// each launch is handed is checked without a GPU.
+// each launch is handed is checked without a GPU.  Allocations of the host code
+// fail on request.
 #include <cstdint>
+#include <cstdlib>
 #include <map>
+#include <new>
 #include <string>
 #include <vector>
 
@@ -11,6 +14,8 @@
 #include "q8_kernels.h"
 
 namespace {
+
+long allocations_left = -1;   // before one fails (negative: none does)
 
 std::map<const void *, std::string> names;
 
@@ -42,7 +47,20 @@ constexpr Kernel kernels[] = {
 
 }  // namespace
 
+void *operator new(size_t n)
+{
+    if (allocations_left >= 0 && allocations_left-- == 0)
+        throw std::bad_alloc();
+    if (void *p = std::malloc(n ? n : 1))
+        return p;
+    throw std::bad_alloc();
+}
+void operator delete(void *p) noexcept { std::free(p); }
+void operator delete(void *p, size_t) noexcept { std::free(p); }
+
 extern "C" {
+
+void fail_allocation(long after) { allocations_left = after; }
 
 extern const char __hip_fatbin[8];
 const char __hip_fatbin[8] = {};

@@ -141,3 +141,35 @@ def test_modelled_costs():
     assert same(plain) == same(kept)
     D.digest_partition_set_keep_mode(p, D.KEEP_F32)
     assert D.digest_profile_model(p) == plain
+
+
+@pytest.mark.parametrize("first,then", [(D.KEEP_F32, D.KEEP_Q8), (D.KEEP_Q8, D.KEEP_F32)])
+def test_keep_mode_without_host_memory(launches, first, then):
+    """A change of the keep mode that finds no host memory changes nothing: the
+    partition stays bound in its mode and can change later."""
+    L, _ = launches
+    p, other = star(100, [64, 64, 5]), star(100, [64, 64, 5])
+    D.digest_partition_set_keep_mode(p, first)
+    D.digest_partition_set_keep_mode(other, then)
+    before = D.digest_partition_query(p)
+    assert before != D.digest_partition_query(other)
+    room = np.zeros(before["workspace_bytes"] + 256, np.uint8)
+    ws = ctypes.c_void_p((room.ctypes.data + 255) // 256 * 256)
+    assert L.digest_partition_bind_workspace(
+        p.handle, ws, ctypes.c_size_t(before["workspace_bytes"]), None) == D.OK
+    failed = 0
+    for after in range(64):
+        L.fail_allocation(ctypes.c_long(after))
+        st = L.digest_partition_set_keep_mode(p.handle, then)
+        L.fail_allocation(ctypes.c_long(-1))
+        if st == D.OK:
+            break
+        failed += 1
+        assert st == D.ENOMEM
+        assert D.digest_partition_query(p) == before
+        assert L.digest_partition_set_keep_mode(p.handle, first) == D.OK   # no change
+        assert D.digest_partition_query(p) == before
+        assert L.digest_pull_q8(p.handle, 0, None, None, None) == D.EINVAL  # (bound)
+    assert failed > 0 and st == D.OK
+    assert D.digest_partition_query(p) == D.digest_partition_query(other)
+    assert L.digest_pull_q8(p.handle, 0, None, None, None) == D.ESTATE      # (unbound)
