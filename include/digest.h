@@ -560,7 +560,9 @@ digest_status digest_muon_average(int32_t count, const int32_t *rows, const int3
  *   exact x_c / scale (ties to even),  value of element c: q_c scale.
  * A scale below the smallest normal number becomes 0 and its row zeros (rows
  * of zeros among them).  A row with a NaN or an infinity gets the scale NaN
- * and codes 0: it reads as NaN and touches no other row.
+ * and codes 0: it reads as NaN and touches no other row.  The scale is rounded,
+ * so that fp32's largest number itself reads back as an infinity (127 times
+ * its scale), every smaller one as a number.
  *   codes    device [n][ldq], 16-byte aligned, ldq a multiple of 16 of at
  *            least DIGEST_Q8_STRIDE(width); the columns from width up to that
  *            are written as zeros and must be zeros where codes are read by
@@ -652,11 +654,14 @@ digest_status digest_pull_q8(digest_partition *p, int32_t level, const int8_t *c
  * How the aggregated inputs AH that the layer forward keeps for the backward
  * are held (host-side state, no device work):
  *   DIGEST_KEEP_F32 (the default): as the floats that were multiplied by W.
- *   DIGEST_KEEP_Q8: in 8 bits, a quarter of the memory; the layers share the
- *     room of one AH in floats, and the weight gradient is formed from the
- *     codes (digest_q8_weight_grad).  The forward's outputs are unchanged, dw
- *     is that of the rounded AH.  Layers computed transform-first keep no AH
- *     (they read h_in again) and are unchanged, and so is the GAT layer.
+ *   DIGEST_KEEP_Q8: in 8 bits, a quarter of each AH; the layers share the room
+ *     of one AH in floats, and the weight gradient is formed from the codes
+ *     (digest_q8_weight_grad).  The forward's outputs are unchanged, dw is that
+ *     of the rounded AH.  Layers computed transform-first keep no AH (they
+ *     read h_in again) and are unchanged, and so is the GAT layer.  The
+ *     workspace has room for every layer's codes, as digest_layer_forward_q8
+ *     may run any of them, and for the weight gradients' partial sums: with
+ *     few aggregate-first layers it may be the larger one of the two modes.
  * A change of mode changes the workspace that the handle needs and unbinds
  * it: query and bind it again.  Callers that capture graphs set the mode
  * before the capture.
