@@ -41,8 +41,9 @@ hipError_t launch_dequantize_rows(int32_t type, int32_t n, int32_t d, const int8
                                   void *y, int64_t ldy, hipStream_t s);
 // out[r] = sum over row r's entries of val scale codes[col] for the rows that
 // the blocks name (as launch_spmm, the n_long long rows first); out is 16-byte
-// aligned, its rows ldo apart, a multiple of 4 and at least d, and written up
-// to the next multiple of 4 columns.
+// aligned, its rows ldo apart, a multiple of 4 and at least d; the columns from
+// d to the next multiple of 4 hold nothing that may be used (short rows' are
+// written, long rows' are not).
 struct SpmmBlock;
 hipError_t launch_q8_aggregate(const SpmmBlock *blocks, int32_t n_blocks, int32_t n_long,
                                const int32_t *rowptr, const int32_t *col, const float *val,
@@ -56,7 +57,7 @@ hipError_t launch_q8_product(int32_t type, int32_t n, int32_t m, int32_t k, cons
 // dw[c][j] = sum_r q[r][c] s_r D[r][j], D = dy or dy 1[y > 0] (y not null);
 // part holds q8_grad_floats floats.
 size_t q8_grad_floats(int32_t n, int32_t k, int32_t m);
-// Slices of the rows that it sums, for rows of 4 to 65,536 floats or less apart.
+// Slices of the rows that it sums, for contiguous dy and y.
 int32_t q8_grad_slices(int32_t n, int32_t k, int32_t m);
 hipError_t launch_q8_weight_grad(int32_t type, int32_t n, int32_t k, int32_t m, const int8_t *q,
                                  int64_t ldq, const float *s, const void *dy, int64_t lddy,

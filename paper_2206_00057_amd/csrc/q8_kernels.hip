@@ -106,9 +106,9 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[4], const Scale &sc)
 // A row in the registers of GL lanes (WAVES == 1, 64 / GL rows a wave) or of
 // WAVES waves of one workgroup, Q vectors of 16 bytes a lane: one reading of x,
 // four 16-byte loads a lane under way, and few lanes to find the largest of.
-// Bound by memory: 304,051 of 306,250 rows of 256 float32 82 us (4.8 TB/s), 16,384
-// x 4,096 bfloat16 40 us (5.0 TB/s); 304,051 x 47 float32, whose rows start
-// anywhere, 15 us.
+// Bound by memory: 304,051 of 306,250 rows of 256 float32 82 to 99 us (3.9 to 4.7
+// TB/s), 16,384 x 4,096 bfloat16 41 us (4.9 TB/s); 304,051 x 47 float32, whose
+// rows start anywhere, 16 us.
 template <class T, int GL, int Q, int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quantize_rows(
     int32_t n, int32_t d, const T *__restrict__ x, int64_t ldx, RowList src, int64_t n_x,
@@ -185,6 +185,9 @@ __global__ __launch_bounds__(WAVES == 1 ? kThreads : WAVES * kWave) void k_quant
 // of 16 rows of one of them, in registers (P > 0: one reading of w), or in two
 // passes (P == 0, rows past 16 P kColThreads / C).  A piece is 16 bytes of codes.
 // Bound by latency: 602 x 256 float32 4 us (17 with 256 threads and two passes).
+// Large weights, a call: 4,096 x 4,096 float32 26 us (3.2 TB/s), bfloat16 32 (1.6:
+// 32 bytes of each row a workgroup), 8,192 x 1,024 bfloat16 92 (0.3: two passes
+// over 64 workgroups).
 constexpr int kColThreads = 1024;
 template <class T, int C, int P>
 __global__ __launch_bounds__(kColThreads) void k_quantize_columns(
@@ -261,7 +264,7 @@ __global__ __launch_bounds__(kColThreads) void k_quantize_columns(
 }
 
 // Lanes and vectors as in k_quantize_rows, rows wider than their GL Q V columns
-// in several turns.  Bound by memory: 304,051 x 256 float32 in any order 66 us (5.9
+// in several turns.  Bound by memory: 304,051 x 256 float32 in any order 67 us (5.8
 // TB/s, the codes partly from the Infinity Cache), 16,384 x 4,096 bfloat16 32 us;
 // rows that are not whole vectors, 304,051 x 47, 31 us.  (A lane an element for
 // them, so that each is stored as one run: 44 us.)
@@ -376,9 +379,9 @@ __global__ __launch_bounds__(kThreads) void k_dequantize_flat(
 // by the latency of few random reads a row.  GL lanes take a row's 16 GL
 // columns.  Short rows (the blocks' runs of at most 8): all of one by GL
 // lanes, which first fetch GL entries with their scales at once and then the
-// entries' codes, U under way.  (A wave a row with the entries dealt to its
-// groups of lanes: 492 us against 260 for 304,051 rows of 256 columns with 7.5
-// entries each; from a float32 store 404.)
+// entries' codes, U under way.  304,051 rows of 256 columns with 7.5 entries each
+// 208 us and 34 for the long ones (259 a call; from a float32 store 404; a wave a
+// row with the entries dealt to its groups of lanes 492).
 template <int GL>
 __global__ __launch_bounds__(8 * GL) void k_q8_aggregate(
     const SpmmBlock *__restrict__ blocks, const int32_t *__restrict__ rowptr,
@@ -529,8 +532,9 @@ __device__ __forceinline__ void store_row(const int (&sum)[N], float sr,
 
 // Few rows: bound by reading the weight's codes, 16 MT channels and 16 NT rows a
 // workgroup, its W waves a share of k each, straight from memory; the waves'
-// sums, whole numbers, are added through LDS.  One row x 4,096 x 4,096 5.3 us (3.2
-// TB/s), 64 rows 12.
+// sums, whole numbers, are added through LDS.  One row x 4,096 x 4,096 5.4 us (3.1
+// TB/s: one wave's loads after another and the sum, for 3.3 at a copy's rate), 64
+// rows 12.
 template <class T, int MT, int NT, int W>
 __global__ __launch_bounds__(W *kWave) void k_q8_few(int32_t n, int32_t m, int32_t k,
                                                      const int8_t *__restrict__ q, int64_t ldq,
@@ -595,7 +599,7 @@ typedef __attribute__((address_space(3))) void lds_void;
 typedef const __attribute__((address_space(1))) void global_void;
 __device__ const uint4 kZeros = {0, 0, 0, 0};
 
-// A tile of BN rows x BM channels a workgroup, (64 TM) channels x 64 rows a wave
+// A tile of BN rows x BM channels a workgroup, 16 TM channels x 64 rows a wave
 // (WM x WN waves).  The channels are the instruction's rows, so that a lane
 // holds channels in a row of one output row.  Lines of 64 k of both operands
 // come straight into a ring of places in LDS: 16 rows of 64 bytes are a block
@@ -606,7 +610,7 @@ __device__ const uint4 kZeros = {0, 0, 0, 0};
 // With 16-bit outputs the channels of a pair of blocks are dealt to the block's
 // rows so that a lane holds eight in a row.
 //
-// 8,192 x 4,096 x 4,096 bfloat16 out at 256 x 256: 124 to 135 us, 2.0 to 2.2 P
+// 8,192 x 4,096 x 4,096 bfloat16 out at 256 x 256: 126 to 144 us, 1.9 to 2.2 P
 // operations a second; the matrix units are busy half the time at the 2.1 GHz that
 // the card's power leaves.  (Fragments read a line ahead, between the matrix
 // instructions: 145 against 152 us there, but 90 against 84 for 16,384 x 640 x 4,096;
@@ -734,7 +738,7 @@ __global__ __launch_bounds__(WM *WN *kWave) void k_q8_gemm(
 // bound by writing y.  The weight's codes stay in LDS (in the places of
 // k_q8_gemm), and each wave takes 16 rows after another straight from memory, the
 // next ones' codes under way while these are multiplied and stored; no barrier
-// after the first.  306,250 x 256 x 256 float32 out 81 to 87 us (4.5 to 4.8 TB/s),
+// after the first.  306,250 x 256 x 256 float32 out 80 to 91 us (4.3 to 4.9 TB/s),
 // 300,000 x 600 x 256 bfloat16 89 (3.8), 16,384 x 640 x 4,096 74 (1.2 P operations a
 // second, of which 27 to store y).
 // (Kept to 128 registers, two workgroups a compute unit: 121; stores past the
@@ -845,13 +849,14 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
 // lane 16 columns in a row of dw to store.
 //
 // Bound by memory where dw is small, by the matrix instructions where it is not:
-// 306,250 x 256 x 256 float32 with ReLU 145 us and 12 for the slices' sum (4.9
-// TB/s; 142 without the slices' stores), 16,384 x 1,024 x 4,096 bfloat16 310 to 350
-// us (1.2 to 1.3 PFLOP/s of three products each, what a large library product
-// reaches here).  Tried on the former: tiles of 128 x 128 288 us, 128 x 256 217, 256
+// 306,250 x 256 x 256 float32 with ReLU 142 to 169 us and 12 for the slices' sum
+// (4.2 to 5.0 TB/s), 16,384 x 1,024 x 4,096 bfloat16 328 to 400 us one after another
+// and about 298 between other work, and 17 (1.0 to 1.4 PFLOP/s of three products
+// each, by the clock that the card's power leaves; a large library product reaches
+// 1.1 to 1.25 here).  Tried on the former, 145 us at the time: tiles of 128 x 128 288 us, 128 x 256 217, 256
 // x 128 213 (each step costs about the same whatever the tile); a second set of
 // fetched registers 213 to 813 (spills, or waits that the compiler cannot count
-// over branches).  29,125 x 602 x 256: 42 us and 12; its 85 slices' stores and 11
+// over branches).  29,125 x 602 x 256: 43 us and 11; its 85 slices' stores and 11
 // steps of 2.4 us, in which operands, splitting and products take turns.
 constexpr int kGradRows = 32, kGradThreads = 512;
 // 32s of rows in a step: a step costs about the same whatever it holds.
