@@ -35,6 +35,12 @@ def q8_rows(n, width, device="cuda"):
             torch.zeros(n, dtype=torch.float32, device=device))
 
 
+def on_stream(stream):
+    """torch's own work on the stream of a call (None: the current one)."""
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int)
+                             else stream)
+
+
 class Q8Weight:
     """A weight matrix W [d_in, d_out] in 8 bits: its columns' codes and scales,
     which the product takes, and the values [d_in, d_out] that they stand for,
@@ -49,9 +55,7 @@ class Q8Weight:
         """Hold W."""
         D.digest_quantize_columns(W, self.codes, self.scales, stream=stream)
         D.digest_dequantize_rows(self.codes, self.scales, self.columns, stream=stream)
-        if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream)
-        with torch.cuda.stream(stream):
+        with on_stream(stream):
             self.values.copy_(self.columns.t())
 
 
@@ -139,10 +143,10 @@ class GpuPartition:
             self.norm_workspace = torch.empty(
                 max([D.digest_layer_norm_query(n, self.widths[l]) for l in hidden] + [256]),
                 dtype=torch.uint8, device=device)
-        if product == "q8":
-            self.Wq = [None] + [Q8Weight(self.widths[l - 1], self.widths[l], device)
-                                for l in range(1, self.L + 1)]
-            self.held = list(self.Wq)   # what each layer's last forward multiplied by
+        # product "q8": the layers' own room for W, made where it is needed, and
+        # what each layer's last forward multiplied by
+        self.Wq = [None] * (self.L + 1)
+        self.held = [None] * (self.L + 1)
         self.loss = torch.zeros(1, **f32)
         self.graphs = {}
         # pulls and pushes: on their own stream (default priority) next to the
@@ -166,6 +170,9 @@ class GpuPartition:
             D.digest_gat_forward(self.p, l, h, W, self.atts[l - 1], out, act, stream=stream)
         elif self.product == "q8":
             if Wq is None:
+                if self.Wq[l] is None:
+                    with on_stream(stream):
+                        self.Wq[l] = Q8Weight(*W.shape, device=self.device)
                 Wq = self.Wq[l]
                 Wq.set(W, stream=stream)
             self.held[l] = Wq
@@ -183,7 +190,7 @@ class GpuPartition:
         dh_halo: also the halo rows' gradient (GCN layers).  With product
         "q8" the values that the forward multiplied by take W's place."""
         out = self.H[l]
-        if self.product == "q8":
+        if self.held[l] is not None:
             W = self.held[l].values
         if self.normed(l):
             out = self.Z[l]

@@ -146,6 +146,7 @@ def test_trainer(exchange):
                              dev(synth.labels(cfg)), [dev(w) for w in synth.weights(cfg)], 0.1, 2,
                              store="q8", keep="q8", product="q8", grad_exchange=exchange)
     tr.init_stores()
+    assert not any(wq for gp in tr.gps for wq in gp.Wq)   # (all take the trainer's)
     for r in (1, 2, 3):
         values = [held(W)[2] for W in tr.W]
         tr.round(r)
@@ -162,3 +163,31 @@ def test_trainer(exchange):
                                                  values[l - 1], dw, dh, halo)
                     assert torch.equal(halo, tr.dh_halo[m][l - 1]) and bool(halo.any())
                 assert torch.equal(dw, gp.dW[l])
+
+
+def test_backward_before_a_forward():
+    cfg, g = tiny()
+    gp = step.GpuPartition(g.n, synth.make_partition(cfg, g, 0), cfg.widths, keep="q8",
+                           product="q8")
+    h, W = torch.zeros(gp.n_own, cfg.widths[1], device="cuda"), dev(synth.weights(cfg)[1])
+    with pytest.raises(D.DigestError) as e:
+        gp.layer_backward(2, h, W, gp.dH[1])
+    assert e.value.status == D.ESTATE
+
+
+def test_layer_on_another_stream():
+    """A layer's calls on a stream given as an object or as a number."""
+    cfg, g = tiny()
+    part = synth.make_partition(cfg, g, 0)
+    W, h = dev(synth.weights(cfg)[0]), dev(synth.features(cfg))[dev(part.owned)]
+    got = []
+    side = torch.cuda.Stream()
+    for stream in (None, side, side.cuda_stream):
+        gp = step.GpuPartition(g.n, part, cfg.widths, keep="q8", product="q8")
+        D.digest_pull(gp.p, 0, dev(synth.features(cfg)))
+        torch.cuda.synchronize()
+        gp.layer_forward(1, h, W, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(gp.held[1].values, held(W)[2])
+        got.append(gp.H[1].clone())
+    assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
