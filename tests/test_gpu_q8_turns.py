@@ -1,5 +1,6 @@
 """Calls on rows held in 8 bits over more rows than two launches take (2^21 each):
 every row is that row's, the ones around the launches' borders among them."""
+import numpy as np
 import pytest
 import torch
 
@@ -84,3 +85,33 @@ def test_rows_into_codes_and_back(listed):
         y = torch.full((N, ld), 9.0, device="cuda")
         D.digest_dequantize_rows(codes, scales, y[:, :d], rows=idx)
         assert torch.equal(y[:, :d], want) and bool((y[:, d:] == 9).all())
+
+
+def test_push_and_pull():
+    """A partition of more owned and halo rows than two launches take."""
+    n, n_halo, d = 2 * TURN + 77, 2 * TURN + 99, 9
+    # row r reads halo nodes r and, the last ones, r + n
+    rows = np.minimum(np.arange(n_halo), n - 1)
+    indptr = np.searchsorted(rows, np.arange(n + 1))
+    owned, halo = np.arange(n) * 2 + 1, np.arange(n_halo) * 2
+    p = D.digest_partition_create(2 * n_halo + 1, indptr, halo, np.ones(n_halo, np.float32), owned,
+                                  halo, [d, d, 2])
+    D.digest_partition_set_pull_mode(p, D.PULL_ROWS)
+    ws = torch.empty(p.workspace_bytes, dtype=torch.uint8, device="cuda")
+    D.digest_partition_bind_workspace(p, ws)
+    x = torch.randn(p.n_global, d, generator=gen(5), device="cuda")
+    codes = torch.empty(p.n_global, 16, dtype=torch.int8, device="cuda")
+    scales = torch.empty(p.n_global, device="cuda")
+    D.digest_quantize_rows(x, codes, scales)
+    to = torch.full_like(codes, 55), torch.full_like(scales, 3.0)
+    mine = torch.from_numpy(owned).cuda()
+    D.digest_push_q8(p, 1, x[mine], *to, D.PUSH_ALL_OWNED)
+    assert torch.equal(to[0][mine], codes[mine]) and torch.equal(to[1][mine], scales[mine])
+    rest = torch.ones(p.n_global, dtype=torch.bool, device="cuda")
+    rest[mine] = False
+    assert bool((to[0][rest] == 55).all()) and bool((to[1][rest] == 3).all())
+    D.digest_pull_q8(p, 1, codes, scales)
+    out = torch.empty(n_halo, d, device="cuda")
+    D.digest_partition_read_halo(p, 1, out)
+    theirs = torch.from_numpy(halo).cuda()
+    assert torch.equal(out, codes[theirs, :d].float() * scales[theirs, None])
