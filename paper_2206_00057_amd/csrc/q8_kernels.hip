@@ -853,11 +853,12 @@ __global__ __launch_bounds__(W *kWave) void k_q8_stream(
 // (4.2 to 5.0 TB/s), 16,384 x 1,024 x 4,096 bfloat16 328 to 400 us one after another
 // and about 298 between other work, and 17 (1.0 to 1.4 PFLOP/s of three products
 // each, by the clock that the card's power leaves; a large library product reaches
-// 1.1 to 1.25 here).  Tried on the former, 145 us at the time: tiles of 128 x 128 288 us, 128 x 256 217, 256
-// x 128 213 (each step costs about the same whatever the tile); a second set of
-// fetched registers 213 to 813 (spills, or waits that the compiler cannot count
-// over branches).  29,125 x 602 x 256: 43 us and 11; its 85 slices' stores and 11
-// steps of 2.4 us, in which operands, splitting and products take turns.
+// 1.1 to 1.25 here).  Tried on the former, 145 us at the time: tiles of 128 x 128
+// 288 us, 128 x 256 217, 256 x 128 213 (each step costs about the same whatever
+// the tile); a second set of fetched registers 213 to 813 (spills, or waits that
+// the compiler cannot count over branches).  29,125 x 602 x 256: 43 us and 11; its
+// 85 slices' stores and 11 steps of 2.4 us, in which operands, splitting and
+// products take turns.
 constexpr int kGradRows = 32, kGradThreads = 512;
 // 32s of rows in a step: a step costs about the same whatever it holds.
 constexpr int grad_blocks(int tc, int tj) { return tc * tj <= 16384 ? 2 : 1; }
